@@ -76,7 +76,8 @@ typedef enum {
     AQSGD_ERR_SHAPE = -5,     /* negative or overflowing batch / n_per / n_samples  */
     AQSGD_ERR_ALIGN = -6,     /* a pointer misses its alignment                     */
     AQSGD_ERR_LAUNCH = -7,    /* the HIP runtime refused the launch, or no memory   */
-    AQSGD_ERR_IO = -8         /* file tier: open / read / write failed              */
+    AQSGD_ERR_IO = -8,        /* file tier: open / read / write failed              */
+    AQSGD_ERR_WORKSPACE = -9  /* a workspace is missing or smaller than asked for    */
 } aqsgd_status;
 
 /* Shape and settings of one call (host memory). */
@@ -292,6 +293,124 @@ int aqsgd_grad_topk_quant(const aqsgd_desc* desc, int32_t keep, const void* grad
                           uint8_t* codes, float* scales, void* stream);
 int aqsgd_grad_topk_dequant(const aqsgd_desc* desc, int32_t keep, const uint8_t* bitmap,
                             const uint8_t* codes, const float* scales, void* out, void* stream);
+
+/*
+ * Products of 8-bit matrices: the linear layers on either side of a boundary, computed on
+ * 8-bit integers instead of on what they stand for.  A stage quantises its activations,
+ * weights and gradients with the same max-abs quantiser as the messages (Section 4.1), one
+ * scale for each token or channel, multiplies the codes exactly and applies the scales to
+ * the sums; the backward message of a token-wise scaled boundary is such a matrix already.
+ *
+ * Signed codes.  A vector v (a row or a column of the matrix) with s = max|v| is sent as
+ *     inv = RN(127 / s),  code = clamp(floor(RN(RN(v * inv) + r)), -127, 127)
+ * with r = 1/2 (nearest, ties upwards) or a uniform draw (stochastic), and stands for
+ * code * (s / 127).  s < 2^-120: scale 0, codes 0.  A vector with an infinity or a NaN in
+ * it: scale NaN, codes 0, so whatever is computed from it is NaN.
+ * Stochastic draws: Philox4x32-10, key = rng_seed, counter = (column / 4 + 2^30 for the row
+ * codes or + 2^31 for the column codes, row, 0, 0), word column % 4, u = (word >> 8) * 2^-24.
+ *
+ * A matrix of codes is int8 [vectors, aqsgd_quant8_stride(length)], one quantised vector
+ * per row, 16-byte aligned; the bytes of a row past the vector's length are zero (aqsgd_quant8
+ * writes them so, and the products below rely on it).
+ *
+ * aqsgd_quant8: x [rows, cols] of desc.dtype, ld elements from one row to the next.
+ *   row_codes   out  int8 [rows, aqsgd_quant8_stride(cols)], row_scales out float[rows]: every
+ *               row as one vector; both or neither NULL
+ *   col_codes   out  int8 [cols, aqsgd_quant8_stride(rows)], col_scales out float[cols]: every
+ *               column as one vector (the codes come out transposed); both or neither NULL
+ *   col_sums    out  float[cols], or NULL: sums of the columns of x itself, in binary32 (the
+ *               gradient of a bias); the same bits on every call
+ *   workspace   aqsgd_quant8_workspace_bytes() bytes of device memory, 16-byte aligned, free
+ *               for other use once the call's work has run; NULL where that is 0
+ * x and the float arrays need their element's alignment.  AQSGD_ERR_WORKSPACE if
+ * workspace_bytes is less than asked for.
+ */
+typedef struct {
+    int64_t rows, cols;   /* of x; 0 rows or columns: nothing happens                  */
+    int64_t ld;           /* elements between the rows of x, at least cols             */
+    int32_t dtype;        /* aqsgd_dtype of x                                          */
+    int32_t rounding;     /* aqsgd_round                                               */
+    uint64_t rng_seed;    /* key of the stochastic rounding                            */
+} aqsgd_quant8_desc;
+
+/* Bytes from one vector's codes to the next: its length rounded up to a multiple of 64 (0 for
+ * a negative or overflowing length). */
+size_t aqsgd_quant8_stride(int64_t length);
+size_t aqsgd_quant8_workspace_bytes(const aqsgd_quant8_desc* desc);
+int aqsgd_quant8(const aqsgd_quant8_desc* desc, const void* x, int8_t* row_codes, float* row_scales,
+                 int8_t* col_codes, float* col_scales, float* col_sums, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/*
+ * out[i, j] = dtype( sum_l a[i, l] * b[j, l]  (+ bias[j])  (+ add[i, j]) ),
+ * a and b standing for their codes and scales.  The sum over the codes is exact; scales
+ * (one factor of a, then one of b), bias and add follow in binary32, in this order, and the
+ * result is rounded once.
+ *   forward            a = row codes of the activations, b = row codes of the weight
+ *   gradient of input  a = row codes of the output's gradient, or its message,
+ *                      b = column codes of the weight
+ *   gradient of weight a = column codes of the output's gradient, b = column codes of the
+ *                      activations, add = out = the sum over the earlier micro-batches
+ *   a_codes    int8 [m, lda], lda = aqsgd_quant8_stride(k); with desc.message the uint8 codes of an
+ *              8-bit message with group == k (aqsgd_grad_quant), [m, k], k a multiple of 16
+ *              (else AQSGD_ERR_GROUP)
+ *   a_scales   float[m]
+ *   b_codes    int8 [n, aqsgd_quant8_stride(k)], b_scales float[n]
+ *   bias       [n] of desc.dtype, or NULL
+ *   add        [m, n] of desc.dtype, or NULL; may be out itself, and must not overlap it otherwise
+ *   out        out [m, n] of desc.dtype
+ * k = 0 is allowed: the sums are 0.  k is at most 131072, so that a sum fits 32 bits (else
+ * AQSGD_ERR_SHAPE).  Codes are 16-byte aligned, the rest needs its element's alignment.
+ *   workspace  as for aqsgd_quant8: aqsgd_matmul8_workspace_bytes(), partial sums where the
+ *              tokens and channels are few and k is long
+ */
+typedef struct {
+    int64_t m, n, k;      /* m or n 0: nothing happens                                 */
+    int32_t dtype;        /* aqsgd_dtype of out, bias and add                          */
+    int32_t message;      /* 0: a_codes are signed codes; 1: an 8-bit message's levels */
+} aqsgd_matmul8_desc;
+
+size_t aqsgd_matmul8_workspace_bytes(const aqsgd_matmul8_desc* desc);
+int aqsgd_matmul8(const aqsgd_matmul8_desc* desc, const void* a_codes, const float* a_scales,
+                  const int8_t* b_codes, const float* b_scales, const void* bias, const void* add,
+                  void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * First half of a feed-forward block in one kernel: the projections of the tokens on w
+ * (as aqsgd_matmul8, with bias), the activation, and with desc.gated its product with
+ * the second projection:
+ *     p = projections, binary32;   h = dtype(act(p[:, :f]) * p[:, f:])   or   dtype(act(p))
+ *   a_codes, a_scales  row codes of the tokens, [m, aqsgd_quant8_stride(k)]
+ *   w_codes, w_scales  row codes of the weights, [w, aqsgd_quant8_stride(k)], w = 2 f (the gate's
+ *              f rows first, then those it is multiplied with) or f
+ *   bias       [w] of desc.dtype, or NULL
+ *   h          out [m, f] of desc.dtype
+ *   pre        out [m, w] of desc.dtype, or NULL: dtype(p), for the backward pass
+ * aqsgd_ffn8_grad, the backward pass to the projections, in binary32 from the stored ones:
+ *     dpre[:, :f] = dtype(dh * pre[:, f:] * act'(pre[:, :f])),  dpre[:, f:] = dtype(dh * act(pre[:, :f]))
+ * or  dpre = dtype(dh * act'(pre));  from there aqsgd_quant8 and aqsgd_matmul8 lead on.
+ *   dh   in [m, f],  pre in [m, w],  dpre out [m, w] (may be pre itself), of desc.dtype; k is ignored
+ * Alignment and limits as for aqsgd_matmul8.  An activation outside the list: AQSGD_ERR_DTYPE.
+ */
+typedef enum {
+    AQSGD_ACT_SILU = 0,       /* x / (1 + exp(-x))                                            */
+    AQSGD_ACT_GELU = 1,       /* x / 2 * (1 + erf(x / sqrt(2)))                               */
+    AQSGD_ACT_GELU_TANH = 2   /* x / 2 * (1 + tanh(sqrt(2 / pi) * (x + 0.044715 x^3)))        */
+} aqsgd_act;
+
+typedef struct {
+    int64_t m, f, k;      /* tokens, width of h, width of the tokens                   */
+    int32_t dtype;        /* aqsgd_dtype of h, pre, bias, dh and dpre                  */
+    int32_t act;          /* aqsgd_act                                                 */
+    int32_t gated;        /* 0 or 1                                                    */
+    int32_t reserved;     /* 0                                                         */
+} aqsgd_ffn8_desc;
+
+int aqsgd_ffn8(const aqsgd_ffn8_desc* desc, const int8_t* a_codes, const float* a_scales,
+               const int8_t* w_codes, const float* w_scales, const void* bias, void* h, void* pre,
+               void* stream);
+int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre, void* dpre,
+                    void* stream);
 
 /*
  * Tiers below HBM for the previous messages (the implementation notes of Section 3.3

@@ -42,7 +42,8 @@ EXPORTS = ("aqsgd_codes_bytes", "aqsgd_scales_count", "aqsgd_encode", "aqsgd_dec
            "aqsgd_tier_prefetch",
            "aqsgd_tier_acquire", "aqsgd_tier_release", "aqsgd_tier_drain", "aqsgd_tier_destroy",
            "aqsgd_topk_bitmap_bytes", "aqsgd_topk_codes_bytes", "aqsgd_grad_topk_quant",
-           "aqsgd_grad_topk_dequant", "aqsgd_check_ids", "aqsgd_set_launch_shape",
+           "aqsgd_grad_topk_dequant", "aqsgd_quant8_stride", "aqsgd_quant8_workspace_bytes", "aqsgd_quant8",
+           "aqsgd_matmul8_workspace_bytes", "aqsgd_matmul8", "aqsgd_ffn8", "aqsgd_ffn8_grad", "aqsgd_check_ids", "aqsgd_set_launch_shape",
            "aqsgd_profile_next_launch", "aqsgd_strerror", "aqsgd_version")
 
 
@@ -63,6 +64,27 @@ class Job(ctypes.Structure):
                 ("scales", ctypes.c_void_p), ("out", ctypes.c_void_p), ("seen", ctypes.c_void_p),
                 ("first", ctypes.c_void_p), ("full", ctypes.c_void_p), ("stamp", ctypes.c_uint32),
                 ("reserved", ctypes.c_uint32)]
+
+
+class Quant8Desc(ctypes.Structure):
+    """Mirror of ``aqsgd_quant8_desc``."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("rounding", ctypes.c_int32), ("rng_seed", ctypes.c_uint64)]
+
+
+class Matmul8Desc(ctypes.Structure):
+    """Mirror of ``aqsgd_matmul8_desc``."""
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("message", ctypes.c_int32)]
+
+
+class Ffn8Desc(ctypes.Structure):
+    """Mirror of ``aqsgd_ffn8_desc``."""
+    _fields_ = [("m", ctypes.c_int64), ("f", ctypes.c_int64), ("k", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("gated", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
 class AqsgdError(RuntimeError):
@@ -118,6 +140,22 @@ def lib() -> ctypes.CDLL:
         L.aqsgd_grad_topk_quant.argtypes = [dp, ctypes.c_int32, vp, vp, vp, vp, vp]
         L.aqsgd_grad_topk_dequant.restype = ctypes.c_int
         L.aqsgd_grad_topk_dequant.argtypes = [dp, ctypes.c_int32, vp, vp, vp, vp, vp]
+        qp, mp, fp, size = (ctypes.POINTER(Quant8Desc), ctypes.POINTER(Matmul8Desc), ctypes.POINTER(Ffn8Desc),
+                            ctypes.c_size_t)
+        L.aqsgd_quant8_stride.restype = size
+        L.aqsgd_quant8_stride.argtypes = [ctypes.c_int64]
+        L.aqsgd_quant8_workspace_bytes.restype = size
+        L.aqsgd_quant8_workspace_bytes.argtypes = [qp]
+        L.aqsgd_quant8.restype = ctypes.c_int
+        L.aqsgd_quant8.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.aqsgd_matmul8_workspace_bytes.restype = size
+        L.aqsgd_matmul8_workspace_bytes.argtypes = [mp]
+        L.aqsgd_matmul8.restype = ctypes.c_int
+        L.aqsgd_matmul8.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.aqsgd_ffn8.restype = ctypes.c_int
+        L.aqsgd_ffn8.argtypes = [fp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.aqsgd_ffn8_grad.restype = ctypes.c_int
+        L.aqsgd_ffn8_grad.argtypes = [fp, vp, vp, vp, vp]
         L.aqsgd_tier_create.restype = ctypes.c_int
         L.aqsgd_tier_create.argtypes = [ctypes.POINTER(vp), vp, vp, vp, ctypes.c_int64, ctypes.c_int64,
                                         ctypes.c_int32, ctypes.c_int32]
@@ -504,6 +542,140 @@ def grad_topk_dequant(desc: Desc, keep: int, bitmap, codes, scales, out, stream=
     _raise(lib().aqsgd_grad_topk_dequant(ctypes.byref(desc), keep, _dev(bitmap, "bitmap"),
                                          _dev(codes, "codes"), _dev(scales, "scales"), _dev(out, "out"),
                                          _stream(stream)))
+
+
+# ---- products of 8-bit matrices ------------------------------------------------------------
+
+def _code(table: dict, what) -> int:
+    return table[what] if what in table else table[DTYPE_NAME[what]]
+
+
+def make_quant8_desc(*, rows: int, cols: int, dtype, ld: int | None = None, rounding: int = NEAREST,
+                     rng_seed: int = 0) -> Quant8Desc:
+    return Quant8Desc(rows, cols, cols if ld is None else ld, _code(DTYPE_CODE, dtype), rounding,
+                      rng_seed & 0xFFFFFFFFFFFFFFFF)
+
+
+def make_matmul8_desc(*, m: int, n: int, k: int, dtype, message: bool = False) -> Matmul8Desc:
+    return Matmul8Desc(m, n, k, _code(DTYPE_CODE, dtype), int(message))
+
+
+def make_ffn8_desc(*, m: int, f: int, k: int = 0, dtype, act: str = "silu", gated: bool = True) -> Ffn8Desc:
+    return Ffn8Desc(m, f, k, _code(DTYPE_CODE, dtype), ACT[act], int(gated), 0)
+
+
+def quant8_stride(length: int) -> int:
+    """Bytes of one vector's codes: ``length`` rounded up to a multiple of 64."""
+    return int(lib().aqsgd_quant8_stride(length))
+
+
+def quant8_workspace_bytes(desc: Quant8Desc) -> int:
+    return int(lib().aqsgd_quant8_workspace_bytes(ctypes.byref(desc)))
+
+
+def matmul8_workspace_bytes(desc: Matmul8Desc) -> int:
+    return int(lib().aqsgd_matmul8_workspace_bytes(ctypes.byref(desc)))
+
+
+def _here(what: str, t, dtype, shape) -> ctypes.c_void_p | None:
+    """The address of a contiguous tensor of this type and shape on the current device."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be of shape {tuple(shape)}, got {tuple(t.shape)}")
+    p = _dev(t, what)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the call is made on cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def _workspace(need: int, workspace, like, stream):
+    """``need`` bytes of device memory: the caller's, or some of the allocator's, which may go to
+    others only after the call's work on ``stream``."""
+    if need == 0:
+        return None, 0
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    else:
+        _want(workspace, "workspace", torch.uint8, need, exact=False)
+        _here("workspace", workspace, torch.uint8, workspace.shape)
+    return ctypes.c_void_p(workspace.data_ptr()), workspace.numel()
+
+
+def quant8(desc: Quant8Desc, x, *, row_codes=None, row_scales=None, col_codes=None, col_scales=None, col_sums=None,
+           workspace=None, stream=None) -> None:
+    """``aqsgd_quant8``: signed 8-bit codes of ``x`` [rows, cols] (row stride ``desc.ld``) with a scale for
+    each row (``row_codes`` [rows, stride(cols)] int8, ``row_scales`` [rows] float32) and / or each column
+    (``col_codes`` [cols, stride(rows)], ``col_scales`` [cols]), and the columns' sums (``col_sums`` [cols])."""
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    rows, cols = desc.rows, desc.cols
+    if x.dtype != _TORCH_OF_CODE[desc.dtype]:
+        raise ValueError(f"x must be {_TORCH_OF_CODE[desc.dtype]}, got {x.dtype}")
+    if tuple(x.shape) != (rows, cols):
+        raise ValueError(f"x must be of shape {(rows, cols)}, got {tuple(x.shape)}")
+    if not x.is_cuda or (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) != desc.ld):
+        raise ValueError(f"x must be a device tensor whose rows are contiguous and {desc.ld} elements apart")
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError(f"x is on {x.device}, the call is made on cuda:{torch.cuda.current_device()}")
+    args = [_here("row_codes", row_codes, torch.int8, (rows, quant8_stride(cols))),
+            _here("row_scales", row_scales, torch.float32, (rows,)),
+            _here("col_codes", col_codes, torch.int8, (cols, quant8_stride(rows))),
+            _here("col_scales", col_scales, torch.float32, (cols,)),
+            _here("col_sums", col_sums, torch.float32, (cols,))]
+    need = quant8_workspace_bytes(desc) if col_codes is not None or col_sums is not None else 0
+    ws, nbytes = _workspace(need, workspace, x, stream)
+    _raise(lib().aqsgd_quant8(ctypes.byref(desc), ctypes.c_void_p(x.data_ptr()), *args, ws, nbytes, _stream(stream)))
+
+
+def matmul8(desc: Matmul8Desc, a_codes, a_scales, b_codes, b_scales, out, *, bias=None, add=None, workspace=None,
+            stream=None) -> None:
+    """``aqsgd_matmul8``: ``out`` [m, n] of the matrices that ``a_codes`` [m, stride(k)] and ``b_codes``
+    [n, stride(k)] stand for (with ``desc.message``: the codes of an 8-bit message, ``m * k`` bytes, uint8)."""
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    td, m, n, k = _TORCH_OF_CODE[desc.dtype], desc.m, desc.n, desc.k
+    if desc.message:
+        _want(a_codes, "a_codes", torch.uint8, m * k, exact=False)
+        a = _here("a_codes", a_codes, torch.uint8, a_codes.shape)
+        _want(a_scales, "a_scales", torch.float32, m, exact=False)
+        sa = _here("a_scales", a_scales, torch.float32, a_scales.shape)
+    else:
+        a = _here("a_codes", a_codes, torch.int8, (m, quant8_stride(k)))
+        sa = _here("a_scales", a_scales, torch.float32, (m,))
+    b = _here("b_codes", b_codes, torch.int8, (n, quant8_stride(k)))
+    sb = _here("b_scales", b_scales, torch.float32, (n,))
+    rest = [_here("bias", bias, td, (n,)), _here("add", add, td, (m, n)), _here("out", out, td, (m, n))]
+    ws, nbytes = _workspace(matmul8_workspace_bytes(desc), workspace, out, stream)
+    _raise(lib().aqsgd_matmul8(ctypes.byref(desc), a, sa, b, sb, *rest, ws, nbytes, _stream(stream)))
+
+
+def ffn8(desc: Ffn8Desc, a_codes, a_scales, w_codes, w_scales, h, *, bias=None, pre=None, stream=None) -> None:
+    """``aqsgd_ffn8``: ``h`` [m, f] of a feed-forward block's first half; ``w_codes`` [2 f, stride(k)] (gate
+    first), or [f, stride(k)] where ``desc.gated`` is 0; ``pre`` [m, 2 f or f] takes the projections."""
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f
+    w, stride = f * (2 if desc.gated else 1), quant8_stride(desc.k)
+    _raise(lib().aqsgd_ffn8(
+        ctypes.byref(desc), _here("a_codes", a_codes, torch.int8, (m, stride)),
+        _here("a_scales", a_scales, torch.float32, (m,)), _here("w_codes", w_codes, torch.int8, (w, stride)),
+        _here("w_scales", w_scales, torch.float32, (w,)), _here("bias", bias, td, (w,)), _here("h", h, td, (m, f)),
+        _here("pre", pre, td, (m, w)), _stream(stream)))
+
+
+def ffn8_grad(desc: Ffn8Desc, dh, pre, dpre, *, stream=None) -> None:
+    """``aqsgd_ffn8_grad``: ``dpre`` [m, 2 f or f] from ``dh`` [m, f] and the stored projections ``pre``."""
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f
+    w = f * (2 if desc.gated else 1)
+    _raise(lib().aqsgd_ffn8_grad(ctypes.byref(desc), _here("dh", dh, td, (m, f)), _here("pre", pre, td, (m, w)),
+                                 _here("dpre", dpre, td, (m, w)), _stream(stream)))
 
 
 def check_ids(sample_ids, n_samples: int, flag, stream=None) -> None:

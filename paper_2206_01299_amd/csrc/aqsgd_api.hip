@@ -1294,6 +1294,7 @@ const char* aqsgd_strerror(int status) {
     case AQSGD_ERR_ALIGN:  return "a pointer misses its required alignment";
     case AQSGD_ERR_LAUNCH: return "the HIP runtime refused the kernel launch, or host memory ran out";
     case AQSGD_ERR_IO:     return "the file tier could not open, size, read or write its file";
+    case AQSGD_ERR_WORKSPACE: return "a workspace is missing or smaller than asked for";
     default:               return "unknown status";
     }
 }

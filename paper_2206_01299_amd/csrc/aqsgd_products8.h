@@ -1,0 +1,156 @@
+// What the 8-bit operators (aqsgd_quant8, aqsgd_matmul8, aqsgd_ffn8) share: the arguments of their
+// kernels, elements of any of the three types, the activations.
+#pragma once
+
+#include "aqsgd_kernels.h"
+
+namespace aqsgd {
+
+constexpr int kCodePad = 64;                     // vectors of codes start at multiples of this many bytes
+constexpr float kCodeHalf = 127.0f;              // largest signed code
+constexpr float kLevelHalf = 127.5f;             // half the top level of an 8-bit message
+constexpr int64_t kMaxSumLength = 131072;        // 131072 * 127 * 128 < 2^31
+
+inline int64_t code_stride(int64_t length) { return (length + kCodePad - 1) / kCodePad * kCodePad; }
+
+// Four consecutive elements at any element's address.
+typedef uint16_t u16x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ f32x4_t load4(int dtype, const void* base, int64_t idx) {
+    f32x4_t v;
+    if (dtype == AQSGD_F32) return *reinterpret_cast<const f32x4_any_t*>(static_cast<const float*>(base) + idx);
+    const u16x4_any_t r = *reinterpret_cast<const u16x4_any_t*>(static_cast<const uint16_t*>(base) + idx);
+    if (dtype == AQSGD_F16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(r[e])));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = bf16_bits_to_f32(r[e]);
+    }
+    return v;
+}
+
+__device__ __forceinline__ float load1(int dtype, const void* base, int64_t idx) {
+    if (dtype == AQSGD_F32) return load_elem<AQSGD_F32>(base, idx);
+    return dtype == AQSGD_F16 ? load_elem<AQSGD_F16>(base, idx) : load_elem<AQSGD_BF16>(base, idx);
+}
+
+__device__ __forceinline__ void store1(int dtype, void* base, int64_t idx, float v) {
+    if (dtype == AQSGD_F32) store_elem<AQSGD_F32>(base, idx, v);
+    else if (dtype == AQSGD_F16) store_elem<AQSGD_F16>(base, idx, v);
+    else store_elem<AQSGD_BF16>(base, idx, v);
+}
+
+typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
+
+__device__ __forceinline__ void store4(int dtype, void* base, int64_t idx, const f32x4_t& v) {
+    if (dtype == AQSGD_F32) {
+        *reinterpret_cast<f32x4_any_t*>(static_cast<float*>(base) + idx) = v;
+    } else if (dtype == AQSGD_F16) {
+        typedef _Float16 half4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+        half4_any_t h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(v[e]);
+        *reinterpret_cast<half4_any_t*>(static_cast<uint16_t*>(base) + idx) = h;
+    } else {
+        u32x2_any_t w;
+        w[0] = f32x2_to_bf16x2(v[0], v[1]);
+        w[1] = f32x2_to_bf16x2(v[2], v[3]);
+        *reinterpret_cast<u32x2_any_t*>(static_cast<uint16_t*>(base) + idx) = w;
+    }
+}
+
+// ---- activations ---------------------------------------------------------------------------
+constexpr float kSqrtHalf = 0.70710678118654752f;          // 1 / sqrt(2)
+constexpr float kDensity = 0.39894228040143268f;           // 1 / sqrt(2 pi)
+constexpr float kTanhSlope = 1.5957691216057308f;          // 2 sqrt(2 / pi)
+
+// p = 1 / (1 + exp(-x)) and q = 1 - p, both without a difference of nearly equal numbers and
+// without an exponential that overflows.
+__device__ __forceinline__ void sigmoids(float x, float& p, float& q) {
+    const float e = expf(-fabsf(x)), r = 1.0f / (1.0f + e), er = e * r;
+    p = x >= 0.0f ? r : er;
+    q = x >= 0.0f ? er : r;
+    if (x != x) p = q = x;
+}
+
+// (1 + tanh(y / 2)) / 2 is the sigmoid of y.
+__device__ __forceinline__ float tanh_argument(float x) { return kTanhSlope * (x + 0.044715f * x * x * x); }
+
+__device__ __forceinline__ float activation(int act, float x) {
+    if (act == AQSGD_ACT_GELU) return 0.5f * x * (1.0f + erff(x * kSqrtHalf));
+    float p, q;
+    sigmoids(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
+    return x * p;
+}
+
+// The activation's value and slope.
+__device__ __forceinline__ void activation_slope(int act, float x, float& value, float& slope) {
+    if (act == AQSGD_ACT_GELU) {
+        const float cdf = 0.5f * (1.0f + erff(x * kSqrtHalf));
+        value = x * cdf;
+        slope = cdf + x * (kDensity * expf(-0.5f * x * x));
+        return;
+    }
+    float p, q;
+    sigmoids(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
+    value = x * p;
+    if (act == AQSGD_ACT_SILU) {
+        slope = p + value * q;
+    } else {
+        const float near0 = fminf(fmaxf(x, -64.0f), 64.0f);      // beyond, p q is 0 and x^2 may be infinite
+        slope = p + near0 * (p * q) * (kTanhSlope * (1.0f + 0.134145f * near0 * near0));
+    }
+}
+
+// ---- the product's arguments -----------------------------------------------------------------
+enum ProductKind {
+    kPlain = 0,        // out = product (+ bias) (+ add)
+    kMessage,          // the same, a is a message's levels
+    kActivation,       // out = act(product + bias), pre = product + bias
+    kGated             // out = act(first half) * second half, pre = both
+};
+
+struct ProductArgs {
+    const uint8_t* a;
+    const int8_t* b;
+    const float* a_scales;
+    const float* b_scales;
+    const void* bias;
+    const void* add;
+    void* out;
+    void* pre;
+    int64_t lda, ldb;          // bytes
+    int32_t m, n, k;           // n: rows of b
+    int32_t dtype, act;
+};
+
+hipError_t launch_product(ProductKind kind, const ProductArgs& p, hipStream_t stream);
+
+// ---- the quantiser's -------------------------------------------------------------------------
+struct Quant8Args {
+    const void* x;
+    int8_t* row_codes;
+    float* row_scales;
+    int8_t* col_codes;
+    float* col_scales;
+    float* col_sums;
+    void* workspace;
+    int64_t ld, row_stride, col_stride;      // elements, bytes, bytes
+    int64_t rows, cols;
+    uint64_t seed;
+};
+
+int64_t quant8_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_quant8(int dtype, int rounding, const Quant8Args& a, hipStream_t stream);
+
+struct Ffn8GradArgs {
+    const void* dh;
+    const void* pre;
+    void* dpre;
+    int64_t m, f;
+    int32_t dtype, act, gated;
+};
+hipError_t launch_ffn8_grad(const Ffn8GradArgs& a, hipStream_t stream);
+
+}  // namespace aqsgd

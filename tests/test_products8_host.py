@@ -1,0 +1,185 @@
+"""The 8-bit operators as far as the host sees them: sizes, refusals before any launch, and the plain
+forms that the GPU tests compare with."""
+import ctypes
+from pathlib import Path
+
+import numpy as np
+import pytest
+import torch
+
+import products8_reference as R
+from paper_2206_01299_amd import binding as B
+
+OK = ctypes.c_void_p(4096)            # never followed
+NULL = None
+
+
+def q8(d, x=OK, rc=OK, rs=OK, cc=OK, cs=OK, sums=OK, ws=OK, n=1 << 40):
+    return B.lib().aqsgd_quant8(ctypes.byref(d) if d else None, x, rc, rs, cc, cs, sums, ws, n, None)
+
+
+def m8(d, a=OK, sa=OK, b=OK, sb=OK, bias=OK, add=OK, out=OK, ws=OK, n=1 << 40):
+    return B.lib().aqsgd_matmul8(ctypes.byref(d) if d else None, a, sa, b, sb, bias, add, out, ws, n, None)
+
+
+def f8(d, a=OK, sa=OK, w=OK, sw=OK, bias=OK, h=OK, pre=OK):
+    return B.lib().aqsgd_ffn8(ctypes.byref(d) if d else None, a, sa, w, sw, bias, h, pre, None)
+
+
+def g8(d, dh=OK, pre=OK, dpre=OK):
+    return B.lib().aqsgd_ffn8_grad(ctypes.byref(d) if d else None, dh, pre, dpre, None)
+
+
+def test_descriptors_match_the_header():
+    assert ctypes.sizeof(B.Quant8Desc) == 40 and B.Quant8Desc.rng_seed.offset == 32
+    assert ctypes.sizeof(B.Matmul8Desc) == 32 and B.Matmul8Desc.message.offset == 28
+    assert ctypes.sizeof(B.Ffn8Desc) == 40 and B.Ffn8Desc.gated.offset == 32
+    header = (Path(B.__file__).resolve().parent.parent / "include" / "aqsgd.h").read_text()
+    for name, value in B.ACT.items():
+        assert f"AQSGD_ACT_{name.upper()} = {value}" in header
+
+
+def test_strides():
+    assert [B.quant8_stride(n) for n in (0, 1, 63, 64, 65, 1600, 1601)] == [0, 64, 64, 64, 128, 1600, 1664]
+    assert B.quant8_stride(-1) == 0 and B.quant8_stride(2 ** 62) == 0
+
+
+def test_quant8_refusals():
+    d = B.make_quant8_desc(rows=16, cols=40, dtype="f16")
+    need = B.quant8_workspace_bytes(d)
+    assert need > 0
+    assert q8(None) == -1
+    for change, status in ((dict(rows=-1), -5), (dict(cols=-1), -5), (dict(ld=39), -5), (dict(dtype=3), -4),
+                           (dict(rounding=2), -4), (dict(rows=2 ** 31), -5), (dict(cols=2 ** 31, ld=2 ** 31), -5),
+                           (dict(ld=2 ** 62), -5), (dict(rows=2 ** 30, ld=2 ** 39), -5)):
+        bad = B.make_quant8_desc(rows=16, cols=40, dtype="f16")
+        for name, v in change.items():
+            setattr(bad, name, v)
+        assert q8(bad) == status, change
+        assert B.quant8_workspace_bytes(bad) == 0
+    for empty in (B.make_quant8_desc(rows=0, cols=40, dtype="f16"), B.make_quant8_desc(rows=16, cols=0, dtype="f16")):
+        assert B.lib().aqsgd_quant8(ctypes.byref(empty), None, None, None, None, None, None, None, 0, None) == 0
+    assert q8(d, x=NULL) == -1 and q8(d, rc=NULL) == -1 and q8(d, rs=NULL) == -1 and q8(d, cc=NULL) == -1
+    assert q8(d, cs=NULL) == -1
+    odd = ctypes.c_void_p(4097)
+    assert q8(d, x=odd) == -6 and q8(d, rc=ctypes.c_void_p(4104)) == -6 and q8(d, cc=ctypes.c_void_p(4104)) == -6
+    assert q8(d, rs=ctypes.c_void_p(4098)) == -6 and q8(d, sums=ctypes.c_void_p(4098)) == -6
+    assert q8(d, ws=ctypes.c_void_p(4104)) == -6
+    assert q8(d, ws=NULL) == -9 and q8(d, n=need - 1) == -9
+    assert q8(d, rc=NULL, rs=NULL, cc=NULL, cs=NULL, sums=NULL, ws=NULL, n=0) == 0      # nothing asked for
+    assert B.strerror(-9) != "unknown status"
+
+
+def test_matmul8_refusals():
+    d = B.make_matmul8_desc(m=16, n=40, k=48, dtype="bf16")
+    assert m8(None) == -1
+    for change, status in ((dict(m=-1), -5), (dict(n=-1), -5), (dict(k=-1), -5), (dict(k=131073), -5),
+                           (dict(m=2 ** 31), -5), (dict(m=2 ** 30, n=2 ** 30), -5), (dict(dtype=-1), -4),
+                           (dict(message=2), -4), (dict(message=1, k=40), -3)):
+        bad = B.make_matmul8_desc(m=16, n=40, k=48, dtype="bf16")
+        for name, v in change.items():
+            setattr(bad, name, v)
+        assert m8(bad) == status, change
+        assert B.matmul8_workspace_bytes(bad) == 0
+    for empty in (B.make_matmul8_desc(m=0, n=40, k=48, dtype="f16"), B.make_matmul8_desc(m=16, n=0, k=48, dtype="f16")):
+        assert B.lib().aqsgd_matmul8(ctypes.byref(empty), *[None] * 8, 0, None) == 0
+    for name in ("a", "sa", "b", "sb", "out"):
+        assert m8(d, **{name: NULL}) == -1, name
+    for name, at in (("a", 4104), ("b", 4104), ("sa", 4098), ("sb", 4098), ("bias", 4097), ("add", 4097), ("out", 4097)):
+        assert m8(d, **{name: ctypes.c_void_p(at)}) == -6, name
+
+
+def test_ffn8_refusals():
+    d = B.make_ffn8_desc(m=16, f=40, k=48, dtype="f32")
+    assert f8(None) == -1 and g8(None) == -1
+    for change, status in ((dict(m=-1), -5), (dict(f=-1), -5), (dict(f=2 ** 30), -5), (dict(f=2 ** 62), -5), (dict(k=131073), -5),
+                           (dict(dtype=3), -4), (dict(act=3), -4), (dict(act=-1), -4), (dict(gated=2), -4),
+                           (dict(reserved=1), -4)):
+        bad = B.make_ffn8_desc(m=16, f=40, k=48, dtype="f32")
+        for name, v in change.items():
+            setattr(bad, name, v)
+        assert f8(bad) == status and g8(bad) == status, change
+    empty = B.make_ffn8_desc(m=0, f=40, k=48, dtype="f32")
+    assert B.lib().aqsgd_ffn8(ctypes.byref(empty), *[None] * 8) == 0
+    assert B.lib().aqsgd_ffn8_grad(ctypes.byref(empty), *[None] * 4) == 0
+    for name in ("a", "sa", "w", "sw", "h"):
+        assert f8(d, **{name: NULL}) == -1, name
+    for name in ("dh", "pre", "dpre"):
+        assert g8(d, **{name: NULL}) == -1 and g8(d, **{name: ctypes.c_void_p(4098)}) == -6, name
+    for name, at in (("a", 4104), ("w", 4104), ("sa", 4098), ("sw", 4098), ("bias", 4098), ("h", 4098), ("pre", 4098)):
+        assert f8(d, **{name: ctypes.c_void_p(at)}) == -6, name
+
+
+def test_the_binding_checks_tensors_against_the_descriptor(monkeypatch):
+    """Host tensors stand in for device ones: the address is replaced, the checks before it are not."""
+    z = torch.zeros
+    d = B.make_matmul8_desc(m=4, n=6, k=70, dtype="f16")
+    good = dict(a=z(4, 128, dtype=torch.int8), sa=z(4), b=z(6, 128, dtype=torch.int8), sb=z(6), out=z(4, 6, dtype=torch.float16))
+
+    def call(**kw):
+        t = {**good, **kw}
+        B.matmul8(d, t["a"], t["sa"], t["b"], t["sb"], t["out"], bias=t.get("bias"), add=t.get("add"))
+
+    with pytest.raises(ValueError, match="device tensor"):
+        call()
+    bad = dict(a=[z(4, 70, dtype=torch.int8), z(4, 128, dtype=torch.uint8), z(5, 128, dtype=torch.int8)], sa=[z(3), z(4).double()],
+               b=[z(6, 192, dtype=torch.int8)], sb=[z(7)], out=[z(4, 6), z(6, 4, dtype=torch.float16)],
+               bias=[z(6), z(4, dtype=torch.float16)], add=[z(6, dtype=torch.float16), z(4, 6)])
+    monkeypatch.setattr(B, "_dev", lambda t, what: ctypes.c_void_p(0))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)          # a host tensor's index
+    monkeypatch.setattr(B, "_stream", lambda s: ctypes.c_void_p(0))
+    with pytest.raises(B.AqsgdError) as e:                                   # as far as the library's own check
+        call()
+    assert e.value.status == -1
+    for name, values in bad.items():
+        for v in values:
+            with pytest.raises(ValueError, match="must be"):
+                call(**{name: v})
+    message = B.make_matmul8_desc(m=4, n=6, k=64, dtype="f16", message=True)
+    with pytest.raises(ValueError, match="at least"):
+        B.matmul8(message, z(255, dtype=torch.uint8), z(4), z(6, 64, dtype=torch.int8), z(6), good["out"])
+    with pytest.raises(ValueError, match="must be"):
+        B.matmul8(message, z(256, dtype=torch.int8), z(4), z(6, 64, dtype=torch.int8), z(6), good["out"])
+    f = B.make_ffn8_desc(m=4, f=6, k=70, dtype="bf16")
+    w = z(12, 128, dtype=torch.int8)
+    for args in ((good["a"], good["sa"], w, z(12), z(4, 12, dtype=torch.bfloat16)), (good["a"], good["sa"], good["b"], z(12), z(4, 6, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError, match="must be of shape"):
+            B.ffn8(f, *args)
+    with pytest.raises(ValueError, match="must be of shape"):
+        B.ffn8_grad(f, z(4, 6, dtype=torch.bfloat16), z(4, 6, dtype=torch.bfloat16), z(4, 12, dtype=torch.bfloat16))
+    q = B.make_quant8_desc(rows=4, cols=70, dtype="f32")
+    for x in (z(4, 70).half(), z(4, 71), z(70, 4).t()):
+        with pytest.raises(ValueError):
+            B.quant8(q, x, row_codes=good["a"], row_scales=good["sa"])
+    with pytest.raises(KeyError):
+        B.make_ffn8_desc(m=4, f=6, k=70, dtype="bf16", act="relu")
+
+
+def test_the_plain_quantiser_by_hand():
+    """Ties go up, the largest value is +-127, a row below the floor and one that is not finite send zeros."""
+    x = np.zeros((5, 6), dtype=np.float32)
+    x[0] = [127, -127, 0.5, -0.5, 1.5, -1.5]
+    x[1] = 2.0 ** -121
+    x[2, 3] = np.inf
+    x[3, 1] = np.nan
+    x[4, 0] = -(2.0 ** -120)
+    codes, scales = R.quantise(x)
+    assert codes.shape == (5, 64) and not codes[:, 6:].any()
+    assert codes[0, :6].tolist() == [127, -127, 1, 0, 2, -1] and scales[0] == 127
+    assert scales[1] == 0 and not codes[1:4].any() and np.isnan(scales[2]) and np.isnan(scales[3])
+    assert scales[4] == np.float32(2.0 ** -120) and codes[4, 0] == -127
+
+
+def test_the_plain_draws_follow_the_published_generator(oracle):
+    """Words against the known-answer vector of an all-zero counter and key, and uniforms in [0, 1)."""
+    assert [hex(int(w)) for w in R.philox(0, 0, 0)] == ["0x6627e8d5", "0xe169c58d", "0xbc57ac4c", "0x9b00dbd8"]
+    u = R.draws(7, 9, 12345, True)
+    assert u.shape == (7, 9) and (u >= 0).all() and (u < 1).all() and not np.array_equal(u, R.draws(7, 9, 12345, False))
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_the_plain_slopes_are_the_differences_of_the_activations(kind):
+    x = np.linspace(-9, 9, 721)
+    h = 1e-5
+    assert np.abs((R.act(x + h, kind) - R.act(x - h, kind)) / (2 * h) - R.act_slope(x, kind)).max() < 1e-9
+    assert np.abs(R.act_slope(x, kind)).max() < R.STEEPEST
