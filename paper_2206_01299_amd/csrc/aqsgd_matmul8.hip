@@ -3,14 +3,16 @@
 
 namespace aqsgd {
 
+extern template hipError_t launch_product_dt<AQSGD_F32>(ProductTile, ProductKind, const ProductArgs&, hipStream_t);
+extern template hipError_t launch_product_dt<AQSGD_F16>(ProductTile, ProductKind, const ProductArgs&, hipStream_t);
+extern template hipError_t launch_product_dt<AQSGD_BF16>(ProductTile, ProductKind, const ProductArgs&, hipStream_t);
+
 hipError_t launch_product(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
-    const int64_t tiles = ((p.m + 63) / 64) * static_cast<int64_t>((p.n + 63) / 64);
-    const dim3 grid(static_cast<unsigned>(tiles)), block(256);
-    switch (kind) {
-    case kPlain:      return launch_kernel(product64_kernel<kPlain>, grid, block, stream, p);
-    case kMessage:    return launch_kernel(product64_kernel<kMessage>, grid, block, stream, p);
-    case kActivation: return launch_kernel(product64_kernel<kActivation>, grid, block, stream, p);
-    default:          return launch_kernel(product64_kernel<kGated>, grid, block, stream, p);
+    const ProductTile tile = static_cast<int64_t>(p.m) * p.n >= 256 * 256 * 128 ? kTile256 : kTile128;
+    switch (p.dtype) {
+    case AQSGD_F32:  return launch_product_dt<AQSGD_F32>(tile, kind, p, stream);
+    case AQSGD_F16:  return launch_product_dt<AQSGD_F16>(tile, kind, p, stream);
+    default:         return launch_product_dt<AQSGD_BF16>(tile, kind, p, stream);
     }
 }
 
