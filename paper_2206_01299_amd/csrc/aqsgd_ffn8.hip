@@ -1,30 +1,95 @@
-// Backward pass of a feed-forward block's first half, to the gradient of its projections.
+// Backward pass of a feed-forward block's first half, to the gradient of its projections: every element by
+// itself, read and written once, so memory bounds it; the activation is a constant of the kernel, and its
+// exponential and reciprocal are the hardware's, or arithmetic would weigh as much.
 #include "aqsgd_products8.h"
 
 namespace aqsgd {
 
-__global__ __launch_bounds__(256) void ffn8_grad_kernel(const Ffn8GradArgs a) {
-    const int64_t w = a.gated ? 2 * a.f : a.f, pieces = (a.f + 3) / 4, total = a.m * pieces;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t row = i / pieces, c = (i - row * pieces) * 4;
-        for (int64_t f = c; f < min(c + 4, a.f); ++f) {
-            const float d = load1(a.dtype, a.dh, row * a.f + f);
-            float value, slope;
-            activation_slope(a.act, load1(a.dtype, a.pre, row * w + f), value, slope);
-            if (a.gated) {
-                const float up = load1(a.dtype, a.pre, row * w + a.f + f);
-                store1(a.dtype, a.dpre, row * w + f, d * up * slope);
-                store1(a.dtype, a.dpre, row * w + a.f + f, d * value);
-            } else {
-                store1(a.dtype, a.dpre, row * w + f, d * slope);
-            }
+// Eight elements at any element's address, of which the first `count` exist.
+template <int DT>
+__device__ __forceinline__ void load_values(const void* base, int64_t at, int count, float (&f)[kChunk]) {
+    if (count >= kChunk) {
+        const char* p = static_cast<const char*>(base) + at * ElemBytes<DT>::value;
+        Raw<DT> r;
+        if constexpr (DT == AQSGD_F32) {
+            r.lo = *reinterpret_cast<const f32x4_any_t*>(p);
+            r.hi = *reinterpret_cast<const f32x4_any_t*>(p + 16);
+        } else {
+            r.v = *reinterpret_cast<const u32x4_any_t*>(p);
         }
+        unpack_raw<DT>(r, f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) f[e] = e < count ? load_elem<DT>(base, at + e) : 0.0f;
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void store_values(void* base, int64_t at, int count, const float (&f)[kChunk]) {
+    if (count >= kChunk) {
+        char* p = static_cast<char*>(base) + at * ElemBytes<DT>::value;
+        const Raw<DT> r = pack_raw<DT>(f);
+        if constexpr (DT == AQSGD_F32) {
+            *reinterpret_cast<f32x4_any_t*>(p) = r.lo;
+            *reinterpret_cast<f32x4_any_t*>(p + 16) = r.hi;
+        } else {
+            *reinterpret_cast<u32x4_any_t*>(p) = r.v;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kChunk - 1; ++e)
+            if (e < count) store_elem<DT>(base, at + e, f[e]);
+    }
+}
+
+// A workgroup takes `across` pieces of eight elements of a row, of as many rows as 256 lanes hold.
+template <int DT, int ACT, bool GATED>
+__global__ __launch_bounds__(256) void ffn8_grad_kernel(const Ffn8GradArgs a, uint32_t across) {
+    const uint32_t ty = threadIdx.x / across, tx = threadIdx.x - ty * across, rows = 256 / across;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * across + tx) * kChunk, w = GATED ? 2 * a.f : a.f;
+    if (ty >= rows || c >= a.f) return;
+    const int count = static_cast<int>(min(a.f - c, static_cast<int64_t>(kChunk)));
+    for (int64_t m = static_cast<int64_t>(blockIdx.y) * rows + ty; m < a.m; m += static_cast<int64_t>(gridDim.y) * rows) {
+        float d[kChunk], g[kChunk], u[kChunk];
+        load_values<DT>(a.dh, m * a.f + c, count, d);
+        load_values<DT>(a.pre, m * w + c, count, g);
+        if constexpr (GATED) load_values<DT>(a.pre, m * w + a.f + c, count, u);
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            float value, slope;
+            activation_slope(ACT, g[e], value, slope);
+            g[e] = GATED ? d[e] * u[e] * slope : d[e] * slope;
+            u[e] = d[e] * value;
+        }
+        store_values<DT>(a.dpre, m * w + c, count, g);
+        if constexpr (GATED) store_values<DT>(a.dpre, m * w + a.f + c, count, u);
+    }
+}
+
+template <int DT, int ACT>
+hipError_t launch_ffn8_grad_as(const Ffn8GradArgs& a, hipStream_t stream) {
+    const int64_t pieces = (a.f + kChunk - 1) / kChunk, across = pieces < 256 ? pieces : 256;
+    const int64_t rows = 256 / across, bands = (a.m + rows - 1) / rows;
+    const dim3 grid(static_cast<unsigned>((pieces + across - 1) / across), static_cast<unsigned>(bands < 65535 ? bands : 65535)), block(256);
+    return a.gated ? launch_kernel(ffn8_grad_kernel<DT, ACT, true>, grid, block, stream, a, static_cast<uint32_t>(across))
+                   : launch_kernel(ffn8_grad_kernel<DT, ACT, false>, grid, block, stream, a, static_cast<uint32_t>(across));
+}
+
+template <int DT>
+hipError_t launch_ffn8_grad_dt(const Ffn8GradArgs& a, hipStream_t stream) {
+    switch (a.act) {
+    case AQSGD_ACT_SILU: return launch_ffn8_grad_as<DT, AQSGD_ACT_SILU>(a, stream);
+    case AQSGD_ACT_GELU: return launch_ffn8_grad_as<DT, AQSGD_ACT_GELU>(a, stream);
+    default:             return launch_ffn8_grad_as<DT, AQSGD_ACT_GELU_TANH>(a, stream);
     }
 }
 
 hipError_t launch_ffn8_grad(const Ffn8GradArgs& a, hipStream_t stream) {
-    const int64_t blocks = (a.m * ((a.f + 3) / 4) + 255) / 256;
-    return launch_kernel(ffn8_grad_kernel, dim3(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), dim3(256), stream, a);
+    switch (a.dtype) {
+    case AQSGD_F32: return launch_ffn8_grad_dt<AQSGD_F32>(a, stream);
+    case AQSGD_F16: return launch_ffn8_grad_dt<AQSGD_F16>(a, stream);
+    default:        return launch_ffn8_grad_dt<AQSGD_BF16>(a, stream);
+    }
 }
 
 }  // namespace aqsgd

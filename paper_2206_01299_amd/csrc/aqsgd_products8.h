@@ -65,13 +65,13 @@ constexpr float kSqrtHalf = 0.70710678118654752f;          // 1 / sqrt(2)
 constexpr float kDensity = 0.39894228040143268f;           // 1 / sqrt(2 pi)
 constexpr float kTanhSlope = 1.5957691216057308f;          // 2 sqrt(2 / pi)
 
-// p = 1 / (1 + exp(-x)) and q = 1 - p, both without a difference of nearly equal numbers and
-// without an exponential that overflows.
+// p = 1 / (1 + exp(-x)) and q = 1 - p, both without a difference of nearly equal numbers and without an
+// exponential that overflows.  The hardware's exponential and reciprocal are off by an ulp at most; the rounding
+// of x log2(e) puts e off by |x| half steps more, which e itself outweighs: p and q are off by 4 half steps of 1.
 __device__ __forceinline__ void sigmoids(float x, float& p, float& q) {
-    const float e = expf(-fabsf(x)), r = 1.0f / (1.0f + e), er = e * r;
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269504088896341f), r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
     p = x >= 0.0f ? r : er;
-    q = x >= 0.0f ? er : r;
-    if (x != x) p = q = x;
+    q = x >= 0.0f ? er : r;                   // a NaN gives e, r and er NaN
 }
 
 // (1 + tanh(y / 2)) / 2 is the sigmoid of y.
@@ -89,7 +89,7 @@ __device__ __forceinline__ void activation_slope(int act, float x, float& value,
     if (act == AQSGD_ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(x * kSqrtHalf));
         value = x * cdf;
-        slope = cdf + x * (kDensity * expf(-0.5f * x * x));
+        slope = cdf + x * (kDensity * __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f));
         return;
     }
     float p, q;

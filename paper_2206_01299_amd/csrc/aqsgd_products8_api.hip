@@ -4,7 +4,7 @@
 namespace aqsgd {
 namespace {
 
-constexpr int64_t kMaxSide = (int64_t{1} << 31) - 1024;      // row and column numbers are 32-bit in the kernels
+constexpr int64_t kMaxSide = int64_t{1} << 30;      // rows and columns: their numbers are 32-bit in the kernels
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool known_dtype(int dtype) { return dtype == AQSGD_F32 || dtype == AQSGD_F16 || dtype == AQSGD_BF16; }
@@ -19,7 +19,7 @@ int check_quant8(const aqsgd_quant8_desc* d) {
     if (!known_dtype(d->dtype)) return AQSGD_ERR_DTYPE;
     if (d->rounding != AQSGD_ROUND_NEAREST && d->rounding != AQSGD_ROUND_STOCHASTIC) return AQSGD_ERR_DTYPE;
     if (!side(d->rows) || !side(d->cols) || d->ld < d->cols || d->ld > (int64_t{1} << 40) || !countable(d->rows, d->cols) ||
-        (d->rows > 0 && d->ld > (int64_t{1} << 60) / d->rows) || (d->rows + 63) / 64 > 65535)
+        (d->rows > 0 && d->ld > (int64_t{1} << 60) / d->rows))
         return AQSGD_ERR_SHAPE;
     return AQSGD_OK;
 }
