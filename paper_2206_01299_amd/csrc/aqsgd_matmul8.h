@@ -8,139 +8,15 @@ namespace aqsgd {
 
 typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
-// A row of b for column c of a tile's columns that start at c0.  In the gated product the columns
-// alternate in sixteens between the gate's rows and those it is multiplied with, so that one lane
-// ends up with both sums of an element.
+// Where column c of a tile whose columns start at n0 has its row of b, in rows from the tile's first (of the gate's
+// half, where gated).  In the gated product the columns alternate in sixteens between the gate's rows and those it
+// is multiplied with, n / 2 further on, so that one lane ends up with both sums of an element.  Columns past the
+// last one read the last one's row.
 template <int KIND>
-__device__ __forceinline__ int32_t row_of_b(int32_t c0, int32_t c, int32_t n) {
-    if constexpr (KIND == kGated) {
-        const int32_t half = n >> 1;
-        const int32_t f = min((c0 >> 1) + ((c >> 5) << 4) + (c & 15), half - 1);
-        return f + ((c & 16) ? half : 0);
-    } else {
-        return min(c0 + c, n - 1);
-    }
+__device__ __forceinline__ uint32_t row_from(int32_t n0, int32_t c, int32_t n) {
+    if constexpr (KIND == kGated) return static_cast<uint32_t>(min(((c >> 5) << 4) + (c & 15), (n >> 1) - 1 - (n0 >> 1)));
+    else return static_cast<uint32_t>(min(c, n - 1 - n0));
 }
-
-// Scales, bias and the rest for four consecutive columns of one row, in binary32.
-__device__ __forceinline__ f32x4_t scaled4(const ProductArgs& p, const f32x4_t& sum, float a_step, int32_t n0, int32_t left) {
-    f32x4_t v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int32_t c = n0 + (e < left ? e : 0);
-        v[e] = sum[e] * a_step * (p.b_scales[c] / kCodeHalf);
-        if (p.bias) v[e] += load1(p.dtype, p.bias, c);
-    }
-    return v;
-}
-
-__device__ __forceinline__ void put4(int dtype, void* base, int64_t idx, const f32x4_t& v, int32_t left) {
-    if (left >= 4) {
-        store4(dtype, base, idx, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < left) store1(dtype, base, idx + e, v[e]);
-    }
-}
-
-// A tile of 64 x 64 sums by four waves, one 64-byte step of k at a time.
-template <int KIND>
-__global__ __launch_bounds__(256) void product64_kernel(const ProductArgs p) {
-    constexpr int kRow = 80;                                   // bytes of a row in LDS: 64 and a pad
-    __shared__ __attribute__((aligned(16))) uint8_t sa[64 * kRow], sb[64 * kRow];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int32_t tiles_n = (p.n + 63) / 64;
-    const int32_t m0 = static_cast<int32_t>(blockIdx.x / tiles_n) * 64, n0 = static_cast<int32_t>(blockIdx.x % tiles_n) * 64;
-    const int32_t row = t >> 2, piece = (t & 3) * 16;
-    const uint8_t* ga = p.a + static_cast<int64_t>(min(m0 + row, p.m - 1)) * p.lda;
-    const int8_t* gb = p.b + static_cast<int64_t>(row_of_b<KIND>(n0, row, p.n)) * p.ldb;
-    const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    i32x4_t acc[2][2] = {};
-    int32_t ones[2] = {0, 0};
-    const int32_t last = KIND == kMessage ? p.k - 16 : 0x7fffffff;     // a message's rows have no padding
-    for (int32_t k = 0; k < p.k; k += 64) {
-        const i32x4_t va = *reinterpret_cast<const i32x4_t*>(ga + min(k + piece, last));
-        const i32x4_t vb = *reinterpret_cast<const i32x4_t*>(gb + k + piece);
-        __syncthreads();
-        *reinterpret_cast<i32x4_t*>(sa + row * kRow + piece) = va;
-        *reinterpret_cast<i32x4_t*>(sb + row * kRow + piece) = vb;
-        __syncthreads();
-        i32x4_t fa[2], fb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fa[i] = *reinterpret_cast<const i32x4_t*>(sa + (wm + 16 * i + (lane & 15)) * kRow + (lane >> 4) * 16);
-            fb[i] = *reinterpret_cast<const i32x4_t*>(sb + (wn + 16 * i + (lane & 15)) * kRow + (lane >> 4) * 16);
-            if constexpr (KIND == kMessage) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    fa[i][e] ^= static_cast<int32_t>(0x80808080u);                      // level - 128
-                    ones[i] = __builtin_amdgcn_sdot4(fb[i][e], 0x01010101, ones[i], false);
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    }
-    if constexpr (KIND == kMessage) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            ones[j] += __shfl_xor(ones[j], 16, kWave);
-            ones[j] += __shfl_xor(ones[j], 32, kWave);
-        }
-    }
-    const int cn = (lane >> 4) * 4;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int32_t m = m0 + wm + 16 * i + (lane & 15);
-        const float a_step = p.a_scales[min(m, p.m - 1)] / (KIND == kMessage ? kLevelHalf : kCodeHalf);
-        f32x4_t sum[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                sum[j][e] = static_cast<float>(acc[i][j][e]);
-                if constexpr (KIND == kMessage)
-                    sum[j][e] += 0.5f * static_cast<float>(__shfl(ones[j], cn + e, kWave));   // levels - 127.5
-            }
-        }
-        if (m >= p.m) continue;
-        if constexpr (KIND == kGated) {
-            const int32_t half = p.n >> 1, f = ((n0 + wn) >> 1) + cn, left = half - f;
-            if (left <= 0) continue;
-            const f32x4_t g = scaled4(p, sum[0], a_step, f, left), u = scaled4(p, sum[1], a_step, half + f, left);
-            f32x4_t h;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = activation(p.act, g[e]) * u[e];
-            put4(p.dtype, p.out, static_cast<int64_t>(m) * half + f, h, left);
-            if (p.pre) {
-                put4(p.dtype, p.pre, static_cast<int64_t>(m) * p.n + f, g, left);
-                put4(p.dtype, p.pre, static_cast<int64_t>(m) * p.n + half + f, u, left);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int32_t n = n0 + wn + 16 * j + cn, left = p.n - n;
-                if (left <= 0) continue;
-                f32x4_t v = scaled4(p, sum[j], a_step, n, left);
-                const int64_t at = static_cast<int64_t>(m) * p.n + n;
-                if constexpr (KIND == kActivation) {
-                    if (p.pre) put4(p.dtype, p.pre, at, v, left);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = activation(p.act, v[e]);
-                } else if (p.add) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < left) v[e] += load1(p.dtype, p.add, at + e);
-                }
-                put4(p.dtype, p.out, at, v, left);
-            }
-        }
-    }
-}
-
 
 // What is left of the sums once they lie in LDS as rows of 32-bit integers: a lane takes four columns of every
 // few rows, so that its scales and bias are read once and a row leaves in whole lines.
@@ -169,8 +45,7 @@ struct Finish {
         }
         return v;
     }
-    // ones: sums of the columns' codes of b (message)
-    __device__ __forceinline__ Finish(const ProductArgs& args, int32_t n0, int lane, const int32_t* ones) : p(args) {
+    __device__ __forceinline__ Finish(const ProductArgs& args, int32_t n0, int lane) : p(args) {
         const int c = (lane % wide) * 4;
         half = p.n >> 1;
         if constexpr (KIND == kGated) {
@@ -189,9 +64,15 @@ struct Finish {
             step_u = steps(half + at);
             bias_u = biases(half + at);
         }
-        if constexpr (KIND == kMessage) {
+    }
+    // A message's levels stand for level - 127.5; the sums are over level - 128, so half the sum of b's codes is
+    // missing.  ones: those sums, `parts` of them `pitch` apart.
+    __device__ __forceinline__ void take_ones(const int32_t* ones, int parts, int pitch) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) extra[e] = 0.5f * static_cast<float>(ones[place + e]);      // levels - 127.5
+        for (int e = 0; e < 4; ++e) {
+            int32_t s = 0;
+            for (int k = 0; k < parts; ++k) s += ones[k * pitch + place + e];
+            extra[e] = 0.5f * static_cast<float>(s);
         }
     }
     __device__ __forceinline__ f32x4_t scaled(const i32x4_t& sum, float a_step, const f32x4_t& st, const f32x4_t& bi) const {
@@ -205,8 +86,9 @@ struct Finish {
         }
         return v;
     }
+    template <bool FULL>
     __device__ __forceinline__ void put(void* base, int64_t at, const f32x4_t& v) const {
-        if (left >= 4) {
+        if (FULL || left >= 4) {
             store4(DT, base, at, v);
         } else {
 #pragma unroll
@@ -214,36 +96,58 @@ struct Finish {
                 if (e < left) store_elem<DT>(base, at + e, v[e]);
         }
     }
-    __device__ __forceinline__ void row(int32_t m, const int32_t* sums) const {
-        if (m >= p.m || left <= 0) return;
-        const float a_step = p.a_scales[m] / (KIND == kMessage ? kLevelHalf : kCodeHalf);
-        f32x4_t v = scaled(*reinterpret_cast<const i32x4_t*>(sums + place), a_step, step, bias);
+    // A row's columns: its sums in LDS, in PARTS parts `pitch` apart.
+    template <int PARTS>
+    __device__ __forceinline__ i32x4_t sum_of(const int32_t* sums, int pitch) const {
+        i32x4_t s = *reinterpret_cast<const i32x4_t*>(sums);
+#pragma unroll
+        for (int k = 1; k < PARTS; ++k) s += *reinterpret_cast<const i32x4_t*>(sums + k * pitch);
+        return s;
+    }
+    static __device__ __forceinline__ float step_of_a(float scale) { return scale / (KIND == kMessage ? kLevelHalf : kCodeHalf); }
+    // What is there already in a row's columns (the plain product with something to add to).
+    template <bool FULL>
+    __device__ __forceinline__ f32x4_t added(int32_t m) const {
+        f32x4_t v = {0, 0, 0, 0};
+        if constexpr (KIND == kPlain || KIND == kMessage) {
+            if (p.add && (FULL || (m < p.m && left > 0))) {
+                const int64_t at = static_cast<int64_t>(m) * p.n + n;
+                if (FULL || left >= 4) {
+                    v = load4(DT, p.add, at);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (e < left) v[e] = load_elem<DT>(p.add, at + e);
+                }
+            }
+        }
+        return v;
+    }
+    // FULL: the row and the four columns exist.
+    template <bool FULL, int PARTS = 1>
+    __device__ __forceinline__ void row(int32_t m, float a_step, const f32x4_t& there, const int32_t* sums, int pitch = 0) const {
+        if (!FULL && (m >= p.m || left <= 0)) return;
+        f32x4_t v = scaled(sum_of<PARTS>(sums + place, pitch), a_step, step, bias);
         if constexpr (KIND == kGated) {
-            const f32x4_t u = scaled(*reinterpret_cast<const i32x4_t*>(sums + place + 16), a_step, step_u, bias_u);
+            const f32x4_t u = scaled(sum_of<PARTS>(sums + place + 16, pitch), a_step, step_u, bias_u);
             f32x4_t h;
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = activation(p.act, v[e]) * u[e];
-            put(p.out, static_cast<int64_t>(m) * half + n, h);
+            put<FULL>(p.out, static_cast<int64_t>(m) * half + n, h);
             if (p.pre) {
-                put(p.pre, static_cast<int64_t>(m) * p.n + n, v);
-                put(p.pre, static_cast<int64_t>(m) * p.n + half + n, u);
+                put<FULL>(p.pre, static_cast<int64_t>(m) * p.n + n, v);
+                put<FULL>(p.pre, static_cast<int64_t>(m) * p.n + half + n, u);
             }
         } else {
             const int64_t at = static_cast<int64_t>(m) * p.n + n;
             if constexpr (KIND == kActivation) {
-                if (p.pre) put(p.pre, at, v);
+                if (p.pre) put<FULL>(p.pre, at, v);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = activation(p.act, v[e]);
             } else if (p.add) {
-                if (left >= 4) {
-                    v += load4(DT, p.add, at);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (e < left) v[e] += load_elem<DT>(p.add, at + e);
-                }
+                v += there;
             }
-            put(p.out, at, v);
+            put<FULL>(p.out, at, v);
         }
     }
 };
@@ -252,13 +156,21 @@ struct Finish {
 // row m0 and virtual column n0 on.  `own`: LDS of the wave's own, store_bytes() of it.
 constexpr int kStoreBlocks = 2;                  // blocks of 16 rows that go through LDS at a time
 constexpr int store_pitch(int tn) { return tn * 16 + 4; }
-constexpr int store_bytes(int tn) { return (kStoreBlocks * 16 * store_pitch(tn) + 16 * tn) * 4; }
+constexpr int store_bytes(int tm, int tn) { return (kStoreBlocks * 16 * store_pitch(tn) + 16 * tn + 16 * tm) * 4; }
 
 template <int KIND, int DT, int TM, int TN>
 __device__ __forceinline__ void store_tile(const ProductArgs& p, const i32x4_t (&acc)[TM][TN], const int32_t (&ones)[TN], int32_t m0,
                                            int32_t n0, int lane, int32_t* own) {
     constexpr int pitch = store_pitch(TN);
     int32_t* sums_of_b = own + kStoreBlocks * 16 * pitch;
+    float* steps_of_a = reinterpret_cast<float*>(sums_of_b + 16 * TN);
+    using F = Finish<KIND, DT, TN * 16>;
+#pragma unroll
+    for (int i = 0; i < (16 * TM + 63) / 64; ++i) {
+        const int r = 64 * i + lane;
+        const float a_step = F::step_of_a(p.a_scales[min(m0 + r, p.m - 1)]);
+        if (r < 16 * TM) steps_of_a[r] = a_step;
+    }
     if constexpr (KIND == kMessage) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -268,16 +180,39 @@ __device__ __forceinline__ void store_tile(const ProductArgs& p, const i32x4_t (
             if (lane < 16) sums_of_b[16 * j + lane] = v;
         }
     }
-    using F = Finish<KIND, DT, TN * 16>;
-    const F finish(p, n0, lane, sums_of_b);
+    F finish(p, n0, lane);
+    if constexpr (KIND == kMessage) finish.take_ones(sums_of_b, 1, 0);
     int32_t* to = own + (lane & 15) * pitch + (lane >> 4) * 4;
+    constexpr int turns = kStoreBlocks * 16 / F::step_rows, ahead = turns < 4 ? turns : 4;
+    const bool full = m0 + 16 * TM <= p.m && n0 + 16 * TN <= (KIND == kGated ? p.n & ~31 : p.n);     // h is whole sixteens there
+    const int mine = lane / F::wide;
 #pragma unroll
     for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
 #pragma unroll
         for (int i = 0; i < kStoreBlocks; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(to + i * 16 * pitch + 16 * j) = acc[i0 + i][j];
-        for (int r = lane / F::wide; r < kStoreBlocks * 16; r += F::step_rows) finish.row(m0 + i0 * 16 + r, own + r * pitch);
+        const int32_t first = m0 + i0 * 16 + mine;
+        if (full) {
+#pragma unroll 1
+            for (int t = 0; t < turns; t += ahead) {
+                f32x4_t there[ahead];
+#pragma unroll
+                for (int u = 0; u < ahead; ++u) there[u] = finish.template added<true>(first + (t + u) * F::step_rows);
+#pragma unroll
+                for (int u = 0; u < ahead; ++u) {
+                    const int r = mine + (t + u) * F::step_rows;
+                    finish.template row<true>(first + (t + u) * F::step_rows, steps_of_a[i0 * 16 + r], there[u], own + r * pitch);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int t = 0; t < turns; ++t) {
+                const int r = mine + t * F::step_rows;
+                const int32_t m = first + t * F::step_rows;
+                finish.template row<false>(m, steps_of_a[i0 * 16 + r], finish.template added<false>(m), own + r * pitch);
+            }
+        }
     }
 }
 
@@ -331,10 +266,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
 #pragma unroll
     for (int i = 0; i < S::loads_b; ++i) {
         const int r = (wave * S::loads_b + i) * 8 + lr;
-        if constexpr (KIND == kGated)
-            off_b[i] = static_cast<uint32_t>(min(((r >> 5) << 4) + (r & 15), half - 1 - (n0 >> 1))) * static_cast<uint32_t>(p.ldb);
-        else
-            off_b[i] = static_cast<uint32_t>(min(r, p.n - 1 - n0)) * static_cast<uint32_t>(p.ldb);
+        off_b[i] = row_from<KIND>(n0, r, p.n) * static_cast<uint32_t>(p.ldb);
     }
     const int32_t halves = (p.k + 63) / 64, steps = (halves + 1) / 2;
     const int32_t last_a = (KIND == kMessage ? p.k : halves * 64) - 16, last_b = halves * 64 - 16;
@@ -396,9 +328,138 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
         if (s + 1 < steps) read_frags(fa0, fb0, buf ^ 1, 0);
         if (2 * s + 1 < halves) multiply(fa1, fb1);
     }
-    static_assert(store_bytes(TN) * S::waves <= 2 * S::stage && TM % kStoreBlocks == 0, "the stages' LDS serves the results");
+    static_assert(store_bytes(TM, TN) * S::waves <= 2 * S::stage && TM % kStoreBlocks == 0, "the stages' LDS serves the results");
     __syncthreads();                         // the last fragments have been read
-    store_tile<KIND, DT, TM, TN>(p, acc, ones, m0 + wm, n0 + wn, lane, reinterpret_cast<int32_t*>(lds + wave * store_bytes(TN)));
+    store_tile<KIND, DT, TM, TN>(p, acc, ones, m0 + wm, n0 + wn, lane, reinterpret_cast<int32_t*>(lds + wave * store_bytes(TM, TN)));
+}
+
+// ---- small products ---------------------------------------------------------------------------
+// 16 R x 16 J sums to a workgroup, its W waves sharing out k in pieces of 128 bytes: nothing is staged, every wave
+// loads the fragments of its pieces from memory into registers, the next ones while it multiplies, and the waves'
+// sums meet in LDS once, at the end.
+template <int R, int J> struct SplitShape {
+    static constexpr int pieces = R + J >= 4 ? 1 : R + J == 3 ? 2 : 3;        // on their way at a time: registers
+    static constexpr int pitch = 16 * J + 4;
+};
+
+template <int KIND, int DT, int R, int J, int W>
+__global__ __launch_bounds__(64 * W) void product_split_kernel(const ProductArgs p, uint32_t tiles_n) {
+    using S = SplitShape<R, J>;
+    constexpr int P = S::pieces, slab = 16 * R * S::pitch;
+    __shared__ __attribute__((aligned(16))) int32_t sums[W * slab];
+    __shared__ int32_t ones_of[KIND == kMessage ? W * 16 * J : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t m0 = static_cast<int32_t>(blockIdx.x / tiles_n) * (16 * R), n0 = static_cast<int32_t>(blockIdx.x % tiles_n) * (16 * J);
+    const int fr = lane & 15, fq = lane >> 4;
+    // rows by their distance from the tile's first, in bytes: below 64 * 131072
+    const int32_t half = p.n >> 1;
+    const uint8_t* base_a = p.a + static_cast<int64_t>(m0) * p.lda;
+    const int8_t* base_b = p.b + static_cast<int64_t>(KIND == kGated ? n0 >> 1 : n0) * p.ldb;
+    const int8_t* base_u = KIND == kGated ? base_b + static_cast<int64_t>(half) * p.ldb : base_b;
+    uint32_t off_a[R], off_b[J];
+#pragma unroll
+    for (int i = 0; i < R; ++i) off_a[i] = static_cast<uint32_t>(min(16 * i + fr, p.m - 1 - m0)) * static_cast<uint32_t>(p.lda);
+#pragma unroll
+    for (int j = 0; j < J; ++j) off_b[j] = row_from<KIND>(n0, 16 * j + fr, p.n) * static_cast<uint32_t>(p.ldb);
+    const int32_t halves = (p.k + 63) / 64, whole = (halves + 1) / 2;
+    const int32_t last_a = (KIND == kMessage ? p.k : halves * 64) - 16;
+    struct Frags { i32x4_t a[P][2][R], b[P][2][J]; };
+    auto load = [&](Frags& f, int32_t first) {
+#pragma unroll
+        for (int u = 0; u < P; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int32_t step = 2 * (first + u * W) + h, k = step * 64 + fq * 16;
+                if (step < halves) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) 
+                        f.b[u][h][j] = *reinterpret_cast<const i32x4_t*>((KIND == kGated && (j & 1) ? base_u : base_b) + (off_b[j] + static_cast<uint32_t>(k)));
+#pragma unroll
+                    for (int i = 0; i < R; ++i) 
+                        f.a[u][h][i] = *reinterpret_cast<const i32x4_t*>(base_a + (off_a[i] + static_cast<uint32_t>(min(k, last_a))));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) f.b[u][h][j] = i32x4_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < R; ++i) f.a[u][h][i] = i32x4_t{0, 0, 0, 0};
+                }
+            }
+    };
+    i32x4_t acc[R][J] = {};
+    int32_t ones[J] = {};
+    auto multiply = [&](Frags& f) {
+#pragma unroll
+        for (int u = 0; u < P; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (KIND == kMessage) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                        for (int i = 0; i < R; ++i) f.a[u][h][i][e] ^= static_cast<int32_t>(0x80808080u);       // level - 128
+#pragma unroll
+                        for (int j = 0; j < J; ++j) ones[j] = __builtin_amdgcn_sdot4(f.b[u][h][j][e], 0x01010101, ones[j], false);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[u][h][j], f.a[u][h][i], acc[i][j], 0, 0, 0);
+            }
+    };
+    Frags x, y;
+    load(x, wave);
+    // what the end needs is asked for now
+    using F = Finish<KIND, DT, 16 * J>;
+    constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
+    F finish(p, n0, lane);
+    float a_step[turns];
+#pragma unroll
+    for (int t = 0; t < turns; ++t)
+        a_step[t] = F::step_of_a(p.a_scales[min(m0 + static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows, p.m - 1)]);
+    for (int32_t at = wave; at < whole; at += 2 * P * W) {
+        load(y, at + P * W);
+        multiply(x);
+        load(x, at + 2 * P * W);
+        multiply(y);
+    }
+    int32_t* own = sums + wave * slab;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            *reinterpret_cast<i32x4_t*>(own + (16 * i + fr) * S::pitch + 16 * j + 4 * fq) = acc[i][j];
+    if constexpr (KIND == kMessage) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            int32_t v = ones[j];
+            v += __shfl_xor(v, 16, kWave);
+            v += __shfl_xor(v, 32, kWave);
+            if (lane < 16) ones_of[(wave * J + j) * 16 + lane] = v;
+        }
+    }
+    __syncthreads();
+    if constexpr (KIND == kMessage) finish.take_ones(ones_of, W, 16 * J);
+#pragma unroll
+    for (int t = 0; t < turns; ++t) {
+        const int r = static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows;
+        if (r < 16 * R) finish.template row<false, W>(m0 + r, a_step[t], finish.template added<false>(m0 + r), sums + r * S::pitch, slab);
+    }
+}
+
+template <int DT, int R, int J, int W>
+hipError_t launch_split_as(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+    const uint32_t tm = (static_cast<uint32_t>(p.m) + 16 * R - 1) / (16 * R), tn = (static_cast<uint32_t>(p.n) + 16 * J - 1) / (16 * J);
+    const dim3 grid(tm * tn), block(64 * W);
+    switch (kind) {
+    case kPlain:      return launch_kernel(product_split_kernel<kPlain, DT, R, J, W>, grid, block, stream, p, tn);
+    case kMessage:    return launch_kernel(product_split_kernel<kMessage, DT, R, J, W>, grid, block, stream, p, tn);
+    case kActivation: return launch_kernel(product_split_kernel<kActivation, DT, R, J, W>, grid, block, stream, p, tn);
+    default:
+        if constexpr (J % 2 == 0) return launch_kernel(product_split_kernel<kGated, DT, R, J, W>, grid, block, stream, p, tn);
+        else return hipErrorInvalidValue;                       // the gate's columns come in pairs of sixteen
+    }
 }
 
 template <int DT, int TM, int TN, int WM, int WN>
@@ -414,13 +475,18 @@ hipError_t launch_tiles_as(ProductKind kind, const ProductArgs& p, hipStream_t s
     }
 }
 
-enum ProductTile { kTile256 = 0, kTile128 };
+enum ProductTile { kTile256 = 0, kTile128, kSplit64, kSplit64x32, kSplit32, kSplit16, kSplit16x32 };
 
 template <int DT>
 hipError_t launch_product_dt(ProductTile tile, ProductKind kind, const ProductArgs& p, hipStream_t stream) {
     switch (tile) {
     case kTile256: return launch_tiles_as<DT, 8, 4, 2, 4>(kind, p, stream);
-    default:       return launch_tiles_as<DT, 4, 4, 2, 2>(kind, p, stream);
+    case kTile128: return launch_tiles_as<DT, 4, 4, 2, 2>(kind, p, stream);
+    case kSplit64: return launch_split_as<DT, 4, 4, 8>(kind, p, stream);
+    case kSplit64x32: return launch_split_as<DT, 4, 2, 8>(kind, p, stream);
+    case kSplit32: return launch_split_as<DT, 2, 2, 8>(kind, p, stream);
+    case kSplit16: return launch_split_as<DT, 1, 1, 8>(kind, p, stream);
+    default:       return launch_split_as<DT, 1, 2, 8>(kind, p, stream);
     }
 }
 
