@@ -315,18 +315,22 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
     if (steps > 0) {
         bring(0, 0);
         __syncthreads();
-        if (steps > 1) bring(1, 1);
+        bring(min(1, steps - 1), 1);
         read_frags(fa0, fb0, 0, 0);
-    }
-    for (int32_t s = 0; s < steps; ++s) {
-        const int buf = s & 1;
-        read_frags(fa1, fb1, buf, 1);
+        for (int32_t s = 0; s < steps - 1; ++s) {
+            const int buf = s & 1;
+            read_frags(fa1, fb1, buf, 1);
+            multiply(fa0, fb0);
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();                             // step s + 1 has arrived; no wave reads step s any more
+            bring(min(s + 2, steps - 1), buf);           // the last one once more: nobody reads it
+            read_frags(fa0, fb0, buf ^ 1, 0);
+            multiply(fa1, fb1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (halves % 2 == 0) read_frags(fa1, fb1, (steps - 1) & 1, 1);
         multiply(fa0, fb0);
-        __builtin_amdgcn_sched_barrier(0);
-        __syncthreads();                     // step s + 1 has arrived; no wave reads step s any more
-        if (s + 2 < steps) bring(s + 2, buf);
-        if (s + 1 < steps) read_frags(fa0, fb0, buf ^ 1, 0);
-        if (2 * s + 1 < halves) multiply(fa1, fb1);
+        if (halves % 2 == 0) multiply(fa1, fb1);
     }
     static_assert(store_bytes(TM, TN) * S::waves <= 2 * S::stage && TM % kStoreBlocks == 0, "the stages' LDS serves the results");
     __syncthreads();                         // the last fragments have been read
