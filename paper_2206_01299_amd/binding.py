@@ -220,7 +220,7 @@ def _load_native():
         warnings.warn(f"{NATIVE_PATH.name} cannot be loaded ({e}): calls go through ctypes, which costs the host some "
                       "9 us a call instead of 4; build it with `python -m paper_2206_01299_amd.build`", RuntimeWarning)
         return _Ctypes()
-    mod.setup(Desc, Job, {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS})
+    mod.setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS})
     return mod
 
 
@@ -611,6 +611,9 @@ def quant8(desc: Quant8Desc, x, *, row_codes=None, row_scales=None, col_codes=No
     """``aqsgd_quant8``: signed 8-bit codes of ``x`` [rows, cols] (row stride ``desc.ld``) with a scale for
     each row (``row_codes`` [rows, stride(cols)] int8, ``row_scales`` [rows] float32) and / or each column
     (``col_codes`` [cols, stride(rows)], ``col_scales`` [cols]), and the columns' sums (``col_sums`` [cols])."""
+    rc = _native.quant8(desc, x, row_codes, row_scales, col_codes, col_scales, col_sums, workspace, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
     rows, cols = desc.rows, desc.cols
@@ -636,6 +639,9 @@ def matmul8(desc: Matmul8Desc, a_codes, a_scales, b_codes, b_scales, out, *, bia
             stream=None) -> None:
     """``aqsgd_matmul8``: ``out`` [m, n] of the matrices that ``a_codes`` [m, stride(k)] and ``b_codes``
     [n, stride(k)] stand for (with ``desc.message``: the codes of an 8-bit message, ``m * k`` bytes, uint8)."""
+    rc = _native.matmul8(desc, a_codes, a_scales, b_codes, b_scales, out, bias, add, workspace, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
     td, m, n, k = _TORCH_OF_CODE[desc.dtype], desc.m, desc.n, desc.k
@@ -657,6 +663,9 @@ def matmul8(desc: Matmul8Desc, a_codes, a_scales, b_codes, b_scales, out, *, bia
 def ffn8(desc: Ffn8Desc, a_codes, a_scales, w_codes, w_scales, h, *, bias=None, pre=None, stream=None) -> None:
     """``aqsgd_ffn8``: ``h`` [m, f] of a feed-forward block's first half; ``w_codes`` [2 f, stride(k)] (gate
     first), or [f, stride(k)] where ``desc.gated`` is 0; ``pre`` [m, 2 f or f] takes the projections."""
+    rc = _native.ffn8(desc, a_codes, a_scales, w_codes, w_scales, h, bias, pre, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
     td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f
@@ -670,6 +679,9 @@ def ffn8(desc: Ffn8Desc, a_codes, a_scales, w_codes, w_scales, h, *, bias=None, 
 
 def ffn8_grad(desc: Ffn8Desc, dh, pre, dpre, *, stream=None) -> None:
     """``aqsgd_ffn8_grad``: ``dpre`` [m, 2 f or f] from ``dh`` [m, f] and the stored projections ``pre``."""
+    rc = _native.ffn8_grad(desc, dh, pre, dpre, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
     td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f

@@ -18,19 +18,32 @@ __device__ __forceinline__ uint32_t row_from(int32_t n0, int32_t c, int32_t n) {
     else return static_cast<uint32_t>(min(c, n - 1 - n0));
 }
 
-// What is left of the sums once they lie in LDS as rows of 32-bit integers: a lane takes four columns of every
-// few rows, so that its scales and bias are read once and a row leaves in whole lines.
-//   sums  LDS, [rows, pitch] of the wave's (or workgroup's) columns from virtual column n0 on
+// What is left of the sums once they lie in LDS as rows of 32-bit integers: a lane takes four columns of every few
+// rows, so that its scales and bias are read once and a row leaves in whole lines.  COLS virtual columns from n0 on.
 template <int KIND, int DT, int COLS>
 struct Finish {
     static constexpr int wide = (KIND == kGated ? COLS / 2 : COLS) / 4;       // lanes to a row
     static constexpr int step_rows = kWave / wide;                            // rows a wave takes at a time
-    static_assert(wide >= 1 && wide <= kWave && kWave % wide == 0, "a wave takes whole rows");
+    static_assert(wide >= 1 && wide <= kWave, "a wave takes whole rows");
     const ProductArgs& p;
     int32_t n, left, half;       // first column (of h, where gated), columns that remain from there
     int place;                   // of the lane's first sum in a row
     f32x4_t step, bias, extra, step_u, bias_u;
 
+    __device__ __forceinline__ Finish(const ProductArgs& args, int32_t n0, int lane) : p(args) {
+        const int c = (lane % wide) * 4;
+        half = p.n >> 1;
+        if constexpr (KIND == kGated) {
+            n = (n0 >> 1) + c;
+            left = half - n;
+            place = ((c >> 4) << 5) + (c & 15);
+        } else {
+            n = n0 + c;
+            left = p.n - n;
+            place = c;
+        }
+    }
+    // Scales and bias of the lane's columns from memory ...
     __device__ __forceinline__ f32x4_t steps(int32_t c) const {
         f32x4_t v;
 #pragma unroll
@@ -45,24 +58,22 @@ struct Finish {
         }
         return v;
     }
-    __device__ __forceinline__ Finish(const ProductArgs& args, int32_t n0, int lane) : p(args) {
-        const int c = (lane % wide) * 4;
-        half = p.n >> 1;
-        if constexpr (KIND == kGated) {
-            n = (n0 >> 1) + c;
-            left = half - n;
-            place = ((c >> 4) << 5) + (c & 15);
-        } else {
-            n = n0 + c;
-            left = p.n - n;
-            place = c;
-        }
+    __device__ __forceinline__ void take_scales() {
         const int32_t at = left > 0 ? n : 0;
         step = steps(at);
         bias = biases(at);
         if constexpr (KIND == kGated) {
             step_u = steps(half + at);
             bias_u = biases(half + at);
+        }
+    }
+    // ... or from LDS, by virtual column.
+    __device__ __forceinline__ void take_scales(const float* b_step, const float* b_bias) {
+        step = *reinterpret_cast<const f32x4_t*>(b_step + place);
+        bias = *reinterpret_cast<const f32x4_t*>(b_bias + place);
+        if constexpr (KIND == kGated) {
+            step_u = *reinterpret_cast<const f32x4_t*>(b_step + place + 16);
+            bias_u = *reinterpret_cast<const f32x4_t*>(b_bias + place + 16);
         }
     }
     // A message's levels stand for level - 127.5; the sums are over level - 128, so half the sum of b's codes is
@@ -96,14 +107,6 @@ struct Finish {
                 if (e < left) store_elem<DT>(base, at + e, v[e]);
         }
     }
-    // A row's columns: its sums in LDS, in PARTS parts `pitch` apart.
-    template <int PARTS>
-    __device__ __forceinline__ i32x4_t sum_of(const int32_t* sums, int pitch) const {
-        i32x4_t s = *reinterpret_cast<const i32x4_t*>(sums);
-#pragma unroll
-        for (int k = 1; k < PARTS; ++k) s += *reinterpret_cast<const i32x4_t*>(sums + k * pitch);
-        return s;
-    }
     static __device__ __forceinline__ float step_of_a(float scale) { return scale / (KIND == kMessage ? kLevelHalf : kCodeHalf); }
     // What is there already in a row's columns (the plain product with something to add to).
     template <bool FULL>
@@ -122,6 +125,14 @@ struct Finish {
             }
         }
         return v;
+    }
+    // A row's columns: its sums in LDS, in PARTS parts `pitch` apart.
+    template <int PARTS>
+    __device__ __forceinline__ i32x4_t sum_of(const int32_t* sums, int pitch) const {
+        i32x4_t s = *reinterpret_cast<const i32x4_t*>(sums);
+#pragma unroll
+        for (int k = 1; k < PARTS; ++k) s += *reinterpret_cast<const i32x4_t*>(sums + k * pitch);
+        return s;
     }
     // FULL: the row and the four columns exist.
     template <bool FULL, int PARTS = 1>
@@ -152,105 +163,48 @@ struct Finish {
     }
 };
 
-// A wave's TM x TN blocks of sums (lane l holds row l % 16 of a block and four columns from (l / 16) * 4 on), from
-// row m0 and virtual column n0 on.  `own`: LDS of the wave's own, store_bytes() of it.
-constexpr int kStoreBlocks = 2;                  // blocks of 16 rows that go through LDS at a time
-constexpr int store_pitch(int tn) { return tn * 16 + 4; }
-constexpr int store_bytes(int tm, int tn) { return (kStoreBlocks * 16 * store_pitch(tn) + 16 * tn + 16 * tm) * 4; }
-
-template <int KIND, int DT, int TM, int TN>
-__device__ __forceinline__ void store_tile(const ProductArgs& p, const i32x4_t (&acc)[TM][TN], const int32_t (&ones)[TN], int32_t m0,
-                                           int32_t n0, int lane, int32_t* own) {
-    constexpr int pitch = store_pitch(TN);
-    int32_t* sums_of_b = own + kStoreBlocks * 16 * pitch;
-    float* steps_of_a = reinterpret_cast<float*>(sums_of_b + 16 * TN);
-    using F = Finish<KIND, DT, TN * 16>;
-#pragma unroll
-    for (int i = 0; i < (16 * TM + 63) / 64; ++i) {
-        const int r = 64 * i + lane;
-        const float a_step = F::step_of_a(p.a_scales[min(m0 + r, p.m - 1)]);
-        if (r < 16 * TM) steps_of_a[r] = a_step;
-    }
-    if constexpr (KIND == kMessage) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            int32_t v = ones[j];
-            v += __shfl_xor(v, 16, kWave);
-            v += __shfl_xor(v, 32, kWave);
-            if (lane < 16) sums_of_b[16 * j + lane] = v;
-        }
-    }
-    F finish(p, n0, lane);
-    if constexpr (KIND == kMessage) finish.take_ones(sums_of_b, 1, 0);
-    int32_t* to = own + (lane & 15) * pitch + (lane >> 4) * 4;
-    constexpr int turns = kStoreBlocks * 16 / F::step_rows, ahead = turns < 4 ? turns : 4;
-    const bool full = m0 + 16 * TM <= p.m && n0 + 16 * TN <= (KIND == kGated ? p.n & ~31 : p.n);     // h is whole sixteens there
-    const int mine = lane / F::wide;
-#pragma unroll
-    for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
-#pragma unroll
-        for (int i = 0; i < kStoreBlocks; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(to + i * 16 * pitch + 16 * j) = acc[i0 + i][j];
-        const int32_t first = m0 + i0 * 16 + mine;
-        if (full) {
-#pragma unroll 1
-            for (int t = 0; t < turns; t += ahead) {
-                f32x4_t there[ahead];
-#pragma unroll
-                for (int u = 0; u < ahead; ++u) there[u] = finish.template added<true>(first + (t + u) * F::step_rows);
-#pragma unroll
-                for (int u = 0; u < ahead; ++u) {
-                    const int r = mine + (t + u) * F::step_rows;
-                    finish.template row<true>(first + (t + u) * F::step_rows, steps_of_a[i0 * 16 + r], there[u], own + r * pitch);
-                }
-            }
-        } else {
-#pragma unroll 1
-            for (int t = 0; t < turns; ++t) {
-                const int r = mine + t * F::step_rows;
-                const int32_t m = first + t * F::step_rows;
-                finish.template row<false>(m, steps_of_a[i0 * 16 + r], finish.template added<false>(m), own + r * pitch);
-            }
-        }
-    }
-}
-
 // ---- large tiles ------------------------------------------------------------------------------
-// TM x TN blocks of 16 x 16 sums to a wave, WM x WN waves to a workgroup, k in steps of 128 bytes.
+// A workgroup of WM x WN waves, each with TM x TN blocks of 16 x 16 sums (lane l holds row l % 16 of a block and four
+// columns from (l / 16) * 4 on); k in steps of 128 bytes, two steps' operands in LDS.
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef const __attribute__((address_space(1))) void* global_ptr;
+
+constexpr int kStoreBlocks = 2;                  // blocks of 16 rows that go through LDS at a time, at the end
 
 template <int TM, int TN, int WM, int WN>
 struct TileShape {
     static constexpr int bm = 16 * TM * WM, bn = 16 * TN * WN, waves = WM * WN;
     static constexpr int row = 128;                               // bytes of k in a step
     static constexpr int stage = (bm + bn) * row;                 // bytes of a step's operands
-    static constexpr int loads_a = bm / 8 / waves, loads_b = bn / 8 / waves;      // 1 KB each, per wave
+    static constexpr int loads_a = (bm / 8 + waves - 1) / waves, loads_b = (bn / 8 + waves - 1) / waves;    // 1 KB each, per wave
+    static constexpr int loads_least = bm / 8 / waves + bn / 8 / waves;
+    static constexpr int pitch = 16 * TN + 4;                     // words of a row of sums, at the end
+    static constexpr int own = kStoreBlocks * 16 * pitch * 4;     // bytes of LDS of a wave, at the end
+    static constexpr int work = 2 * stage > own * waves ? 2 * stage : own * waves;
+    static constexpr int scales = (bm + 2 * bn) * 4;              // a's steps, b's steps, bias
+    static constexpr int ones = WM * bn * 4;                      // sums of b's codes (message)
+    static constexpr int lds = work + scales + ones;
+    static_assert(TM % kStoreBlocks == 0, "the blocks leave in twos");
 };
 
-// Tile of workgroup b: the eight XCDs take the workgroups in turn, so that b mod 8 is the XCD; each gets a
-// contiguous run of the tiles, which go down in bands of kBand tile rows, so that the tiles an XCD works on
-// at a time share rows of a and of b in its L2.
-constexpr int kBand = 4;
-__device__ __forceinline__ void tile_of(uint32_t b, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
-    const uint32_t q = total >> 3, r = total & 7, x = b & 7;
-    const uint32_t t = x * q + min(x, r) + (b >> 3);
-    const uint32_t band = t / (kBand * tiles_n), in = t - band * kBand * tiles_n;
-    const uint32_t rows = min(static_cast<uint32_t>(kBand), tiles_m - band * kBand);
-    tm = band * kBand + in % rows;
-    tn = in / rows;
+// Waits for all but the last N loads from memory of this wave, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void barrier_but_last() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 template <int KIND, int DT, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const ProductArgs p, uint32_t tiles_m, uint32_t tiles_n) {
+__device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, int32_t n0, uint8_t* lds) {
     using S = TileShape<TM, TN, WM, WN>;
-    __shared__ __attribute__((aligned(128))) uint8_t lds[2 * S::stage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = (wave / WN) * TM * 16, wn = (wave % WN) * TN * 16;
-    uint32_t tm, tn;
-    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
-    const int32_t m0 = static_cast<int32_t>(tm) * S::bm, n0 = static_cast<int32_t>(tn) * S::bn;
+    float* a_steps = reinterpret_cast<float*>(lds + S::work);
+    float* b_steps = a_steps + S::bm;
+    float* b_bias = b_steps + S::bn;
+    int32_t* b_ones = reinterpret_cast<int32_t*>(b_bias + S::bn);
 
     // A wave's load brings 8 rows of 128 bytes to 1 KB of LDS, lane l the 16 bytes at l * 16 there.  Piece c of
     // row r lies at place c ^ (r & 7), so that the 16 rows of a fragment spread over all banks.
@@ -262,12 +216,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
     uint32_t off_a[S::loads_a], off_b[S::loads_b];
 #pragma unroll
     for (int i = 0; i < S::loads_a; ++i)
-        off_a[i] = static_cast<uint32_t>(min((wave * S::loads_a + i) * 8 + lr, p.m - 1 - m0)) * static_cast<uint32_t>(p.lda);
+        off_a[i] = static_cast<uint32_t>(min((i * S::waves + wave) * 8 + lr, p.m - 1 - m0)) * static_cast<uint32_t>(p.lda);
 #pragma unroll
-    for (int i = 0; i < S::loads_b; ++i) {
-        const int r = (wave * S::loads_b + i) * 8 + lr;
-        off_b[i] = row_from<KIND>(n0, r, p.n) * static_cast<uint32_t>(p.ldb);
-    }
+    for (int i = 0; i < S::loads_b; ++i) off_b[i] = row_from<KIND>(n0, (i * S::waves + wave) * 8 + lr, p.n) * static_cast<uint32_t>(p.ldb);
     const int32_t halves = (p.k + 63) / 64, steps = (halves + 1) / 2;
     const int32_t last_a = (KIND == kMessage ? p.k : halves * 64) - 16, last_b = halves * 64 - 16;
     auto bring = [&](int32_t step, int buf) {
@@ -275,14 +226,38 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
         const uint32_t ka = min(k, last_a), kb = min(k, last_b);
         uint8_t* to = lds + buf * S::stage;
 #pragma unroll
-        for (int i = 0; i < S::loads_a; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr)(base_a + (off_a[i] + ka)), (lds_ptr)(to + (wave * S::loads_a + i) * 1024), 16, 0, 0);
+        for (int i = 0; i < S::loads_a; ++i) {
+            const int at = i * S::waves + wave;
+            if (S::bm / 8 % S::waves == 0 || at < S::bm / 8)
+                __builtin_amdgcn_global_load_lds((global_ptr)(base_a + (off_a[i] + ka)), (lds_ptr)(to + at * 1024), 16, 0, 0);
+        }
 #pragma unroll
         for (int i = 0; i < S::loads_b; ++i) {
-            const int8_t* b = KIND == kGated && (((wave * S::loads_b + i) * 8) & 16) ? base_u : base_b;
-            __builtin_amdgcn_global_load_lds((global_ptr)(b + (off_b[i] + kb)), (lds_ptr)(to + S::bm * S::row + (wave * S::loads_b + i) * 1024), 16, 0, 0);
+            const int at = i * S::waves + wave;
+            const int8_t* b = KIND == kGated && (at & 2) ? base_u : base_b;
+            if (S::bn / 8 % S::waves == 0 || at < S::bn / 8)
+                __builtin_amdgcn_global_load_lds((global_ptr)(b + (off_b[i] + kb)), (lds_ptr)(to + S::bm * S::row + at * 1024), 16, 0, 0);
         }
     };
+    // What the end needs is asked for first and lies in LDS by then: nothing is waited for there.
+    static_assert(S::bm <= 64 * S::waves && S::bn <= 64 * S::waves, "a lane for every row and column");
+    const int t = threadIdx.x;
+    float a_scale = 0.0f, b_scale = 0.0f, b_add = 0.0f;
+    if (t < S::bm) a_scale = p.a_scales[min(m0 + t, p.m - 1)];
+    if (t < S::bn) {
+        const int32_t r = static_cast<int32_t>(row_from<KIND>(n0, t, p.n)) + (KIND == kGated ? (n0 >> 1) + ((t & 16) ? half : 0) : n0);
+        b_scale = p.b_scales[r];
+        if (p.bias) b_add = load_elem<DT>(p.bias, r);
+    }
+    if (steps > 0) {
+        bring(0, 0);
+        bring(min(1, steps - 1), 1);
+    }
+    if (t < S::bm) a_steps[t] = Finish<KIND, DT, 16 * TN>::step_of_a(a_scale);
+    if (t < S::bn) {
+        b_steps[t] = b_scale / kCodeHalf;
+        b_bias[t] = b_add;
+    }
     // Fragments: lane l holds 16 bytes of row l % 16, piece (l / 16) of the half step.
     const int fr = lane & 15, fq = lane >> 4;
     const int at0 = fr * S::row + ((fq ^ (fr & 7)) * 16), at1 = at0 ^ 64;
@@ -295,16 +270,19 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
     };
     i32x4_t acc[TM][TN] = {};
     int32_t ones[TN] = {};
-    auto multiply = [&](i32x4_t (&fa)[TM], i32x4_t (&fb)[TN]) {
+    // Of the WM waves that hold the same columns of b, each adds up the codes of every WM-th half step.
+    auto multiply = [&](i32x4_t (&fa)[TM], i32x4_t (&fb)[TN], int32_t h) {
         if constexpr (KIND == kMessage) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) fa[i][e] ^= static_cast<int32_t>(0x80808080u);      // level - 128
+            if (h % WM == wave / WN) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+                for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) ones[j] = __builtin_amdgcn_sdot4(fb[j][e], 0x01010101, ones[j], false);
+                    for (int e = 0; e < 4; ++e) ones[j] = __builtin_amdgcn_sdot4(fb[j][e], 0x01010101, ones[j], false);
+            }
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -312,29 +290,128 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
             for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
     };
     i32x4_t fa0[TM], fb0[TN], fa1[TM], fb1[TN];
+    // The schedule of a half step: its products with the other accesses between them, so that none of them holds the
+    // wave's products back (a load takes the memory pipe 16 cycles, and eight waves issue theirs at once).
+    const auto interleave = [&](auto loads) {
+        constexpr int ds = TM + TN, n = TM * TN, vm = decltype(loads)::value;
+        constexpr int pairs = vm > 0 ? (ds + 1) / 2 : ds;                  // products between the reads
+        constexpr int each = vm > 0 ? (n - pairs > vm ? (n - pairs) / (vm > 0 ? vm : 1) : 1) : (n / pairs > 1 ? 2 : 1);
+#pragma unroll
+        for (int i = 0; i < pairs; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, vm > 0 ? 2 : 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, vm > 0 ? 1 : each, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < vm; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, each, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, n, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
     if (steps > 0) {
-        bring(0, 0);
-        __syncthreads();
-        bring(min(1, steps - 1), 1);
+        barrier_but_last<S::loads_least>();
         read_frags(fa0, fb0, 0, 0);
         for (int32_t s = 0; s < steps - 1; ++s) {
             const int buf = s & 1;
             read_frags(fa1, fb1, buf, 1);
-            multiply(fa0, fb0);
-            __builtin_amdgcn_sched_barrier(0);
-            __syncthreads();                             // step s + 1 has arrived; no wave reads step s any more
-            bring(min(s + 2, steps - 1), buf);           // the last one once more: nobody reads it
+            multiply(fa0, fb0, 2 * s);
+            interleave(std::integral_constant<int, 0>());
+            barrier_but_last<0>();                       // step s + 1 has arrived; no wave reads step s any more
             read_frags(fa0, fb0, buf ^ 1, 0);
-            multiply(fa1, fb1);
-            __builtin_amdgcn_sched_barrier(0);
+            bring(min(s + 2, steps - 1), buf);           // the last one once more: nobody reads it
+            multiply(fa1, fb1, 2 * s + 1);
+            interleave(std::integral_constant<int, S::loads_a + S::loads_b>());
         }
         if (halves % 2 == 0) read_frags(fa1, fb1, (steps - 1) & 1, 1);
-        multiply(fa0, fb0);
-        if (halves % 2 == 0) multiply(fa1, fb1);
+        multiply(fa0, fb0, 2 * steps - 2);
+        if (halves % 2 == 0) multiply(fa1, fb1, 2 * steps - 1);
     }
-    static_assert(store_bytes(TM, TN) * S::waves <= 2 * S::stage && TM % kStoreBlocks == 0, "the stages' LDS serves the results");
-    __syncthreads();                         // the last fragments have been read
-    store_tile<KIND, DT, TM, TN>(p, acc, ones, m0 + wm, n0 + wn, lane, reinterpret_cast<int32_t*>(lds + wave * store_bytes(TM, TN)));
+    if constexpr (KIND == kMessage) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            int32_t v = ones[j];
+            v += __shfl_xor(v, 16, kWave);
+            v += __shfl_xor(v, 32, kWave);
+            if (lane < 16) b_ones[(wave / WN) * S::bn + wn + 16 * j + lane] = v;
+        }
+    }
+    barrier_but_last<0>();                               // the last fragments have been read, the last loads are in
+
+    using F = Finish<KIND, DT, TN * 16>;
+    F finish(p, n0 + wn, lane);
+    finish.take_scales(b_steps + wn, b_bias + wn);
+    if constexpr (KIND == kMessage) finish.take_ones(b_ones + wn, WM, S::bn);
+    int32_t* own = reinterpret_cast<int32_t*>(lds + wave * S::own);
+    int32_t* to = own + fr * S::pitch + fq * 4;
+    constexpr int rows = kStoreBlocks * 16, turns = (rows + F::step_rows - 1) / F::step_rows, ahead = turns % 8 == 0 ? 8 : turns % 4 == 0 ? 4 : turns % 2 == 0 ? 2 : 1;
+    const bool full = m0 + wm + 16 * TM <= p.m && n0 + wn + 16 * TN <= (KIND == kGated ? p.n & ~31 : p.n);     // h is whole sixteens there
+    const int mine = lane / F::wide;
+    const bool busy = F::step_rows * F::wide == kWave || mine < F::step_rows;
+#pragma unroll
+    for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
+#pragma unroll
+        for (int i = 0; i < kStoreBlocks; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(to + i * 16 * S::pitch + 16 * j) = acc[i0 + i][j];
+        const int32_t first = m0 + wm + i0 * 16 + mine;
+        const float* a_step = a_steps + wm + i0 * 16 + mine;
+        if (full && rows % F::step_rows == 0) {
+            if (busy) {
+#pragma unroll 1
+                for (int t = 0; t < turns; t += ahead) {
+                    f32x4_t there[ahead];
+#pragma unroll
+                    for (int u = 0; u < ahead; ++u) there[u] = finish.template added<true>(first + (t + u) * F::step_rows);
+#pragma unroll
+                    for (int u = 0; u < ahead; ++u) {
+                        const int r = (t + u) * F::step_rows;
+                        finish.template row<true>(first + r, a_step[r], there[u], own + (mine + r) * S::pitch);
+                    }
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int r = 0; r < rows; r += F::step_rows) {
+                if (!busy || mine + r >= rows) continue;
+                finish.template row<false>(first + r, a_step[r], finish.template added<false>(first + r), own + (mine + r) * S::pitch);
+            }
+        }
+    }
+}
+
+// Tile t of a grid of tiles: they go down in bands of kBand tile rows, so that the tiles an XCD works on at a time
+// share rows of a and of b in its L2.
+constexpr uint32_t kBand = 4;
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+    const uint32_t band = t / (kBand * tiles_n), in = t - band * kBand * tiles_n;
+    const uint32_t rows = min(kBand, tiles_m - band * kBand);
+    tm = band * kBand + in % rows;
+    tn = in / rows;
+}
+// The eight XCDs take the workgroups in turn, so that b mod 8 is the XCD; each gets a contiguous run of 0 .. total - 1.
+__device__ __forceinline__ uint32_t spread_over_xcds(uint32_t b, uint32_t total) {
+    const uint32_t q = total >> 3, r = total & 7, x = b & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+
+// Workgroups 0 .. wide_tiles_n * tiles_m - 1 take tiles of full width, the others narrower ones (NARROW blocks to a
+// wave) of the columns that are left.
+template <int KIND, int DT, int TM, int TN, int WM, int WN, int NARROW>
+__global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const ProductArgs p, uint32_t tiles_m, uint32_t wide_tiles_n,
+                                                                       uint32_t narrow_tiles_n) {
+    using S = TileShape<TM, TN, WM, WN>;
+    __shared__ __attribute__((aligned(128))) uint8_t lds[S::lds];
+    const uint32_t wide = tiles_m * wide_tiles_n;
+    uint32_t tm, tn;
+    if (NARROW == 0 || blockIdx.x < wide) {
+        tile_of(spread_over_xcds(blockIdx.x, wide), tiles_m, wide_tiles_n, tm, tn);
+        product_tile<KIND, DT, TM, TN, WM, WN>(p, static_cast<int32_t>(tm) * S::bm, static_cast<int32_t>(tn) * S::bn, lds);
+    } else if constexpr (NARROW > 0) {
+        tile_of(spread_over_xcds(blockIdx.x - wide, tiles_m * narrow_tiles_n), tiles_m, narrow_tiles_n, tm, tn);
+        product_tile<KIND, DT, TM, NARROW, WM, WN>(p, static_cast<int32_t>(tm) * S::bm,
+                                                   static_cast<int32_t>(wide_tiles_n) * S::bn + static_cast<int32_t>(tn) * (16 * NARROW * WN), lds);
+    }
 }
 
 // ---- small products ---------------------------------------------------------------------------
@@ -418,6 +495,7 @@ __global__ __launch_bounds__(64 * W) void product_split_kernel(const ProductArgs
     using F = Finish<KIND, DT, 16 * J>;
     constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
     F finish(p, n0, lane);
+    finish.take_scales();
     float a_step[turns];
 #pragma unroll
     for (int t = 0; t < turns; ++t)
@@ -466,26 +544,52 @@ hipError_t launch_split_as(ProductKind kind, const ProductArgs& p, hipStream_t s
     }
 }
 
-template <int DT, int TM, int TN, int WM, int WN>
-hipError_t launch_tiles_as(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
-    using S = TileShape<TM, TN, WM, WN>;
-    const uint32_t tm = (static_cast<uint32_t>(p.m) + S::bm - 1) / S::bm, tn = (static_cast<uint32_t>(p.n) + S::bn - 1) / S::bn;
-    const dim3 grid(tm * tn), block(64 * S::waves);
+// How a product is cut: rows of tiles, columns of tiles of full width, columns of narrower ones.
+struct TilePlan {
+    uint32_t tiles_m, wide_n, narrow_n;
+    int narrow;                                  // blocks to a wave of the narrower ones, 0: none
+};
+
+template <int DT, int TM, int TN, int WM, int WN, int NARROW>
+hipError_t launch_tiles_as(ProductKind kind, const TilePlan& t, const ProductArgs& p, hipStream_t stream) {
+    const dim3 grid(t.tiles_m * (t.wide_n + t.narrow_n)), block(64 * WM * WN);
     switch (kind) {
-    case kPlain:      return launch_kernel(product_tile_kernel<kPlain, DT, TM, TN, WM, WN>, grid, block, stream, p, tm, tn);
-    case kMessage:    return launch_kernel(product_tile_kernel<kMessage, DT, TM, TN, WM, WN>, grid, block, stream, p, tm, tn);
-    case kActivation: return launch_kernel(product_tile_kernel<kActivation, DT, TM, TN, WM, WN>, grid, block, stream, p, tm, tn);
-    default:          return launch_kernel(product_tile_kernel<kGated, DT, TM, TN, WM, WN>, grid, block, stream, p, tm, tn);
+    case kPlain:
+        return launch_kernel(product_tile_kernel<kPlain, DT, TM, TN, WM, WN, NARROW>, grid, block, stream, p, t.tiles_m, t.wide_n, t.narrow_n);
+    case kMessage:
+        return launch_kernel(product_tile_kernel<kMessage, DT, TM, TN, WM, WN, NARROW>, grid, block, stream, p, t.tiles_m, t.wide_n, t.narrow_n);
+    case kActivation:
+        return launch_kernel(product_tile_kernel<kActivation, DT, TM, TN, WM, WN, NARROW>, grid, block, stream, p, t.tiles_m, t.wide_n, t.narrow_n);
+    default:
+        if constexpr (NARROW % 2 == 0)           // the gate's columns come in pairs of sixteen
+            return launch_kernel(product_tile_kernel<kGated, DT, TM, TN, WM, WN, NARROW>, grid, block, stream, p, t.tiles_m, t.wide_n, t.narrow_n);
+        else return hipErrorInvalidValue;
     }
 }
 
-enum ProductTile { kTile256 = 0, kTile128, kSplit64, kSplit64x32, kSplit32, kSplit16, kSplit16x32 };
+template <int DT>
+hipError_t launch_tiles256_dt(ProductKind kind, const TilePlan& t, const ProductArgs& p, hipStream_t stream) {
+    switch (t.narrow) {
+    case 0: return launch_tiles_as<DT, 4, 8, 4, 2, 0>(kind, t, p, stream);
+    case 2: return launch_tiles_as<DT, 4, 8, 4, 2, 2>(kind, t, p, stream);
+    case 3: return launch_tiles_as<DT, 4, 8, 4, 2, 3>(kind, t, p, stream);
+    case 4: return launch_tiles_as<DT, 4, 8, 4, 2, 4>(kind, t, p, stream);
+    case 5: return launch_tiles_as<DT, 4, 8, 4, 2, 5>(kind, t, p, stream);
+    case 6: return launch_tiles_as<DT, 4, 8, 4, 2, 6>(kind, t, p, stream);
+    default: return launch_tiles_as<DT, 4, 8, 4, 2, 7>(kind, t, p, stream);
+    }
+}
 
 template <int DT>
-hipError_t launch_product_dt(ProductTile tile, ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+hipError_t launch_tiles128_dt(ProductKind kind, const TilePlan& t, const ProductArgs& p, hipStream_t stream) {
+    return launch_tiles_as<DT, 4, 4, 2, 2, 0>(kind, t, p, stream);
+}
+
+enum SplitTile { kSplit64 = 0, kSplit64x32, kSplit32, kSplit16, kSplit16x32 };
+
+template <int DT>
+hipError_t launch_split_dt(SplitTile tile, ProductKind kind, const ProductArgs& p, hipStream_t stream) {
     switch (tile) {
-    case kTile256: return launch_tiles_as<DT, 8, 4, 2, 4>(kind, p, stream);
-    case kTile128: return launch_tiles_as<DT, 4, 4, 2, 2>(kind, p, stream);
     case kSplit64: return launch_split_as<DT, 4, 4, 8>(kind, p, stream);
     case kSplit64x32: return launch_split_as<DT, 4, 2, 8>(kind, p, stream);
     case kSplit32: return launch_split_as<DT, 2, 2, 8>(kind, p, stream);
@@ -493,5 +597,10 @@ hipError_t launch_product_dt(ProductTile tile, ProductKind kind, const ProductAr
     default:       return launch_split_as<DT, 1, 2, 8>(kind, p, stream);
     }
 }
+
+#define AQSGD_PRODUCT_DT(EXTERN, DT)                                                                                        \
+    EXTERN template hipError_t launch_tiles256_dt<DT>(ProductKind, const TilePlan&, const ProductArgs&, hipStream_t);      \
+    EXTERN template hipError_t launch_tiles128_dt<DT>(ProductKind, const TilePlan&, const ProductArgs&, hipStream_t);      \
+    EXTERN template hipError_t launch_split_dt<DT>(SplitTile, ProductKind, const ProductArgs&, hipStream_t);
 
 }  // namespace aqsgd

@@ -1,6 +1,6 @@
-// Tiles of 8-bit products with bfloat16 results.
+// 8-bit products with bfloat16 results.
 #include "aqsgd_matmul8.h"
 
 namespace aqsgd {
-template hipError_t launch_product_dt<AQSGD_BF16>(ProductTile, ProductKind, const ProductArgs&, hipStream_t);
+AQSGD_PRODUCT_DT(, AQSGD_BF16)
 }

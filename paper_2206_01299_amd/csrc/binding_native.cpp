@@ -14,6 +14,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -44,10 +45,20 @@ struct Api {
     decltype(&aqsgd_grad_topk_quant) grad_topk_quant;
     decltype(&aqsgd_grad_topk_dequant) grad_topk_dequant;
     decltype(&aqsgd_run_jobs) run_jobs;
+    decltype(&aqsgd_quant8_stride) quant8_stride;
+    decltype(&aqsgd_quant8_workspace_bytes) quant8_workspace_bytes;
+    decltype(&aqsgd_quant8) quant8;
+    decltype(&aqsgd_matmul8_workspace_bytes) matmul8_workspace_bytes;
+    decltype(&aqsgd_matmul8) matmul8;
+    decltype(&aqsgd_ffn8) ffn8;
+    decltype(&aqsgd_ffn8_grad) ffn8_grad;
 };
 Api g_api;
 PyTypeObject* g_desc_type = nullptr;      // the binding's ctypes mirrors of aqsgd_desc and aqsgd_job
 PyTypeObject* g_job_type = nullptr;
+PyTypeObject* g_quant8_type = nullptr;    // and of the descriptors of the 8-bit operators
+PyTypeObject* g_matmul8_type = nullptr;
+PyTypeObject* g_ffn8_type = nullptr;
 
 // The memory of a ctypes structure of exactly this type, while the view lives.
 class View {
@@ -145,8 +156,8 @@ struct Call {
     }
 };
 
-template <typename F>
-PyObject* launch(const Call& c, F&& f) {
+template <typename C, typename F>
+PyObject* launch(const C& c, F&& f) {
     if (!c.ok) Py_RETURN_NONE;
     int status;
     Py_BEGIN_ALLOW_THREADS
@@ -284,6 +295,130 @@ AQSGD_ENTRY(py_grad_topk_dequant, 7, {
     return launch(c, [&] { return g_api.grad_topk_dequant(&c.d, keep, m.bitmap, m.codes, m.scales, out, s); });
 })
 
+// ---- products of 8-bit matrices ------------------------------------------------------------
+bool known_type(int32_t dtype, c10::ScalarType& type) {
+    switch (dtype) {
+    case AQSGD_F32:  type = c10::ScalarType::Float; return true;
+    case AQSGD_F16:  type = c10::ScalarType::Half; return true;
+    case AQSGD_BF16: type = c10::ScalarType::BFloat16; return true;
+    default:         return false;
+    }
+}
+
+// A call of these operators: tensors of exact shapes on the current device; None where one may be left out.
+template <typename Desc>
+struct Call8 {
+    Desc d = {};
+    c10::ScalarType type = c10::ScalarType::Float;
+    bool ok = false;
+    int device;
+
+    Call8(PyObject* desc, PyTypeObject* mirror) : device(c10::hip::current_device()) {
+        View v(desc, mirror, sizeof(Desc));
+        if (!v) return;
+        std::memcpy(&d, v.template as<Desc>(), sizeof d);
+        ok = known_type(d.dtype, type);
+    }
+    const at::Tensor* on_device(PyObject* o, c10::ScalarType t) {
+        if (!ok || !THPVariable_CheckExact(o)) { ok = false; return nullptr; }
+        const at::Tensor& x = THPVariable_Unpack(o);
+        ok = x.is_cuda() && x.scalar_type() == t && x.get_device() == device;
+        return ok ? &x : nullptr;
+    }
+    void* matrix(PyObject* o, c10::ScalarType t, int64_t rows, int64_t cols, bool optional = false) {
+        if (optional && o == Py_None) return nullptr;
+        const at::Tensor* x = on_device(o, t);
+        ok = x && x->dim() == 2 && x->size(0) == rows && x->size(1) == cols && x->is_contiguous();
+        return ok ? x->data_ptr() : nullptr;
+    }
+    void* vector(PyObject* o, c10::ScalarType t, int64_t n, bool optional = false) {
+        if (optional && o == Py_None) return nullptr;
+        const at::Tensor* x = on_device(o, t);
+        ok = x && x->dim() == 1 && x->size(0) == n && x->is_contiguous();
+        return ok ? x->data_ptr() : nullptr;
+    }
+    void* at_least(PyObject* o, c10::ScalarType t, int64_t n) {
+        const at::Tensor* x = on_device(o, t);
+        ok = x && x->numel() >= n && x->is_contiguous();
+        return ok ? x->data_ptr() : nullptr;
+    }
+    // The caller's workspace; a call that needs one and brings none goes back, to be given some.
+    void* workspace(PyObject* o, size_t need, size_t& bytes) {
+        bytes = 0;
+        if (!ok || (o == Py_None && need == 0)) return nullptr;
+        void* p = at_least(o, c10::ScalarType::Byte, static_cast<int64_t>(need));
+        if (ok) bytes = need;
+        return p;
+    }
+    void* stream(PyObject* o) {
+        if (!ok) return nullptr;
+        if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
+        PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
+        if (!h) { PyErr_Clear(); ok = false; return nullptr; }
+        void* s = PyLong_Check(h) ? PyLong_AsVoidPtr(h) : nullptr;
+        if (!PyLong_Check(h) || PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+        Py_DECREF(h);
+        return s;
+    }
+};
+
+AQSGD_ENTRY(py_quant8, 9, {
+    Call8<aqsgd_quant8_desc> c(p[0], g_quant8_type);
+    const auto f32 = c10::ScalarType::Float; const auto i8 = c10::ScalarType::Char;
+    const at::Tensor* x = c.on_device(p[1], c.type);
+    c.ok = x && x->dim() == 2 && x->size(0) == c.d.rows && x->size(1) == c.d.cols && (c.d.cols <= 1 || x->stride(1) == 1) &&
+           (c.d.rows <= 1 || x->stride(0) == c.d.ld);
+    if (!c.ok) Py_RETURN_NONE;
+    const void* at = x->data_ptr();
+    const int64_t across = static_cast<int64_t>(g_api.quant8_stride(c.d.cols)); const int64_t down = static_cast<int64_t>(g_api.quant8_stride(c.d.rows));
+    auto* rc = static_cast<int8_t*>(c.matrix(p[2], i8, c.d.rows, across, true)); auto* rs = static_cast<float*>(c.vector(p[3], f32, c.d.rows, true));
+    auto* cc = static_cast<int8_t*>(c.matrix(p[4], i8, c.d.cols, down, true)); auto* cs = static_cast<float*>(c.vector(p[5], f32, c.d.cols, true));
+    auto* sums = static_cast<float*>(c.vector(p[6], f32, c.d.cols, true));
+    size_t bytes; void* ws = c.workspace(p[7], c.ok && (p[4] != Py_None || p[6] != Py_None) ? g_api.quant8_workspace_bytes(&c.d) : 0, bytes);
+    void* s = c.stream(p[8]);
+    return launch(c, [&] { return g_api.quant8(&c.d, at, rc, rs, cc, cs, sums, ws, bytes, s); });
+})
+
+AQSGD_ENTRY(py_matmul8, 10, {
+    Call8<aqsgd_matmul8_desc> c(p[0], g_matmul8_type);
+    if (!c.ok) Py_RETURN_NONE;
+    const auto f32 = c10::ScalarType::Float; const auto i8 = c10::ScalarType::Char;
+    const int64_t stride = static_cast<int64_t>(g_api.quant8_stride(c.d.k));
+    int64_t levels;
+    if (__builtin_mul_overflow(c.d.m, c.d.k, &levels)) Py_RETURN_NONE;
+    const void* a = c.d.message ? c.at_least(p[1], c10::ScalarType::Byte, levels) : c.matrix(p[1], i8, c.d.m, stride);
+    auto* sa = static_cast<float*>(c.d.message ? c.at_least(p[2], f32, c.d.m) : c.vector(p[2], f32, c.d.m));
+    auto* b = static_cast<int8_t*>(c.matrix(p[3], i8, c.d.n, stride)); auto* sb = static_cast<float*>(c.vector(p[4], f32, c.d.n));
+    void* out = c.matrix(p[5], c.type, c.d.m, c.d.n);
+    void* bias = c.vector(p[6], c.type, c.d.n, true); void* add = c.matrix(p[7], c.type, c.d.m, c.d.n, true);
+    size_t bytes; void* ws = c.workspace(p[8], c.ok ? g_api.matmul8_workspace_bytes(&c.d) : 0, bytes);
+    void* s = c.stream(p[9]);
+    return launch(c, [&] { return g_api.matmul8(&c.d, a, sa, b, sb, bias, add, out, ws, bytes, s); });
+})
+
+AQSGD_ENTRY(py_ffn8, 9, {
+    Call8<aqsgd_ffn8_desc> c(p[0], g_ffn8_type);
+    int64_t w = 0;
+    if (!c.ok || __builtin_mul_overflow(c.d.f, c.d.gated ? 2 : 1, &w)) Py_RETURN_NONE;
+    const auto f32 = c10::ScalarType::Float; const auto i8 = c10::ScalarType::Char;
+    const int64_t stride = static_cast<int64_t>(g_api.quant8_stride(c.d.k));
+    auto* a = static_cast<int8_t*>(c.matrix(p[1], i8, c.d.m, stride)); auto* sa = static_cast<float*>(c.vector(p[2], f32, c.d.m));
+    auto* b = static_cast<int8_t*>(c.matrix(p[3], i8, w, stride)); auto* sb = static_cast<float*>(c.vector(p[4], f32, w));
+    void* h = c.matrix(p[5], c.type, c.d.m, c.d.f); void* bias = c.vector(p[6], c.type, w, true);
+    void* pre = c.matrix(p[7], c.type, c.d.m, w, true);
+    void* s = c.stream(p[8]);
+    return launch(c, [&] { return g_api.ffn8(&c.d, a, sa, b, sb, bias, h, pre, s); });
+})
+
+AQSGD_ENTRY(py_ffn8_grad, 5, {
+    Call8<aqsgd_ffn8_desc> c(p[0], g_ffn8_type);
+    int64_t w = 0;
+    if (!c.ok || __builtin_mul_overflow(c.d.f, c.d.gated ? 2 : 1, &w)) Py_RETURN_NONE;
+    void* dh = c.matrix(p[1], c.type, c.d.m, c.d.f); void* pre = c.matrix(p[2], c.type, c.d.m, w); void* dpre = c.matrix(p[3], c.type, c.d.m, w);
+    void* s = c.stream(p[4]);
+    return launch(c, [&] { return g_api.ffn8_grad(&c.d, dh, pre, dpre, s); });
+})
+
 // ---- jobs -------------------------------------------------------------------------------
 PyObject* new_job(const Call& c, const aqsgd_job& j) {
     if (!c.ok) Py_RETURN_NONE;
@@ -363,15 +498,18 @@ AQSGD_ENTRY(py_run_jobs, 2, {
     return PyLong_FromLong(status);
 })
 
-// setup(Desc, Job, {name: address}): called once by binding.py after it has loaded the library.
+// setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, {name: address}): called once by binding.py after it has loaded
+// the library.
 PyObject* py_setup(PyObject*, PyObject* const* p, Py_ssize_t np) {
-    if (np != 3 || !PyType_Check(p[0]) || !PyType_Check(p[1]) || !PyDict_Check(p[2])) {
-        PyErr_SetString(PyExc_TypeError, "setup(Desc, Job, addresses)");
+    bool types = np == 6;
+    for (Py_ssize_t i = 0; types && i < 5; ++i) types = PyType_Check(p[i]);
+    if (!types || !PyDict_Check(p[5])) {
+        PyErr_SetString(PyExc_TypeError, "setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, addresses)");
         return nullptr;
     }
 #define AQSGD_TAKE(name)                                                              \
     {                                                                                 \
-        PyObject* a = PyDict_GetItemString(p[2], "aqsgd_" #name);                     \
+        PyObject* a = PyDict_GetItemString(p[5], "aqsgd_" #name);                     \
         void* f = a ? PyLong_AsVoidPtr(a) : nullptr;                                  \
         if (!f) {                                                                     \
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "aqsgd_" #name);   \
@@ -383,10 +521,13 @@ PyObject* py_setup(PyObject*, PyObject* const* p, Py_ssize_t np) {
     AQSGD_TAKE(topk_codes_bytes) AQSGD_TAKE(encode) AQSGD_TAKE(decode) AQSGD_TAKE(grad_quant)
     AQSGD_TAKE(grad_dequant) AQSGD_TAKE(seed) AQSGD_TAKE(encode_seen) AQSGD_TAKE(decode_seen)
     AQSGD_TAKE(encode_lowbit) AQSGD_TAKE(decode_lowbit) AQSGD_TAKE(grad_topk_quant)
-    AQSGD_TAKE(grad_topk_dequant) AQSGD_TAKE(run_jobs)
+    AQSGD_TAKE(grad_topk_dequant) AQSGD_TAKE(run_jobs) AQSGD_TAKE(quant8_stride) AQSGD_TAKE(quant8_workspace_bytes)
+    AQSGD_TAKE(quant8) AQSGD_TAKE(matmul8_workspace_bytes) AQSGD_TAKE(matmul8) AQSGD_TAKE(ffn8) AQSGD_TAKE(ffn8_grad)
 #undef AQSGD_TAKE
-    Py_INCREF(p[0]);
-    Py_INCREF(p[1]);
+    for (Py_ssize_t i = 0; i < 5; ++i) Py_INCREF(p[i]);
+    g_quant8_type = reinterpret_cast<PyTypeObject*>(p[2]);
+    g_matmul8_type = reinterpret_cast<PyTypeObject*>(p[3]);
+    g_ffn8_type = reinterpret_cast<PyTypeObject*>(p[4]);
     g_desc_type = reinterpret_cast<PyTypeObject*>(p[0]);
     g_job_type = reinterpret_cast<PyTypeObject*>(p[1]);
     Py_RETURN_NONE;
@@ -399,6 +540,7 @@ PyMethodDef methods[] = {
     AQSGD_METHOD(encode_lowbit), AQSGD_METHOD(decode_lowbit), AQSGD_METHOD(grad_topk_quant),
     AQSGD_METHOD(grad_topk_dequant), AQSGD_METHOD(encode_job), AQSGD_METHOD(decode_job),
     AQSGD_METHOD(grad_quant_job), AQSGD_METHOD(grad_dequant_job), AQSGD_METHOD(run_jobs),
+    AQSGD_METHOD(quant8), AQSGD_METHOD(matmul8), AQSGD_METHOD(ffn8), AQSGD_METHOD(ffn8_grad),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "The binding's per-call work (see binding.py).", -1, methods,
