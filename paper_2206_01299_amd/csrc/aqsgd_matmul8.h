@@ -43,28 +43,60 @@ struct Finish {
             place = c;
         }
     }
-    // Scales and bias of the lane's columns from memory ...
-    __device__ __forceinline__ f32x4_t steps(int32_t c) const {
+    // Scales and bias of the lane's columns from memory (to be settled once they are needed) ...
+    __device__ __forceinline__ f32x4_t scales(int32_t c, bool whole) const {
+        if (whole) return *reinterpret_cast<const f32x4_any_t*>(p.b_scales + c);
         f32x4_t v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = p.b_scales[c + (e < left ? e : 0)] / kCodeHalf;
+        for (int e = 0; e < 4; ++e) v[e] = p.b_scales[c + (e < left ? e : 0)];
         return v;
     }
-    __device__ __forceinline__ f32x4_t biases(int32_t c) const {
+    __device__ __forceinline__ f32x4_t biases(int32_t c, bool whole) const {          // bits, as they are stored
         f32x4_t v = {0, 0, 0, 0};
-        if (p.bias) {
+        if (!p.bias) return v;
+        if constexpr (DT == AQSGD_F32) {
+            const float* b = static_cast<const float*>(p.bias) + c;
+            if (whole) return *reinterpret_cast<const f32x4_any_t*>(b);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = load_elem<DT>(p.bias, c + (e < left ? e : 0));
+            for (int e = 0; e < 4; ++e) v[e] = b[e < left ? e : 0];
+        } else {
+            const uint16_t* b = static_cast<const uint16_t*>(p.bias) + c;
+            u16x4_any_t w;
+            if (whole) {
+                w = *reinterpret_cast<const u16x4_any_t*>(b);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = b[e < left ? e : 0];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(static_cast<uint32_t>(w[e]));
         }
         return v;
     }
-    __device__ __forceinline__ void take_scales() {
+    static __device__ __forceinline__ float value_of(float bits) {
+        if constexpr (DT == AQSGD_F32) return bits;
+        else if constexpr (DT == AQSGD_F16) return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(__float_as_uint(bits))));
+        else return bf16_bits_to_f32(__float_as_uint(bits));
+    }
+    // whole: all of the tile's columns exist.
+    __device__ __forceinline__ void ask_scales(bool whole) {
         const int32_t at = left > 0 ? n : 0;
-        step = steps(at);
-        bias = biases(at);
+        step = scales(at, whole);
+        bias = biases(at, whole);
         if constexpr (KIND == kGated) {
-            step_u = steps(half + at);
-            bias_u = biases(half + at);
+            step_u = scales(half + at, whole);
+            bias_u = biases(half + at, whole);
+        }
+    }
+    __device__ __forceinline__ void settle_scales() {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            step[e] = step[e] / kCodeHalf;
+            bias[e] = value_of(bias[e]);
+            if constexpr (KIND == kGated) {
+                step_u[e] = step_u[e] / kCodeHalf;
+                bias_u[e] = value_of(bias_u[e]);
+            }
         }
     }
     // ... or from LDS, by virtual column.
@@ -418,14 +450,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
 // 16 R x 16 J sums to a workgroup, its W waves sharing out k in pieces of 128 bytes: nothing is staged, every wave
 // loads the fragments of its pieces from memory into registers, the next ones while it multiplies, and the waves'
 // sums meet in LDS once, at the end.
-template <int R, int J> struct SplitShape {
-    static constexpr int pieces = R + J >= 4 ? 1 : R + J == 3 ? 2 : 3;        // on their way at a time: registers
+template <int KIND, int R, int J> struct SplitShape {
+    // Pieces that are asked for together, twice over: as many as leave the registers of four waves to a SIMD.
+    static constexpr int most = R + J >= 4 ? 1 : R + J == 3 ? 2 : 3;
+    static constexpr int pieces = most > 1 && (KIND == kMessage || KIND == kGated) ? most - 1 : most;
+    static constexpr int waves = R + J <= 4 ? 4 : 2;                          // of a SIMD: two workgroups to a CU, or one
     static constexpr int pitch = 16 * J + 4;
 };
 
 template <int KIND, int DT, int R, int J, int W>
-__global__ __launch_bounds__(64 * W) void product_split_kernel(const ProductArgs p, uint32_t tiles_n) {
-    using S = SplitShape<R, J>;
+__global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void product_split_kernel(const ProductArgs p, uint32_t tiles_n) {
+    using S = SplitShape<KIND, R, J>;
     constexpr int P = S::pieces, slab = 16 * R * S::pitch;
     __shared__ __attribute__((aligned(16))) int32_t sums[W * slab];
     __shared__ int32_t ones_of[KIND == kMessage ? W * 16 * J : 1];
@@ -495,11 +530,11 @@ __global__ __launch_bounds__(64 * W) void product_split_kernel(const ProductArgs
     using F = Finish<KIND, DT, 16 * J>;
     constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
     F finish(p, n0, lane);
-    finish.take_scales();
+    finish.ask_scales(n0 + 16 * J <= (KIND == kGated ? p.n & ~31 : p.n));         // h is whole sixteens there
     float a_step[turns];
 #pragma unroll
     for (int t = 0; t < turns; ++t)
-        a_step[t] = F::step_of_a(p.a_scales[min(m0 + static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows, p.m - 1)]);
+        a_step[t] = p.a_scales[min(m0 + static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows, p.m - 1)];
     for (int32_t at = wave; at < whole; at += 2 * P * W) {
         load(y, at + P * W);
         multiply(x);
@@ -523,10 +558,11 @@ __global__ __launch_bounds__(64 * W) void product_split_kernel(const ProductArgs
     }
     __syncthreads();
     if constexpr (KIND == kMessage) finish.take_ones(ones_of, W, 16 * J);
+    finish.settle_scales();
 #pragma unroll
     for (int t = 0; t < turns; ++t) {
         const int r = static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows;
-        if (r < 16 * R) finish.template row<false, W>(m0 + r, a_step[t], finish.template added<false>(m0 + r), sums + r * S::pitch, slab);
+        if (r < 16 * R) finish.template row<false, W>(m0 + r, F::step_of_a(a_step[t]), finish.template added<false>(m0 + r), sums + r * S::pitch, slab);
     }
 }
 
