@@ -124,8 +124,7 @@ struct Finish {
         for (int e = 0; e < 4; ++e) {
             float x = static_cast<float>(sum[e]);
             if constexpr (KIND == kMessage) x += extra[e];
-            v[e] = x * a_step * st[e];
-            if (p.bias) v[e] += bi[e];
+            v[e] = x * a_step * st[e] + bi[e];          // without a bias: 0
         }
         return v;
     }
@@ -140,12 +139,12 @@ struct Finish {
         }
     }
     static __device__ __forceinline__ float step_of_a(float scale) { return scale / (KIND == kMessage ? kLevelHalf : kCodeHalf); }
-    // What is there already in a row's columns (the plain product with something to add to).
-    template <bool FULL>
+    // What is there already in a row's columns, or 0.
+    template <bool FULL, bool ADD>
     __device__ __forceinline__ f32x4_t added(int32_t m) const {
         f32x4_t v = {0, 0, 0, 0};
-        if constexpr (KIND == kPlain || KIND == kMessage) {
-            if (p.add && (FULL || (m < p.m && left > 0))) {
+        if constexpr (ADD) {
+            if (FULL || (m < p.m && left > 0)) {
                 const int64_t at = static_cast<int64_t>(m) * p.n + n;
                 if (FULL || left >= 4) {
                     v = load4(DT, p.add, at);
@@ -187,7 +186,7 @@ struct Finish {
                 if (p.pre) put<FULL>(p.pre, at, v);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = activation(p.act, v[e]);
-            } else if (p.add) {
+            } else {
                 v += there;
             }
             put<FULL>(p.out, at, v);
@@ -376,40 +375,46 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
     if constexpr (KIND == kMessage) finish.take_ones(b_ones + wn, WM, S::bn);
     int32_t* own = reinterpret_cast<int32_t*>(lds + wave * S::own);
     int32_t* to = own + fr * S::pitch + fq * 4;
-    constexpr int rows = kStoreBlocks * 16, turns = (rows + F::step_rows - 1) / F::step_rows, ahead = turns % 8 == 0 ? 8 : turns % 4 == 0 ? 4 : turns % 2 == 0 ? 2 : 1;
+    constexpr int rows = kStoreBlocks * 16, turns = (rows + F::step_rows - 1) / F::step_rows;
+    constexpr int ahead = turns % 8 == 0 ? 8 : turns % 4 == 0 ? 4 : turns % 2 == 0 ? 2 : 1;
     const bool full = m0 + wm + 16 * TM <= p.m && n0 + wn + 16 * TN <= (KIND == kGated ? p.n & ~31 : p.n);     // h is whole sixteens there
     const int mine = lane / F::wide;
     const bool busy = F::step_rows * F::wide == kWave || mine < F::step_rows;
+    const auto store = [&](auto adds) {
+        constexpr bool ADD = decltype(adds)::value;
 #pragma unroll
-    for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
+        for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
 #pragma unroll
-        for (int i = 0; i < kStoreBlocks; ++i)
+            for (int i = 0; i < kStoreBlocks; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(to + i * 16 * S::pitch + 16 * j) = acc[i0 + i][j];
-        const int32_t first = m0 + wm + i0 * 16 + mine;
-        const float* a_step = a_steps + wm + i0 * 16 + mine;
-        if (full && rows % F::step_rows == 0) {
-            if (busy) {
+                for (int j = 0; j < TN; ++j) *reinterpret_cast<i32x4_t*>(to + i * 16 * S::pitch + 16 * j) = acc[i0 + i][j];
+            const int32_t first = m0 + wm + i0 * 16 + mine;
+            const float* a_step = a_steps + wm + i0 * 16 + mine;
+            if (full && rows % F::step_rows == 0) {
+                if (busy) {
 #pragma unroll 1
-                for (int t = 0; t < turns; t += ahead) {
-                    f32x4_t there[ahead];
+                    for (int t = 0; t < turns; t += ahead) {
+                        f32x4_t there[ahead];
 #pragma unroll
-                    for (int u = 0; u < ahead; ++u) there[u] = finish.template added<true>(first + (t + u) * F::step_rows);
+                        for (int u = 0; u < ahead; ++u) there[u] = finish.template added<true, ADD>(first + (t + u) * F::step_rows);
 #pragma unroll
-                    for (int u = 0; u < ahead; ++u) {
-                        const int r = (t + u) * F::step_rows;
-                        finish.template row<true>(first + r, a_step[r], there[u], own + (mine + r) * S::pitch);
+                        for (int u = 0; u < ahead; ++u) {
+                            const int r = (t + u) * F::step_rows;
+                            finish.template row<true>(first + r, a_step[r], there[u], own + (mine + r) * S::pitch);
+                        }
                     }
                 }
-            }
-        } else {
+            } else {
 #pragma unroll 1
-            for (int r = 0; r < rows; r += F::step_rows) {
-                if (!busy || mine + r >= rows) continue;
-                finish.template row<false>(first + r, a_step[r], finish.template added<false>(first + r), own + (mine + r) * S::pitch);
+                for (int r = 0; r < rows; r += F::step_rows) {
+                    if (!busy || mine + r >= rows) continue;
+                    finish.template row<false>(first + r, a_step[r], finish.template added<false, ADD>(first + r), own + (mine + r) * S::pitch);
+                }
             }
         }
-    }
+    };
+    if ((KIND == kPlain || KIND == kMessage) && p.add) store(std::true_type());
+    else store(std::false_type());
 }
 
 // Tile t of a grid of tiles: they go down in bands of kBand tile rows, so that the tiles an XCD works on at a time
@@ -562,7 +567,10 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
 #pragma unroll
     for (int t = 0; t < turns; ++t) {
         const int r = static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows;
-        if (r < 16 * R) finish.template row<false, W>(m0 + r, F::step_of_a(a_step[t]), finish.template added<false>(m0 + r), sums + r * S::pitch, slab);
+        if (r >= 16 * R) continue;
+        const bool adds = (KIND == kPlain || KIND == kMessage) && p.add;
+        finish.template row<false, W>(m0 + r, F::step_of_a(a_step[t]), adds ? finish.template added<false, true>(m0 + r) : f32x4_t{0, 0, 0, 0},
+                                      sums + r * S::pitch, slab);
     }
 }
 
