@@ -20,7 +20,11 @@ __device__ __forceinline__ uint32_t row_from(int32_t n0, int32_t c, int32_t n) {
 
 // What is left of the sums once they lie in LDS as rows of 32-bit integers: a lane takes four columns of every few
 // rows, so that its scales and bias are read once and a row leaves in whole lines.  COLS virtual columns from n0 on.
-template <int KIND, int DT, int COLS>
+//
+// STREAM: a large product's results go past the caches, in which they would take the room of the rows of a and b that
+// other tiles still need: 4096 x 12800 x 1600 gated, with what the backward pass needs, 125.4 us with ordinary stores,
+// 106.6 so; 16384 x 16384 x 4096 float32 998 and 927.  Small ones wait for memory then: 48 x 304 x 368 4.0 and 4.3.
+template <int KIND, int DT, int COLS, bool STREAM>
 struct Finish {
     static constexpr int wide = (KIND == kGated ? COLS / 2 : COLS) / 4;       // lanes to a row
     static constexpr int step_rows = kWave / wide;                            // rows a wave takes at a time
@@ -131,7 +135,7 @@ struct Finish {
     template <bool FULL>
     __device__ __forceinline__ void put(void* base, int64_t at, const f32x4_t& v) const {
         if (FULL || left >= 4) {
-            store4(DT, base, at, v);
+            store4<DT, STREAM>(base, at, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 3; ++e)
@@ -147,7 +151,7 @@ struct Finish {
             if (FULL || (m < p.m && left > 0)) {
                 const int64_t at = static_cast<int64_t>(m) * p.n + n;
                 if (FULL || left >= 4) {
-                    v = load4(DT, p.add, at);
+                    v = load4<DT>(p.add, at);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 3; ++e)
@@ -284,7 +288,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
         bring(0, 0);
         bring(min(1, steps - 1), 1);
     }
-    if (t < S::bm) a_steps[t] = Finish<KIND, DT, 16 * TN>::step_of_a(a_scale);
+    if (t < S::bm) a_steps[t] = Finish<KIND, DT, 16 * TN, true>::step_of_a(a_scale);
     if (t < S::bn) {
         b_steps[t] = b_scale / kCodeHalf;
         b_bias[t] = b_add;
@@ -369,7 +373,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
     }
     barrier_but_last<0>();                               // the last fragments have been read, the last loads are in
 
-    using F = Finish<KIND, DT, TN * 16>;
+    using F = Finish<KIND, DT, TN * 16, true>;
     F finish(p, n0 + wn, lane);
     finish.take_scales(b_steps + wn, b_bias + wn);
     if constexpr (KIND == kMessage) finish.take_ones(b_ones + wn, WM, S::bn);
@@ -532,7 +536,7 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
     Frags x, y;
     load(x, wave);
     // what the end needs is asked for now
-    using F = Finish<KIND, DT, 16 * J>;
+    using F = Finish<KIND, DT, 16 * J, false>;
     constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
     F finish(p, n0, lane);
     finish.ask_scales(n0 + 16 * J <= (KIND == kGated ? p.n & ~31 : p.n));         // h is whole sixteens there

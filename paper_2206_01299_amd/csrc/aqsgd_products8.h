@@ -16,47 +16,44 @@ inline int64_t code_stride(int64_t length) { return (length + kCodePad - 1) / kC
 // Four consecutive elements at any element's address.
 typedef uint16_t u16x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
 
-__device__ __forceinline__ f32x4_t load4(int dtype, const void* base, int64_t idx) {
-    f32x4_t v;
-    if (dtype == AQSGD_F32) return *reinterpret_cast<const f32x4_any_t*>(static_cast<const float*>(base) + idx);
-    const u16x4_any_t r = *reinterpret_cast<const u16x4_any_t*>(static_cast<const uint16_t*>(base) + idx);
-    if (dtype == AQSGD_F16) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(r[e])));
+template <int DT>
+__device__ __forceinline__ f32x4_t load4(const void* base, int64_t idx) {
+    if constexpr (DT == AQSGD_F32) {
+        return *reinterpret_cast<const f32x4_any_t*>(static_cast<const float*>(base) + idx);
     } else {
+        const u16x4_any_t r = *reinterpret_cast<const u16x4_any_t*>(static_cast<const uint16_t*>(base) + idx);
+        f32x4_t v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = bf16_bits_to_f32(r[e]);
+        for (int e = 0; e < 4; ++e)
+            v[e] = DT == AQSGD_F16 ? static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(r[e]))) : bf16_bits_to_f32(r[e]);
+        return v;
     }
-    return v;
-}
-
-__device__ __forceinline__ float load1(int dtype, const void* base, int64_t idx) {
-    if (dtype == AQSGD_F32) return load_elem<AQSGD_F32>(base, idx);
-    return dtype == AQSGD_F16 ? load_elem<AQSGD_F16>(base, idx) : load_elem<AQSGD_BF16>(base, idx);
-}
-
-__device__ __forceinline__ void store1(int dtype, void* base, int64_t idx, float v) {
-    if (dtype == AQSGD_F32) store_elem<AQSGD_F32>(base, idx, v);
-    else if (dtype == AQSGD_F16) store_elem<AQSGD_F16>(base, idx, v);
-    else store_elem<AQSGD_BF16>(base, idx, v);
 }
 
 typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(2)));
 
-__device__ __forceinline__ void store4(int dtype, void* base, int64_t idx, const f32x4_t& v) {
-    if (dtype == AQSGD_F32) {
-        *reinterpret_cast<f32x4_any_t*>(static_cast<float*>(base) + idx) = v;
-    } else if (dtype == AQSGD_F16) {
-        typedef _Float16 half4_any_t __attribute__((ext_vector_type(4), aligned(2)));
-        half4_any_t h;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(v[e]);
-        *reinterpret_cast<half4_any_t*>(static_cast<uint16_t*>(base) + idx) = h;
+// STREAM: past the caches, for results of which there are many.
+template <int DT, bool STREAM>
+__device__ __forceinline__ void store4(void* base, int64_t idx, const f32x4_t& v) {
+    if constexpr (DT == AQSGD_F32) {
+        f32x4_any_t* to = reinterpret_cast<f32x4_any_t*>(static_cast<float*>(base) + idx);
+        if constexpr (STREAM) __builtin_nontemporal_store(v, to);
+        else *to = v;
     } else {
         u32x2_any_t w;
-        w[0] = f32x2_to_bf16x2(v[0], v[1]);
-        w[1] = f32x2_to_bf16x2(v[2], v[3]);
-        *reinterpret_cast<u32x2_any_t*>(static_cast<uint16_t*>(base) + idx) = w;
+        if constexpr (DT == AQSGD_F16) {
+            typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+            half4_t h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = static_cast<_Float16>(v[e]);
+            w = __builtin_bit_cast(u32x2_any_t, h);
+        } else {
+            w[0] = f32x2_to_bf16x2(v[0], v[1]);
+            w[1] = f32x2_to_bf16x2(v[2], v[3]);
+        }
+        u32x2_any_t* to = reinterpret_cast<u32x2_any_t*>(static_cast<uint16_t*>(base) + idx);
+        if constexpr (STREAM) __builtin_nontemporal_store(w, to);
+        else *to = w;
     }
 }
 
