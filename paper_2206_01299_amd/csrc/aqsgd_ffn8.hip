@@ -5,57 +5,56 @@
 
 namespace aqsgd {
 
-// Eight elements at any element's address, of which the first `count` exist.
+// A lane's elements: 16 bytes, at any element's address, of which the first `count` exist.  Results go past the caches:
+// 4096 x 6400 float16 gated 48.4 us, with ordinary stores 52.2.
+template <int DT> constexpr int kPiece = DT == AQSGD_F32 ? 4 : 8;
+
 template <int DT>
-__device__ __forceinline__ void load_values(const void* base, int64_t at, int count, float (&f)[kChunk]) {
-    if (count >= kChunk) {
-        const char* p = static_cast<const char*>(base) + at * ElemBytes<DT>::value;
+__device__ __forceinline__ void load_values(const void* base, int64_t at, int count, float (&f)[kPiece<DT>]) {
+    const char* p = static_cast<const char*>(base) + at * ElemBytes<DT>::value;
+    if (count < kPiece<DT>) {
+#pragma unroll
+        for (int e = 0; e < kPiece<DT>; ++e) f[e] = e < count ? load_elem<DT>(base, at + e) : 0.0f;
+    } else if constexpr (DT == AQSGD_F32) {
+        const f32x4_t v = *reinterpret_cast<const f32x4_any_t*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = v[e];
+    } else {
         Raw<DT> r;
-        if constexpr (DT == AQSGD_F32) {
-            r.lo = *reinterpret_cast<const f32x4_any_t*>(p);
-            r.hi = *reinterpret_cast<const f32x4_any_t*>(p + 16);
-        } else {
-            r.v = *reinterpret_cast<const u32x4_any_t*>(p);
-        }
+        r.v = *reinterpret_cast<const u32x4_any_t*>(p);
         unpack_raw<DT>(r, f);
-    } else {
-#pragma unroll
-        for (int e = 0; e < kChunk; ++e) f[e] = e < count ? load_elem<DT>(base, at + e) : 0.0f;
     }
 }
 
 template <int DT>
-__device__ __forceinline__ void store_values(void* base, int64_t at, int count, const float (&f)[kChunk]) {
-    if (count >= kChunk) {
-        char* p = static_cast<char*>(base) + at * ElemBytes<DT>::value;
-        const Raw<DT> r = pack_raw<DT>(f);
-        if constexpr (DT == AQSGD_F32) {
-            *reinterpret_cast<f32x4_any_t*>(p) = r.lo;
-            *reinterpret_cast<f32x4_any_t*>(p + 16) = r.hi;
-        } else {
-            *reinterpret_cast<u32x4_any_t*>(p) = r.v;
-        }
-    } else {
+__device__ __forceinline__ void store_values(void* base, int64_t at, int count, const float (&f)[kPiece<DT>]) {
+    char* p = static_cast<char*>(base) + at * ElemBytes<DT>::value;
+    if (count < kPiece<DT>) {
 #pragma unroll
-        for (int e = 0; e < kChunk - 1; ++e)
+        for (int e = 0; e < kPiece<DT> - 1; ++e)
             if (e < count) store_elem<DT>(base, at + e, f[e]);
+    } else if constexpr (DT == AQSGD_F32) {
+        stream16(p, f32x4_t{f[0], f[1], f[2], f[3]});
+    } else {
+        stream16(p, pack_raw<DT>(f).v);
     }
 }
 
-// A workgroup takes `across` pieces of eight elements of a row, of as many rows as 256 lanes hold.
+// A workgroup takes `across` pieces of a row, of as many rows as 256 lanes hold.
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void ffn8_grad_kernel(const Ffn8GradArgs a, uint32_t across) {
+    constexpr int N = kPiece<DT>;
     const uint32_t ty = threadIdx.x / across, tx = threadIdx.x - ty * across, rows = 256 / across;
-    const int64_t c = (static_cast<int64_t>(blockIdx.x) * across + tx) * kChunk, w = GATED ? 2 * a.f : a.f;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x) * across + tx) * N, w = GATED ? 2 * a.f : a.f;
     if (ty >= rows || c >= a.f) return;
-    const int count = static_cast<int>(min(a.f - c, static_cast<int64_t>(kChunk)));
+    const int count = static_cast<int>(min(a.f - c, static_cast<int64_t>(N)));
     for (int64_t m = static_cast<int64_t>(blockIdx.y) * rows + ty; m < a.m; m += static_cast<int64_t>(gridDim.y) * rows) {
-        float d[kChunk], g[kChunk], u[kChunk];
+        float d[N], g[N], u[N];
         load_values<DT>(a.dh, m * a.f + c, count, d);
         load_values<DT>(a.pre, m * w + c, count, g);
         if constexpr (GATED) load_values<DT>(a.pre, m * w + a.f + c, count, u);
 #pragma unroll
-        for (int e = 0; e < kChunk; ++e) {
+        for (int e = 0; e < N; ++e) {
             float value, slope;
             activation_slope(ACT, g[e], value, slope);
             g[e] = GATED ? d[e] * u[e] * slope : d[e] * slope;
@@ -68,7 +67,7 @@ __global__ __launch_bounds__(256) void ffn8_grad_kernel(const Ffn8GradArgs a, ui
 
 template <int DT, int ACT>
 hipError_t launch_ffn8_grad_as(const Ffn8GradArgs& a, hipStream_t stream) {
-    const int64_t pieces = (a.f + kChunk - 1) / kChunk, across = pieces < 256 ? pieces : 256;
+    const int64_t pieces = (a.f + kPiece<DT> - 1) / kPiece<DT>, across = pieces < 256 ? pieces : 256;
     const int64_t rows = 256 / across, bands = (a.m + rows - 1) / rows;
     const dim3 grid(static_cast<unsigned>((pieces + across - 1) / across), static_cast<unsigned>(bands < 65535 ? bands : 65535)), block(256);
     return a.gated ? launch_kernel(ffn8_grad_kernel<DT, ACT, true>, grid, block, stream, a, static_cast<uint32_t>(across))

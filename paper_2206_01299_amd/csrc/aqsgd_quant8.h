@@ -164,10 +164,11 @@ __device__ __forceinline__ void code_offsets(uint64_t seed, int64_t row, int64_t
     }
 }
 
-// Eight neighbouring codes of a row.
+// Eight neighbouring codes of a row.  Codes go past the caches, which hold the elements for the second pass: 16384 x
+// 4096 float32 both ways 127.5 us, with ordinary stores 138.9.
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void store_row_codes(int8_t* out, const int32_t (&k)[kChunk]) {
-    *reinterpret_cast<u32x2_t*>(out) = u32x2_t{pack_codes(k[0], k[1], k[2], k[3]), pack_codes(k[4], k[5], k[6], k[7])};
+    __builtin_nontemporal_store(u32x2_t{pack_codes(k[0], k[1], k[2], k[3]), pack_codes(k[4], k[5], k[6], k[7])}, reinterpret_cast<u32x2_t*>(out));
 }
 
 // ---- rows alone ---------------------------------------------------------------------------------
@@ -410,8 +411,8 @@ __device__ __forceinline__ void tile_codes(const Quant8Args& a, Raw<DT> (&raw)[4
         const int k = threadIdx.x + 256 * i, col = k / (4 * HALVES), piece = k % (4 * HALVES);
         const int64_t out_c = c0 + col, out_r = r0 + piece * 16;
         if (out_c < a.cols && out_r < a.col_stride)
-            *reinterpret_cast<u32x4_t*>(a.col_codes + out_c * a.col_stride + out_r) =
-                *reinterpret_cast<const u32x4_t*>(&turned[turned_at<HALVES>(col, piece)]);
+            __builtin_nontemporal_store(*reinterpret_cast<const u32x4_t*>(&turned[turned_at<HALVES>(col, piece)]),
+                                        reinterpret_cast<u32x4_t*>(a.col_codes + out_c * a.col_stride + out_r));
     }
     __syncthreads();
 }
