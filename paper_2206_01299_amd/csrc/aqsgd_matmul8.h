@@ -628,9 +628,11 @@ hipError_t launch_tiles256_dt(ProductKind kind, const TilePlan& t, const Product
     }
 }
 
+// Tiles of 128 rows and 128 or 64 columns, two or three workgroups to a CU.
 template <int DT>
-hipError_t launch_tiles128_dt(ProductKind kind, const TilePlan& t, const ProductArgs& p, hipStream_t stream) {
-    return launch_tiles_as<DT, 4, 4, 2, 2, 0>(kind, t, p, stream);
+hipError_t launch_tiles128_dt(int cols, ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+    const TilePlan t{(static_cast<uint32_t>(p.m) + 127) / 128, (static_cast<uint32_t>(p.n) + cols - 1) / cols, 0, 0};
+    return cols == 128 ? launch_tiles_as<DT, 4, 4, 2, 2, 0>(kind, t, p, stream) : launch_tiles_as<DT, 4, 2, 2, 2, 0>(kind, t, p, stream);
 }
 
 enum SplitTile { kSplit64 = 0, kSplit64x32, kSplit32, kSplit16, kSplit16x32 };
@@ -648,7 +650,7 @@ hipError_t launch_split_dt(SplitTile tile, ProductKind kind, const ProductArgs& 
 
 #define AQSGD_PRODUCT_DT(EXTERN, DT)                                                                                        \
     EXTERN template hipError_t launch_tiles256_dt<DT>(ProductKind, const TilePlan&, const ProductArgs&, hipStream_t);      \
-    EXTERN template hipError_t launch_tiles128_dt<DT>(ProductKind, const TilePlan&, const ProductArgs&, hipStream_t);      \
+    EXTERN template hipError_t launch_tiles128_dt<DT>(int, ProductKind, const ProductArgs&, hipStream_t);                  \
     EXTERN template hipError_t launch_split_dt<DT>(SplitTile, ProductKind, const ProductArgs&, hipStream_t);
 
 }  // namespace aqsgd

@@ -21,7 +21,7 @@ template <int DT> struct Tiles256 {
     static hipError_t go(ProductKind k, const TilePlan& t, const ProductArgs& p, hipStream_t s) { return launch_tiles256_dt<DT>(k, t, p, s); }
 };
 template <int DT> struct Tiles128 {
-    static hipError_t go(ProductKind k, const TilePlan& t, const ProductArgs& p, hipStream_t s) { return launch_tiles128_dt<DT>(k, t, p, s); }
+    static hipError_t go(int cols, ProductKind k, const ProductArgs& p, hipStream_t s) { return launch_tiles128_dt<DT>(cols, k, p, s); }
 };
 template <int DT> struct Split {
     static hipError_t go(SplitTile t, ProductKind k, const ProductArgs& p, hipStream_t s) { return launch_split_dt<DT>(t, k, p, s); }
@@ -29,23 +29,25 @@ template <int DT> struct Split {
 
 uint32_t tiles(int64_t n, int64_t side) { return static_cast<uint32_t>((n + side - 1) / side); }
 
-// What a call takes on an idle MI355X, in microseconds, for each kernel: a tile alone, and what every 256 tiles add,
-// both straight lines in k (thousands).  Fitted to 110 products with m, n up to 16384 and k from 16 to 16384, drawn
-// evenly over their logarithms, each timed with every kernel in a captured graph: the mean distance is 8 to 11 %,
-// and the kernel that the lines pick is 1.4 % slower on average than the best one.  Sides measured (us): 1 x 6400 x
-// 1600 4.9 with 16 x 16, 6.6 with 64 x 64, 12.7 with 128 x 128; 512 x 512 x 4096 10.4 with 32 x 32, 17.9 with 16 x 16
-// and with 64 x 64; 777 x 1001 x 1333 8.2 with 64 x 64, 9.8 with 32 x 32, 13.8 with 128 x 128; 1024 x 4096 x 1024 11.6
-// with 128 x 128, 18.5 with 256 x 256, 27 with 64 x 64.
-struct Line { int rows, cols; float alone, alone_k, more, more_k; };
-constexpr Line kTile128Line = {128, 128, 5.2f, 4.36f, 2.4f, 3.68f};
+// What a call takes on an idle MI355X, in microseconds, for each kernel: a tile alone, and what every 256 tiles beyond
+// the first few add, both straight lines in k (thousands).  Fitted to 160 products with m, n up to 16384 and k from 16
+// to 16384, drawn evenly over their logarithms, each timed with every kernel in a captured graph: the mean distance is
+// 7 to 10 %, and the kernel that the lines pick is 2 % slower on average than the best one.  Sides measured (us):
+// 1 x 6400 x 1600 4.9 with 16 x 16, 6.6 with 64 x 64, 12.7 with 128 x 128; 512 x 512 x 4096 10.4 with 32 x 32, 17.9
+// with 16 x 16 and with 64 x 64; 777 x 1001 x 1333 8.2 with 64 x 64, 9.8 with 32 x 32, 13.8 with 128 x 128; 4349 x 449 x
+// 688 7.8 with 128 x 64, 10.2 with 128 x 128, 14.1 with 32 x 32; 1024 x 4096 x 1024 11.6 with 128 x 128, 18.5 with 256 x
+// 256, 27 with 64 x 64; 7373 x 7896 x 383 55.8 with 128 x 128, 77.9 with 128 x 64, whose rows of results are half as
+// long, so it is left out from 1024 tiles on.
+struct Line { int rows, cols; float alone, alone_k, more, more_k, first; };
 constexpr Line kSplitLines[] = {            // by SplitTile
-    {64, 64, 3.9f, 1.84f, 2.7f, 2.93f}, {64, 32, 3.4f, 1.43f, 1.8f, 2.16f}, {32, 32, 3.2f, 0.95f, 0.66f, 1.31f},
-    {16, 16, 3.3f, 0.51f, 0.66f, 0.53f}, {16, 32, 3.3f, 0.73f, 0.64f, 0.90f}};
+    {64, 64, 4.06f, 2.16f, 2.56f, 3.44f, 0.32f}, {64, 32, 3.65f, 1.54f, 1.69f, 2.55f, 0.48f}, {32, 32, 3.41f, 1.13f, 0.77f, 1.48f, 0.62f},
+    {16, 16, 3.46f, 0.61f, 0.72f, 0.59f, 0.57f}, {16, 32, 3.47f, 0.87f, 0.77f, 0.92f, 0.71f}};
+constexpr Line kTile128Line = {128, 128, 4.81f, 4.44f, 2.74f, 3.67f, 0.16f}, kTile128x64Line = {128, 64, 4.08f, 2.61f, 0.92f, 2.43f, 0.0f};
 
 float cost(const Line& l, const ProductArgs& p) {
     const float k = 0.001f * static_cast<float>(p.k);
-    const float many = static_cast<float>(tiles(p.m, l.rows)) * static_cast<float>(tiles(p.n, l.cols)) * (1.0f / 256);
-    return l.alone + l.alone_k * k + many * (l.more + l.more_k * k);
+    const float many = static_cast<float>(tiles(p.m, l.rows)) * static_cast<float>(tiles(p.n, l.cols)) * (1.0f / 256) - l.first;
+    return l.alone + l.alone_k * k + (many > 0.0f ? many * (l.more + l.more_k * k) : 0.0f);
 }
 
 // Tiles of 256 rows, one workgroup to a CU.  A tile of w columns takes 8 us and (0.45 + 0.0043 w) us for every 128
@@ -97,18 +99,4 @@ TilePlan plan256(ProductKind kind, const ProductArgs& p, float& best) {
 }  // namespace
 
 hipError_t launch_product(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
-    int split = -1;
-    float best = cost(kTile128Line, p);
-    for (int t = kSplit64; t <= kSplit16x32; ++t) {
-        if (kind == kGated && t == kSplit16) continue;            // the gate's columns come in pairs of sixteen
-        const float c = cost(kSplitLines[t], p);
-        if (c < best) { best = c; split = t; }
-    }
-    if (split >= 0) return by_dtype<Split>(p.dtype, static_cast<SplitTile>(split), kind, p, stream);
-    float large;
-    const TilePlan plan = plan256(kind, p, large);
-    if (large < best) return by_dtype<Tiles256>(p.dtype, kind, plan, p, stream);
-    return by_dtype<Tiles128>(p.dtype, kind, TilePlan{tiles(p.m, 128), tiles(p.n, 128), 0, 0}, p, stream);
-}
 
-}  // namespace aqsgd
