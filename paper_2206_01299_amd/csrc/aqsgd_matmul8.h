@@ -173,9 +173,15 @@ struct Finish {
     template <bool FULL, int PARTS = 1>
     __device__ __forceinline__ void row(int32_t m, float a_step, const f32x4_t& there, const int32_t* sums, int pitch = 0) const {
         if (!FULL && (m >= p.m || left <= 0)) return;
-        f32x4_t v = scaled(sum_of<PARTS>(sums + place, pitch), a_step, step, bias);
+        i32x4_t u = {0, 0, 0, 0};
+        if constexpr (KIND == kGated) u = sum_of<PARTS>(sums + place + 16, pitch);
+        finish<FULL>(m, a_step, there, sum_of<PARTS>(sums + place, pitch), u);
+    }
+    template <bool FULL>
+    __device__ __forceinline__ void finish(int32_t m, float a_step, const f32x4_t& there, const i32x4_t& sum, const i32x4_t& sum_u) const {
+        f32x4_t v = scaled(sum, a_step, step, bias);
         if constexpr (KIND == kGated) {
-            const f32x4_t u = scaled(sum_of<PARTS>(sums + place + 16, pitch), a_step, step_u, bias_u);
+            const f32x4_t u = scaled(sum_u, a_step, step_u, bias_u);
             f32x4_t h;
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = activation(p.act, v[e]) * u[e];
@@ -458,7 +464,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void product_tile_kernel(const Pro
 // ---- small products ---------------------------------------------------------------------------
 // 16 R x 16 J sums to a workgroup, its W waves sharing out k in pieces of 128 bytes: nothing is staged, every wave
 // loads the fragments of its pieces from memory into registers, the next ones while it multiplies, and the waves'
-// sums meet in LDS once, at the end.
+// sums meet in LDS once, at the end.  Where tiles are few and k is long, the pieces of a tile are shared out over several
+// workgroups (SLICED): each leaves its sums in the workspace, and a second kernel joins and finishes them.
+struct Slices {
+    int32_t* sums;             // [slices, m, pitch], then the sums of b's codes [slices, pitch]
+    int32_t count, pieces;     // of slices; of 128 bytes of k to a slice
+    int32_t pitch;
+};
+
 template <int KIND, int R, int J> struct SplitShape {
     // Pieces that are asked for together, twice over: as many as leave the registers of four waves to a SIMD.
     static constexpr int most = R + J >= 4 ? 1 : R + J == 3 ? 2 : 3;
@@ -467,8 +480,8 @@ template <int KIND, int R, int J> struct SplitShape {
     static constexpr int pitch = 16 * J + 4;
 };
 
-template <int KIND, int DT, int R, int J, int W>
-__global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void product_split_kernel(const ProductArgs p, uint32_t tiles_n) {
+template <int KIND, int DT, int R, int J, int W, bool SLICED>
+__global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void product_split_kernel(const ProductArgs p, uint32_t tiles_n, Slices slices) {
     using S = SplitShape<KIND, R, J>;
     constexpr int P = S::pieces, slab = 16 * R * S::pitch;
     __shared__ __attribute__((aligned(16))) int32_t sums[W * slab];
@@ -486,8 +499,9 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
     for (int i = 0; i < R; ++i) off_a[i] = static_cast<uint32_t>(min(16 * i + fr, p.m - 1 - m0)) * static_cast<uint32_t>(p.lda);
 #pragma unroll
     for (int j = 0; j < J; ++j) off_b[j] = row_from<KIND>(n0, 16 * j + fr, p.n) * static_cast<uint32_t>(p.ldb);
-    const int32_t halves = (p.k + 63) / 64, whole = (halves + 1) / 2;
-    const int32_t last_a = (KIND == kMessage ? p.k : halves * 64) - 16;
+    const int32_t last_a = (KIND == kMessage ? p.k : (p.k + 63) / 64 * 64) - 16;
+    const int32_t slice = SLICED ? static_cast<int32_t>(blockIdx.y) : 0, begin = SLICED ? slice * slices.pieces : 0;
+    const int32_t halves = SLICED ? min((p.k + 63) / 64, 2 * (begin + slices.pieces)) : (p.k + 63) / 64, whole = (halves + 1) / 2;
     struct Frags { i32x4_t a[P][2][R], b[P][2][J]; };
     auto load = [&](Frags& f, int32_t first) {
 #pragma unroll
@@ -534,17 +548,17 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
             }
     };
     Frags x, y;
-    load(x, wave);
+    load(x, begin + wave);
     // what the end needs is asked for now
     using F = Finish<KIND, DT, 16 * J, false>;
     constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
     F finish(p, n0, lane);
-    finish.ask_scales(n0 + 16 * J <= (KIND == kGated ? p.n & ~31 : p.n));         // h is whole sixteens there
+    if (!SLICED) finish.ask_scales(n0 + 16 * J <= (KIND == kGated ? p.n & ~31 : p.n));         // h is whole sixteens there
     float a_step[turns];
 #pragma unroll
-    for (int t = 0; t < turns; ++t)
+    for (int t = 0; t < turns && !SLICED; ++t)
         a_step[t] = p.a_scales[min(m0 + static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows, p.m - 1)];
-    for (int32_t at = wave; at < whole; at += 2 * P * W) {
+    for (int32_t at = begin + wave; at < whole; at += 2 * P * W) {
         load(y, at + P * W);
         multiply(x);
         load(x, at + 2 * P * W);
@@ -566,6 +580,23 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
         }
     }
     __syncthreads();
+    if constexpr (SLICED) {
+#pragma unroll
+        for (int t = 0; t < turns; ++t) {
+            const int r = static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows;
+            if (r < 16 * R && m0 + r < p.m)
+                *reinterpret_cast<i32x4_t*>(slices.sums + (static_cast<int64_t>(slice) * p.m + m0 + r) * slices.pitch + n0 + finish.place) =
+                    finish.template sum_of<W>(sums + r * S::pitch + finish.place, slab);
+        }
+        if constexpr (KIND == kMessage) {
+            if (m0 == 0 && threadIdx.x < 16 * J) {
+                int32_t s = 0;
+                for (int w = 0; w < W; ++w) s += ones_of[w * 16 * J + threadIdx.x];
+                slices.sums[(static_cast<int64_t>(slices.count) * p.m + slice) * slices.pitch + n0 + threadIdx.x] = s;
+            }
+        }
+        return;
+    }
     if constexpr (KIND == kMessage) finish.take_ones(ones_of, W, 16 * J);
     finish.settle_scales();
 #pragma unroll
@@ -578,16 +609,53 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
     }
 }
 
-template <int DT, int R, int J, int W>
-hipError_t launch_split_as(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+// The slices' sums joined: a lane takes four columns of a row.
+template <int KIND, int DT>
+__global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs p, Slices slices) {
+    const uint32_t fours = (static_cast<uint32_t>(p.n) + 3) / 4, i = blockIdx.x * 256 + threadIdx.x;
+    const int32_t m = static_cast<int32_t>(i / fours), n = static_cast<int32_t>(i % fours) * 4;
+    if (m >= p.m) return;
+    using F = Finish<KIND, DT, 256, false>;
+    F finish(p, n, 0);
+    finish.ask_scales(n + 4 <= p.n);
+    const float a_scale = p.a_scales[m];
+    const f32x4_t there = p.add ? finish.template added<false, true>(m) : f32x4_t{0, 0, 0, 0};
+    i32x4_t sum = {0, 0, 0, 0}, ones = {0, 0, 0, 0};
+    for (int32_t s = 0; s < slices.count; ++s) {
+        sum += *reinterpret_cast<const i32x4_t*>(slices.sums + (static_cast<int64_t>(s) * p.m + m) * slices.pitch + n);
+        if constexpr (KIND == kMessage)
+            ones += *reinterpret_cast<const i32x4_t*>(slices.sums + (static_cast<int64_t>(slices.count) * p.m + s) * slices.pitch + n);
+    }
+    if constexpr (KIND == kMessage) finish.take_ones(reinterpret_cast<const int32_t*>(&ones), 1, 0);
+    finish.settle_scales();
+    finish.template finish<false>(m, F::step_of_a(a_scale), there, sum, sum);
+}
+
+template <int KIND, int DT, int R, int J, int W>
+hipError_t launch_split_kind(const ProductArgs& p, const Slices& slices, hipStream_t stream) {
     const uint32_t tm = (static_cast<uint32_t>(p.m) + 16 * R - 1) / (16 * R), tn = (static_cast<uint32_t>(p.n) + 16 * J - 1) / (16 * J);
-    const dim3 grid(tm * tn), block(64 * W);
+    if constexpr (KIND == kPlain || KIND == kMessage) {
+        if (slices.count > 1) {
+            ProfileSpan span;
+            const hipError_t err = launch_kernel(product_split_kernel<KIND, DT, R, J, W, true>, dim3(tm * tn, static_cast<unsigned>(slices.count)),
+                                                 dim3(64 * W), stream, p, tn, slices);
+            span.last();
+            if (err != hipSuccess) return err;
+            const uint32_t fours = static_cast<uint32_t>(p.m) * ((static_cast<uint32_t>(p.n) + 3) / 4);
+            return launch_kernel(product_join_kernel<KIND, DT>, dim3((fours + 255) / 256), dim3(256), stream, p, slices);
+        }
+    }
+    return launch_kernel(product_split_kernel<KIND, DT, R, J, W, false>, dim3(tm * tn), dim3(64 * W), stream, p, tn, slices);
+}
+
+template <int DT, int R, int J, int W>
+hipError_t launch_split_as(ProductKind kind, const ProductArgs& p, const Slices& slices, hipStream_t stream) {
     switch (kind) {
-    case kPlain:      return launch_kernel(product_split_kernel<kPlain, DT, R, J, W>, grid, block, stream, p, tn);
-    case kMessage:    return launch_kernel(product_split_kernel<kMessage, DT, R, J, W>, grid, block, stream, p, tn);
-    case kActivation: return launch_kernel(product_split_kernel<kActivation, DT, R, J, W>, grid, block, stream, p, tn);
+    case kPlain:      return launch_split_kind<kPlain, DT, R, J, W>(p, slices, stream);
+    case kMessage:    return launch_split_kind<kMessage, DT, R, J, W>(p, slices, stream);
+    case kActivation: return launch_split_kind<kActivation, DT, R, J, W>(p, slices, stream);
     default:
-        if constexpr (J % 2 == 0) return launch_kernel(product_split_kernel<kGated, DT, R, J, W>, grid, block, stream, p, tn);
+        if constexpr (J % 2 == 0) return launch_split_kind<kGated, DT, R, J, W>(p, slices, stream);
         else return hipErrorInvalidValue;                       // the gate's columns come in pairs of sixteen
     }
 }
@@ -638,19 +706,19 @@ hipError_t launch_tiles128_dt(int cols, ProductKind kind, const ProductArgs& p, 
 enum SplitTile { kSplit64 = 0, kSplit64x32, kSplit32, kSplit16, kSplit16x32 };
 
 template <int DT>
-hipError_t launch_split_dt(SplitTile tile, ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+hipError_t launch_split_dt(SplitTile tile, ProductKind kind, const ProductArgs& p, const Slices& slices, hipStream_t stream) {
     switch (tile) {
-    case kSplit64: return launch_split_as<DT, 4, 4, 8>(kind, p, stream);
-    case kSplit64x32: return launch_split_as<DT, 4, 2, 8>(kind, p, stream);
-    case kSplit32: return launch_split_as<DT, 2, 2, 8>(kind, p, stream);
-    case kSplit16: return launch_split_as<DT, 1, 1, 8>(kind, p, stream);
-    default:       return launch_split_as<DT, 1, 2, 8>(kind, p, stream);
+    case kSplit64: return launch_split_as<DT, 4, 4, 8>(kind, p, slices, stream);
+    case kSplit64x32: return launch_split_as<DT, 4, 2, 8>(kind, p, slices, stream);
+    case kSplit32: return launch_split_as<DT, 2, 2, 8>(kind, p, slices, stream);
+    case kSplit16: return launch_split_as<DT, 1, 1, 8>(kind, p, slices, stream);
+    default:       return launch_split_as<DT, 1, 2, 8>(kind, p, slices, stream);
     }
 }
 
 #define AQSGD_PRODUCT_DT(EXTERN, DT)                                                                                        \
     EXTERN template hipError_t launch_tiles256_dt<DT>(ProductKind, const TilePlan&, const ProductArgs&, hipStream_t);      \
     EXTERN template hipError_t launch_tiles128_dt<DT>(int, ProductKind, const ProductArgs&, hipStream_t);                  \
-    EXTERN template hipError_t launch_split_dt<DT>(SplitTile, ProductKind, const ProductArgs&, hipStream_t);
+    EXTERN template hipError_t launch_split_dt<DT>(SplitTile, ProductKind, const ProductArgs&, const Slices&, hipStream_t);
 
 }  // namespace aqsgd

@@ -24,30 +24,45 @@ template <int DT> struct Tiles128 {
     static hipError_t go(int cols, ProductKind k, const ProductArgs& p, hipStream_t s) { return launch_tiles128_dt<DT>(cols, k, p, s); }
 };
 template <int DT> struct Split {
-    static hipError_t go(SplitTile t, ProductKind k, const ProductArgs& p, hipStream_t s) { return launch_split_dt<DT>(t, k, p, s); }
+    static hipError_t go(SplitTile t, ProductKind k, const ProductArgs& p, const Slices& l, hipStream_t s) { return launch_split_dt<DT>(t, k, p, l, s); }
 };
 
 uint32_t tiles(int64_t n, int64_t side) { return static_cast<uint32_t>((n + side - 1) / side); }
 
-// What a call takes on an idle MI355X, in microseconds, for each kernel: a tile alone, and what every 256 tiles beyond
-// the first few add, both straight lines in k (thousands).  Fitted to 160 products with m, n up to 16384 and k from 16
-// to 16384, drawn evenly over their logarithms, each timed with every kernel in a captured graph: the mean distance is
-// 7 to 10 %, and the kernel that the lines pick is 2 % slower on average than the best one.  Sides measured (us):
+// What a call takes on an idle MI355X, in microseconds, for each kernel: a tile alone, and what every 256 tiles add, a
+// part of it only with every full round of the CUs; both straight lines in k (thousands).  Fitted to 550 products with
+// m, n up to 16384 and k from 16 to 16384, drawn evenly over their logarithms, and 98 whose sides are powers of two or
+// the widths of models, each timed with every kernel in a captured graph: the mean distance is 7 to 12 %, and the
+// kernel that the lines pick is 1 % slower on average than the best one (30 % at worst).  Sides measured (us):
 // 1 x 6400 x 1600 4.9 with 16 x 16, 6.6 with 64 x 64, 12.7 with 128 x 128; 512 x 512 x 4096 10.4 with 32 x 32, 17.9
-// with 16 x 16 and with 64 x 64; 777 x 1001 x 1333 8.2 with 64 x 64, 9.8 with 32 x 32, 13.8 with 128 x 128; 4349 x 449 x
-// 688 7.8 with 128 x 64, 10.2 with 128 x 128, 14.1 with 32 x 32; 1024 x 4096 x 1024 11.6 with 128 x 128, 18.5 with 256 x
+// with 16 x 16 and with 64 x 64; 4349 x 449 x 688 7.8 with 128 x 64, 10.2 with 128 x 128, 14.1 with 32 x 32; one of those
+// that the lines miss: 777 x 1001 x 1333 10.0 with 128 x 64, which they take, 8.3 with 64 x 64; 1024 x 4096 x 1024 11.6 with 128 x 128, 18.5 with 256 x
 // 256, 27 with 64 x 64; 7373 x 7896 x 383 55.8 with 128 x 128, 77.9 with 128 x 64, whose rows of results are half as
 // long, so it is left out from 1024 tiles on.
-struct Line { int rows, cols; float alone, alone_k, more, more_k, first; };
+struct Line { int rows, cols; float alone, alone_k, more, more_k, rounds; };
 constexpr Line kSplitLines[] = {            // by SplitTile
-    {64, 64, 4.06f, 2.16f, 2.56f, 3.44f, 0.32f}, {64, 32, 3.65f, 1.54f, 1.69f, 2.55f, 0.48f}, {32, 32, 3.41f, 1.13f, 0.77f, 1.48f, 0.62f},
-    {16, 16, 3.46f, 0.61f, 0.72f, 0.59f, 0.57f}, {16, 32, 3.47f, 0.87f, 0.77f, 0.92f, 0.71f}};
-constexpr Line kTile128Line = {128, 128, 4.81f, 4.44f, 2.74f, 3.67f, 0.16f}, kTile128x64Line = {128, 64, 4.08f, 2.61f, 0.92f, 2.43f, 0.0f};
+    {64, 64, 4.17f, 2.47f, 2.71f, 3.32f, 0.67f}, {64, 32, 3.57f, 1.62f, 1.63f, 2.51f, 0.62f}, {32, 32, 3.31f, 1.10f, 0.60f, 1.54f, 0.59f},
+    {16, 16, 3.40f, 0.49f, 0.57f, 0.73f, 0.59f}, {16, 32, 3.33f, 0.87f, 0.54f, 1.12f, 0.55f}};
+constexpr Line kTile128Line = {128, 128, 5.81f, 4.29f, 2.54f, 3.67f, 0.72f}, kTile128x64Line = {128, 64, 4.11f, 3.16f, 0.92f, 1.19f, 0.12f};
 
-float cost(const Line& l, const ProductArgs& p) {
-    const float k = 0.001f * static_cast<float>(p.k);
-    const float many = static_cast<float>(tiles(p.m, l.rows)) * static_cast<float>(tiles(p.n, l.cols)) * (1.0f / 256) - l.first;
-    return l.alone + l.alone_k * k + (many > 0.0f ? many * (l.more + l.more_k * k) : 0.0f);
+float cost(const Line& l, const ProductShape& p, int slices = 1) {
+    const float k = 0.001f * static_cast<float>(p.k) / static_cast<float>(slices);
+    const int64_t all = static_cast<int64_t>(tiles(p.m, l.rows)) * tiles(p.n, l.cols) * slices;
+    const float many = l.rounds * static_cast<float>((all - 1) >> 8) + (1.0f - l.rounds) * static_cast<float>(all) * (1.0f / 256);
+    return l.alone + l.alone_k * k + many * (l.more + l.more_k * k);
+}
+
+// Slices of k, where tiles are few and k is long: a second launch, and the sums once out and once in again, at a
+// microsecond a megabyte (16 x 256 x 16384 8.3 us, in one piece 16.3; 204 x 340 x 10592 15.4 and 21.5; with more sums it
+// soon costs more than it gives: 512 x 512 x 8192 24.2 and 17.8).
+float join_cost(const ProductShape& p, int slices) {
+    return 3.0f + static_cast<float>(slices) * static_cast<float>(p.m) * static_cast<float>(p.n) * 8e-6f;
+}
+
+// Where one tile spans all columns, every row of a comes from memory, and a tile of 128 rows has less of it on its way
+// than its steps need: 14696 x 56 x 10448 52.8 us with 64 x 64, 71.9 with 128 x 64; 8794 x 64 x 8106 27.5 and 43.5.
+float streams(const ProductShape& p, int cols) {
+    return p.n <= cols && static_cast<int64_t>(p.m) * p.k > (int64_t{32} << 20) ? 1.6f : 1.0f;
 }
 
 // Tiles of 256 rows, one workgroup to a CU.  A tile of w columns takes 8 us and (0.45 + 0.0043 w) us for every 128
@@ -74,7 +89,7 @@ float makespan(uint32_t wide, uint32_t narrow, float t_wide, float t_narrow) {
     return end;
 }
 
-TilePlan plan256(ProductKind kind, const ProductArgs& p, float& best) {
+TilePlan plan256(ProductKind kind, const ProductShape& p, float& best) {
     const float steps = static_cast<float>(tiles(p.k, 128)), t_wide = tile256_time(8, steps);
     TilePlan plan{tiles(p.m, 256), tiles(p.n, 256), 0, 0};
     best = 2.0f + makespan(plan.tiles_m * plan.wide_n, 0, t_wide, t_wide);
@@ -96,7 +111,67 @@ TilePlan plan256(ProductKind kind, const ProductArgs& p, float& best) {
     return plan;
 }
 
+// How a product goes: in slices of k or whole by tiles of the waves' registers, by tiles of 128 rows, or of 256.
+struct Choice {
+    int split = -1, slices = 1, cols = 128;
+    bool large = false;
+    TilePlan plan = {};
+};
+
+Choice choose(ProductKind kind, const ProductShape& p) {
+    Choice c;
+    float best = cost(kTile128Line, p) * streams(p, 128);
+    if (static_cast<int64_t>(tiles(p.m, 128)) * tiles(p.n, 64) <= 1024) {
+        const float now = cost(kTile128x64Line, p) * streams(p, 64);
+        if (now < best) { best = now; c.cols = 64; }
+    }
+    const bool may_slice = (kind == kPlain || kind == kMessage) && p.k >= 4096 && static_cast<int64_t>(p.m) * p.n <= 1 << 20;
+    for (int t = kSplit64; t <= kSplit16x32; ++t) {
+        if (kind == kGated && t == kSplit16) continue;            // the gate's columns come in pairs of sixteen
+        float now = cost(kSplitLines[t], p);
+        if (now < best) { best = now; c.split = t; c.slices = 1; }
+        for (int slices = 2; may_slice && slices <= 16 && p.k >= 2048 * slices; slices *= 2) {
+            now = cost(kSplitLines[t], p, slices) + join_cost(p, slices);
+            if (now < 0.9f * best) { best = now; c.split = t; c.slices = slices; }
+        }
+    }
+    if (c.split >= 0) return c;
+    float large;
+    c.plan = plan256(kind, p, large);
+    c.large = large < best;
+    return c;
+}
+
+// The slices' sums in the workspace: rows of whole tiles.
+Slices slices_of(const Choice& c, const ProductShape& p) {
+    Slices s = {nullptr, 1, 0, 0};
+    if (c.split < 0 || c.slices == 1) return s;
+    const int32_t pieces = static_cast<int32_t>(tiles(p.k, 128));
+    s.pieces = (pieces + c.slices - 1) / c.slices;
+    s.count = (pieces + s.pieces - 1) / s.pieces;
+    const int cols = kSplitLines[c.split].cols;
+    s.pitch = static_cast<int32_t>(tiles(p.n, cols)) * cols;
+    return s;
+}
+
 }  // namespace
 
-hipError_t launch_product(ProductKind kind, const ProductArgs& p, hipStream_t stream) {
+int64_t product_workspace_bytes(ProductKind kind, const ProductShape& p) {
+    if (p.m == 0 || p.n == 0 || p.k < 4096) return 0;
+    const Slices s = slices_of(choose(kind, p), p);
+    return s.count > 1 ? static_cast<int64_t>(s.count) * (p.m + 1) * s.pitch * 4 : 0;
+}
 
+hipError_t launch_product(ProductKind kind, const ProductArgs& p, void* workspace, hipStream_t stream) {
+    const ProductShape shape{p.m, p.n, p.k};
+    const Choice c = choose(kind, shape);
+    if (c.split >= 0) {
+        Slices s = slices_of(c, shape);
+        s.sums = static_cast<int32_t*>(workspace);
+        return by_dtype<Split>(p.dtype, static_cast<SplitTile>(c.split), kind, p, s, stream);
+    }
+    if (c.large) return by_dtype<Tiles256>(p.dtype, kind, c.plan, p, stream);
+    return by_dtype<Tiles128>(p.dtype, c.cols, kind, p, stream);
+}
+
+}  // namespace aqsgd

@@ -122,7 +122,9 @@ struct ProductArgs {
     int32_t dtype, act;
 };
 
-hipError_t launch_product(ProductKind kind, const ProductArgs& p, hipStream_t stream);
+struct ProductShape { int32_t m, n, k; };
+int64_t product_workspace_bytes(ProductKind kind, const ProductShape& p);
+hipError_t launch_product(ProductKind kind, const ProductArgs& p, void* workspace, hipStream_t stream);
 
 // ---- the quantiser's -------------------------------------------------------------------------
 struct Quant8Args {

@@ -84,8 +84,9 @@ int aqsgd_quant8(const aqsgd_quant8_desc* d, const void* x, int8_t* row_codes, f
 }
 
 size_t aqsgd_matmul8_workspace_bytes(const aqsgd_matmul8_desc* d) {
-    (void)d;
-    return 0;
+    if (check_matmul8(d) != AQSGD_OK) return 0;
+    const ProductShape p{static_cast<int32_t>(d->m), static_cast<int32_t>(d->n), static_cast<int32_t>(d->k)};
+    return static_cast<size_t>(product_workspace_bytes(d->message ? kMessage : kPlain, p));
 }
 
 int aqsgd_matmul8(const aqsgd_matmul8_desc* d, const void* a_codes, const float* a_scales, const int8_t* b_codes,
@@ -110,7 +111,7 @@ int aqsgd_matmul8(const aqsgd_matmul8_desc* d, const void* a_codes, const float*
     p.ldb = code_stride(d->k);
     p.m = static_cast<int32_t>(d->m); p.n = static_cast<int32_t>(d->n); p.k = static_cast<int32_t>(d->k);
     p.dtype = d->dtype;
-    return status(launch_product(d->message ? kMessage : kPlain, p, static_cast<hipStream_t>(stream)));
+    return status(launch_product(d->message ? kMessage : kPlain, p, workspace, static_cast<hipStream_t>(stream)));
 }
 
 int aqsgd_ffn8(const aqsgd_ffn8_desc* d, const int8_t* a_codes, const float* a_scales, const int8_t* w_codes,
@@ -130,7 +131,7 @@ int aqsgd_ffn8(const aqsgd_ffn8_desc* d, const int8_t* a_codes, const float* a_s
     p.lda = p.ldb = code_stride(d->k);
     p.m = static_cast<int32_t>(d->m); p.n = static_cast<int32_t>(d->f * (d->gated ? 2 : 1)); p.k = static_cast<int32_t>(d->k);
     p.dtype = d->dtype; p.act = d->act;
-    return status(launch_product(d->gated ? kGated : kActivation, p, static_cast<hipStream_t>(stream)));
+    return status(launch_product(d->gated ? kGated : kActivation, p, nullptr, static_cast<hipStream_t>(stream)));
 }
 
 int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* d, const void* dh, const void* pre, void* dpre, void* stream) {
