@@ -326,7 +326,8 @@ int aqsgd_grad_topk_dequant(const aqsgd_desc* desc, int32_t keep, const uint8_t*
  * workspace_bytes is less than asked for.
  */
 typedef struct {
-    int64_t rows, cols;   /* of x; 0 rows or columns: nothing happens                  */
+    int64_t rows, cols;   /* of x; 0 rows: the columns are empty, scales and sums 0;   */
+                          /* 0 columns: the rows are, scales 0 (no codes, no workspace) */
     int64_t ld;           /* elements between the rows of x, at least cols             */
     int32_t dtype;        /* aqsgd_dtype of x                                          */
     int32_t rounding;     /* aqsgd_round                                               */

@@ -591,15 +591,22 @@ def _here(what: str, t, dtype, shape) -> ctypes.c_void_p | None:
     return p
 
 
+def _check_stream(stream) -> None:
+    if stream is None:
+        return
+    here = torch.cuda.current_device()
+    if getattr(stream, "device_index", here) != here:
+        raise ValueError(f"the stream is of cuda:{stream.device_index}, the call is made on cuda:{here}")
+
+
 def _workspace(need: int, workspace, like, stream):
-    """``need`` bytes of device memory: the caller's, or some of the allocator's, which may go to
-    others only after the call's work on ``stream``."""
+    """``need`` bytes of device memory: the caller's, or some of the allocator's, taken and given back in the
+    order of ``stream``'s work."""
     if need == 0:
         return None, 0
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        with torch.cuda.stream(stream):
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
     else:
         _want(workspace, "workspace", torch.uint8, need, exact=False)
         _here("workspace", workspace, torch.uint8, workspace.shape)
@@ -616,12 +623,13 @@ def quant8(desc: Quant8Desc, x, *, row_codes=None, row_scales=None, col_codes=No
         return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
     rows, cols = desc.rows, desc.cols
     if x.dtype != _TORCH_OF_CODE[desc.dtype]:
         raise ValueError(f"x must be {_TORCH_OF_CODE[desc.dtype]}, got {x.dtype}")
     if tuple(x.shape) != (rows, cols):
         raise ValueError(f"x must be of shape {(rows, cols)}, got {tuple(x.shape)}")
-    if not x.is_cuda or (cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) != desc.ld):
+    if not x.is_cuda or (cols > 1 and x.stride(1) != 1) or (rows > 1 and cols > 0 and x.stride(0) != desc.ld):
         raise ValueError(f"x must be a device tensor whose rows are contiguous and {desc.ld} elements apart")
     if x.device.index != torch.cuda.current_device():
         raise ValueError(f"x is on {x.device}, the call is made on cuda:{torch.cuda.current_device()}")
@@ -644,6 +652,7 @@ def matmul8(desc: Matmul8Desc, a_codes, a_scales, b_codes, b_scales, out, *, bia
         return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
     td, m, n, k = _TORCH_OF_CODE[desc.dtype], desc.m, desc.n, desc.k
     if desc.message:
         _want(a_codes, "a_codes", torch.uint8, m * k, exact=False)
@@ -668,6 +677,7 @@ def ffn8(desc: Ffn8Desc, a_codes, a_scales, w_codes, w_scales, h, *, bias=None, 
         return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
     td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f
     w, stride = f * (2 if desc.gated else 1), quant8_stride(desc.k)
     _raise(lib().aqsgd_ffn8(
@@ -684,6 +694,7 @@ def ffn8_grad(desc: Ffn8Desc, dh, pre, dpre, *, stream=None) -> None:
         return _raise(rc) if rc else None
     if desc.dtype not in _TORCH_OF_CODE:
         raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
     td, m, f = _TORCH_OF_CODE[desc.dtype], desc.m, desc.f
     w = f * (2 if desc.gated else 1)
     _raise(lib().aqsgd_ffn8_grad(ctypes.byref(desc), _here("dh", dh, td, (m, f)), _here("pre", pre, td, (m, w)),

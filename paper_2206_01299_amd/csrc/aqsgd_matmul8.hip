@@ -111,6 +111,8 @@ TilePlan plan256(ProductKind kind, const ProductShape& p, float& best) {
     return plan;
 }
 
+constexpr int64_t kMostSplitTiles = (int64_t{1} << 23) - 1;       // of 512 lanes: a grid takes fewer than 2^32
+
 // How a product goes: in slices of k or whole by tiles of the waves' registers, by tiles of 128 rows, or of 256.
 struct Choice {
     int split = -1, slices = 1, cols = 128;
@@ -128,6 +130,7 @@ Choice choose(ProductKind kind, const ProductShape& p) {
     const bool may_slice = (kind == kPlain || kind == kMessage) && p.k >= 4096 && static_cast<int64_t>(p.m) * p.n <= 1 << 20;
     for (int t = kSplit64; t <= kSplit16x32; ++t) {
         if (kind == kGated && t == kSplit16) continue;            // the gate's columns come in pairs of sixteen
+        if (static_cast<int64_t>(tiles(p.m, kSplitLines[t].rows)) * tiles(p.n, kSplitLines[t].cols) > kMostSplitTiles) continue;
         float now = cost(kSplitLines[t], p);
         if (now < best) { best = now; c.split = t; c.slices = 1; }
         for (int slices = 2; may_slice && slices <= 16 && p.k >= 2048 * slices; slices *= 2) {

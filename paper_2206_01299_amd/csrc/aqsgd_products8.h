@@ -141,6 +141,7 @@ struct Quant8Args {
 };
 
 int64_t quant8_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_quant8_empty(float* scales, float* sums, int64_t count, hipStream_t stream);
 hipError_t launch_quant8(int dtype, int rounding, const Quant8Args& a, hipStream_t stream);
 
 struct Ffn8GradArgs {

@@ -62,7 +62,13 @@ int aqsgd_quant8(const aqsgd_quant8_desc* d, const void* x, int8_t* row_codes, f
                  float* col_scales, float* col_sums, void* workspace, size_t workspace_bytes, void* stream) {
     const int rc = check_quant8(d);
     if (rc != AQSGD_OK) return rc;
-    if (d->rows == 0 || d->cols == 0) return AQSGD_OK;
+    if (d->rows == 0 || d->cols == 0) {              // the other side's vectors are empty
+        float* scales = d->rows ? row_scales : col_scales;
+        float* sums = d->rows ? nullptr : col_sums;
+        if (!aligned(scales, 4) || !aligned(sums, 4)) return AQSGD_ERR_ALIGN;
+        if (d->rows + d->cols == 0 || (!scales && !sums)) return AQSGD_OK;
+        return status(launch_quant8_empty(scales, sums, d->rows + d->cols, static_cast<hipStream_t>(stream)));
+    }
     if (!x || !row_codes != !row_scales || !col_codes != !col_scales) return AQSGD_ERR_NULL;
     if (!aligned(x, elem_bytes(d->dtype)) || !aligned(row_codes, 16) || !aligned(row_scales, 4) || !aligned(col_codes, 16) ||
         !aligned(col_scales, 4) || !aligned(col_sums, 4))

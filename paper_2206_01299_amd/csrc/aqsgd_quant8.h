@@ -260,7 +260,8 @@ inline ColumnPlan column_plan(int64_t rows, int64_t cols) {
     p.tile_rows = tiles < 512 ? 64 : 128;
     p.band_tiles = tiles < 2048 ? 1 : tiles < 8192 ? tiles / 1024 : 8;
     p.bands = (rows + p.tile_rows * p.band_tiles - 1) / (p.tile_rows * p.band_tiles);
-    const int64_t most = p.spans < 4 ? 128 / p.spans : 32;
+    constexpr int64_t kMost = (int64_t{1} << 23) - 1;                  // workgroups of 512 lanes: a grid takes fewer than 2^32
+    const int64_t most = p.spans < 4 ? 128 / p.spans : p.spans > kMost / 32 ? kMost / p.spans : 32;
     const int64_t want = (rows + 31) / 32 < most ? (rows + 31) / 32 : most;
     p.block_rows = (rows + want - 1) / want;
     p.blocks = (rows + p.block_rows - 1) / p.block_rows;

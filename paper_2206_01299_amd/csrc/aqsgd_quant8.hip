@@ -16,6 +16,19 @@ int64_t quant8_workspace_bytes(int64_t rows, int64_t cols) {
     return (2 * p.blocks * cols + p.spans * rows) * 4;
 }
 
+// Vectors of no elements: scale 0 and sum 0, so that a product over no tokens is 0.
+static __global__ __launch_bounds__(256) void quant8_empty_kernel(float* scales, float* sums, int64_t count) {
+    for (int64_t i = blockIdx.x * int64_t{256} + threadIdx.x; i < count; i += int64_t{256} * gridDim.x) {
+        if (scales) scales[i] = 0.0f;
+        if (sums) sums[i] = 0.0f;
+    }
+}
+
+hipError_t launch_quant8_empty(float* scales, float* sums, int64_t count, hipStream_t stream) {
+    const int64_t blocks = (count + 255) / 256;
+    return launch_kernel(quant8_empty_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(256), stream, scales, sums, count);
+}
+
 hipError_t launch_quant8(int dtype, int rounding, const Quant8Args& a, hipStream_t stream) {
     const bool draw = rounding == AQSGD_ROUND_STOCHASTIC;
     switch (dtype) {

@@ -353,6 +353,12 @@ struct Call8 {
     void* stream(PyObject* o) {
         if (!ok) return nullptr;
         if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
+        if (PyObject* index = PyObject_GetAttrString(o, "device_index")) {           // a stream of torch's: of this device
+            ok = PyLong_Check(index) && PyLong_AsLong(index) == device;
+            Py_DECREF(index);
+        }
+        PyErr_Clear();
+        if (!ok) return nullptr;
         PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
         if (!h) { PyErr_Clear(); ok = false; return nullptr; }
         void* s = PyLong_Check(h) ? PyLong_AsVoidPtr(h) : nullptr;
@@ -367,7 +373,7 @@ AQSGD_ENTRY(py_quant8, 9, {
     const auto f32 = c10::ScalarType::Float; const auto i8 = c10::ScalarType::Char;
     const at::Tensor* x = c.on_device(p[1], c.type);
     c.ok = x && x->dim() == 2 && x->size(0) == c.d.rows && x->size(1) == c.d.cols && (c.d.cols <= 1 || x->stride(1) == 1) &&
-           (c.d.rows <= 1 || x->stride(0) == c.d.ld);
+           (c.d.rows <= 1 || c.d.cols == 0 || x->stride(0) == c.d.ld);
     if (!c.ok) Py_RETURN_NONE;
     const void* at = x->data_ptr();
     const int64_t across = static_cast<int64_t>(g_api.quant8_stride(c.d.cols)); const int64_t down = static_cast<int64_t>(g_api.quant8_stride(c.d.rows));

@@ -1,5 +1,7 @@
 """The 8-bit operators on the GPU against their plain forms in 64 bits: codes and scales exactly, products
 and activations within the roundings that their binary32 steps make."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -501,3 +503,201 @@ def test_two_graphs_that_share_a_workspace():
         for _, x, cc, cs in graphs:
             codes, scales = R.quantise(x.cpu().numpy().T)
             assert np.array_equal(cc.cpu().numpy(), codes) and np.array_equal(cs.cpu().numpy(), scales)
+
+
+def test_two_graphs_that_share_the_workspace_of_sliced_sums():
+    """Long sums of few tiles go in slices through a workspace; replayed in turn, with eager calls between."""
+    ws, graphs = None, []
+    rng = np.random.default_rng(8)
+    for m, n, k, message in ((16, 256, 16384, False), (5, 70, 20000, True)):
+        d = B.make_matmul8_desc(m=m, n=n, k=k, dtype="f32", message=message)
+        need = B.matmul8_workspace_bytes(d)
+        assert need > 0
+        if ws is None or ws.numel() < need:
+            ws = torch.empty(4 * need, dtype=torch.uint8, device="cuda")
+        ops = [torch.from_numpy(v).cuda() for v in operands(rng, m, n, k, message)]
+        out = torch.empty((m, n), device="cuda")
+        B.matmul8(d, *ops, out, workspace=ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.matmul8(d, *ops, out, workspace=ws)
+        graphs.append((d, g, ops, out))
+    for turn in range(4):
+        for _, g, ops, out in graphs:
+            ops[0].copy_(ops[0].flip(0) if turn % 2 else ops[0].roll(1, 0))
+            out.fill_(float("nan"))
+            g.replay()
+        torch.cuda.synchronize()
+        for d, _, ops, out in graphs:
+            again = torch.empty_like(out)
+            B.matmul8(d, *ops, again)
+            off = 127.5 if d.message else 0.0
+            k = d.k
+            want = ((ops[0][:, :k].double() - off) @ ops[2][:, :k].double().t())
+            want = want * (ops[1].double() / (127.5 if d.message else 127.0))[:, None] * (ops[3].double() / 127.0)[None, :]
+            assert torch.equal(out, again)
+            # the sum's rounding, two steps' and two products'
+            assert ((out.double() - want).abs() <= 6 * R.U * want.abs()).all()
+
+
+def test_workspaces_come_in_the_order_of_the_calls_stream():
+    """What the binding allocates for a call on another stream is no memory that the current stream may still use."""
+    side, need = torch.cuda.Stream(), 5 << 20
+    torch.cuda.synchronize()
+    mine = torch.empty(need, dtype=torch.uint8, device="cuda")
+    at = mine.data_ptr()
+    like = torch.empty(1, device="cuda")
+    del mine
+    given, _ = B._workspace(need, None, like, side)
+    assert given.value != at
+    again, _ = B._workspace(need, None, like, None)
+    assert again.value == at
+    x = torch.randn(300, 200, device="cuda")
+    d = B.make_quant8_desc(rows=300, cols=200, dtype="f32")
+    cc, cs = torch.empty((200, R.stride(300)), dtype=torch.int8, device="cuda"), torch.empty(200, device="cuda")
+    torch.cuda.synchronize()
+    B.quant8(d, x, col_codes=cc, col_scales=cs, stream=side)
+    torch.cuda.synchronize()
+    codes, scales = R.quantise(x.cpu().numpy().T)
+    assert np.array_equal(cc.cpu().numpy(), codes) and np.array_equal(cs.cpu().numpy(), scales)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_tokens(dtype):
+    """A micro-batch without a token: its columns' scales and sums are 0, and it adds nothing to a weight's gradient."""
+    td = B.DTYPE_NAME[dtype]
+    codes, scales, sums = {}, {}, {}
+    for name, cols in (("x", 70), ("dy", 1300)):
+        d = B.make_quant8_desc(rows=0, cols=cols, dtype=dtype)
+        sc, su = (Framed((cols,), torch.float32) for _ in range(2))
+        sc.t.fill_(float("nan")); su.t.fill_(float("nan"))
+        codes[name] = torch.empty((cols, 0), dtype=torch.int8, device="cuda")
+        B.quant8(d, torch.empty((0, cols), dtype=td, device="cuda"), row_codes=torch.empty((0, R.stride(cols)), dtype=torch.int8, device="cuda"),
+                 row_scales=torch.empty(0, device="cuda"), col_codes=codes[name], col_scales=sc.t, col_sums=su.t)
+        torch.cuda.synchronize()
+        sc.check(name); su.check(name)
+        assert (sc.t == 0).all() and (su.t == 0).all()
+        scales[name] = sc.t
+    grad = torch.randn(1300, 70, device="cuda")
+    before = grad.clone()
+    B.matmul8(B.make_matmul8_desc(m=1300, n=70, k=0, dtype="f32"), codes["dy"], scales["dy"], codes["x"], scales["x"], grad, add=grad)
+    assert torch.equal(grad, before)
+    rs = torch.full((5,), float("nan"), device="cuda")
+    B.quant8(B.make_quant8_desc(rows=5, cols=0, dtype=dtype), torch.empty((5, 0), dtype=td, device="cuda"),
+             row_codes=torch.empty((5, 0), dtype=torch.int8, device="cuda"), row_scales=rs)
+    assert (rs == 0).all()
+
+
+def test_the_native_path_gives_what_the_ctypes_one_does(monkeypatch):
+    """The same bits by both ways of the binding, with and without a workspace, on the current and on a named stream."""
+    m, k, f = 70, 128, 96
+    inputs = stage_inputs(m, k, f, "f16")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    first = [stage_step(*inputs, "f16"), stage_step(*inputs, "f16", stream=side)]
+    torch.cuda.synchronize()
+    monkeypatch.setattr(B, "_native", B._Ctypes())
+    second = [stage_step(*inputs, "f16"), stage_step(*inputs, "f16", stream=side)]
+    torch.cuda.synchronize()
+    for n, want in first[0].items():
+        for got in (first[1], *second):
+            assert torch.equal(got[n], want), n
+
+
+def test_calls_of_two_threads_at_once():
+    """Each thread its own stream and results; the library keeps nothing between them."""
+    want = {}
+    jobs = [(96, 64, 80), (130, 160, 112)]
+    inputs = [stage_inputs(*j, "bf16", seed=i) for i, j in enumerate(jobs)]
+    want = [{n: t.clone() for n, t in stage_step(*x, "bf16").items()} for x in inputs]
+    torch.cuda.synchronize()
+    got, errors = [[], []], []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(8):
+                    got[i].append(stage_step(*inputs[i], "bf16"))
+            stream.synchronize()
+        except Exception as e:                                              # told to the test's own thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for i in range(2):
+        for r in got[i]:
+            for n, t in want[i].items():
+                assert torch.equal(r[n], t), n
+
+
+def test_the_time_of_a_call_of_two_launches():
+    """aqsgd_profile_next_launch around calls that take one launch and two."""
+    x = torch.randn(4096, 1600, device="cuda")
+    d = B.make_quant8_desc(rows=4096, cols=1600, dtype="f32")
+    cc, cs = torch.empty((1600, 4096), dtype=torch.int8, device="cuda"), torch.empty(1600, device="cuda")
+    dm = B.make_matmul8_desc(m=16, n=256, k=16384, dtype="f32")
+    ops = [torch.from_numpy(v).cuda() for v in operands(np.random.default_rng(0), 16, 256, 16384)]
+    out = torch.empty((16, 256), device="cuda")
+    for call in (lambda: B.quant8(d, x, col_codes=cc, col_scales=cs), lambda: B.matmul8(dm, *ops, out)):
+        call()
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record(); stop.record()                                       # makes the events
+        torch.cuda.synchronize()
+        B.profile_next_launch(start, stop)
+        call()
+        torch.cuda.synchronize()
+        assert 0.001 < start.elapsed_time(stop) < 5.0
+
+
+# ---- the largest -------------------------------------------------------------------------------
+
+def test_matmul8_of_more_rows_than_a_grid_of_small_tiles_counts():
+    """2^29 tokens: codes and results whose offsets pass 32 bits, and more tiles of the small kernels than a grid takes."""
+    m, n, k = (1 << 29) + 65, 16, 16
+    if torch.cuda.mem_get_info()[0] < (120 << 30):
+        pytest.skip("needs 80 GB")
+    torch.manual_seed(0)
+    b = torch.randint(-127, 128, (n, 64), dtype=torch.int8, device="cuda")
+    b[:, k:] = 0
+    sb = torch.rand(n, device="cuda") + 0.5
+    a = torch.zeros((m, 64), dtype=torch.int8, device="cuda")
+    period = torch.randint(-127, 128, (999983, k), dtype=torch.int8, device="cuda")
+    for at in range(0, m, 999983):
+        a[at:at + 999983, :k] = period[:min(999983, m - at)]
+    sa = torch.rand(999983, device="cuda").repeat(m // 999983 + 1)[:m].contiguous()
+    out = torch.empty((m, n), device="cuda")
+    B.matmul8(B.make_matmul8_desc(m=m, n=n, k=k, dtype="f32"), a, sa, b, sb, out)
+    torch.cuda.synchronize()
+    # sums below 2^24 are exact in binary32, and the steps follow one by one (on the host: divided, not multiplied
+    # with a reciprocal)
+    want = (period.float().cpu() @ b[:, :k].float().cpu().t()) * (sa[:999983].cpu() / torch.tensor([127.0]))[:, None]
+    want = (want * (sb.cpu() / torch.tensor([127.0]))[None, :]).cuda()
+    for at in range(0, m, 999983):
+        assert torch.equal(out[at:at + 999983], want[:min(999983, m - at)]), at
+    del a, sa, out
+    torch.cuda.empty_cache()
+
+
+def test_quant8_sums_of_the_most_columns():
+    """2^30 columns of 33 rows: more workgroups of a block of rows each than a grid takes."""
+    rows, cols = 33, 1 << 30
+    if torch.cuda.mem_get_info()[0] < (130 << 30):
+        pytest.skip("needs 90 GB")
+    line = ((torch.arange(1 << 24, device="cuda") % 61).half() - 30) / 8
+    x = torch.empty((rows, cols), dtype=torch.float16, device="cuda")
+    for r in range(rows):
+        x[r].view(64, 1 << 24)[:] = line * (1 + r % 2)
+    sums = torch.full((cols,), float("nan"), device="cuda")
+    B.quant8(B.make_quant8_desc(rows=rows, cols=cols, dtype="f16"), x, col_sums=sums)
+    torch.cuda.synchronize()
+    want = line.float() * 49                                                # 17 rows once, 16 twice: exact
+    for part in sums.view(64, 1 << 24):
+        assert torch.equal(part, want)
+    del x, sums
+    torch.cuda.empty_cache()

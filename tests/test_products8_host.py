@@ -2,6 +2,7 @@
 forms that the GPU tests compare with."""
 import ctypes
 from pathlib import Path
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -153,6 +154,39 @@ def test_the_binding_checks_tensors_against_the_descriptor(monkeypatch):
             B.quant8(q, x, row_codes=good["a"], row_scales=good["sa"])
     with pytest.raises(KeyError):
         B.make_ffn8_desc(m=4, f=6, k=70, dtype="bf16", act="relu")
+
+
+def test_vectors_of_no_elements_are_refused_where_their_scales_miss_their_alignment():
+    for rows, cols, name in ((0, 40, "cs"), (0, 40, "sums"), (16, 0, "rs")):
+        d = B.make_quant8_desc(rows=rows, cols=cols, dtype="f16")
+        assert q8(d, **{name: ctypes.c_void_p(4098)}) == -6 and B.quant8_workspace_bytes(d) == 0
+    assert q8(B.make_quant8_desc(rows=0, cols=0, dtype="f16")) == 0
+
+
+def test_long_sums_of_few_tiles_need_a_workspace():
+    d = B.make_matmul8_desc(m=16, n=256, k=16384, dtype="f16")
+    need = B.matmul8_workspace_bytes(d)
+    assert need >= 2 * 16 * 256 * 4
+    assert m8(d, ws=NULL) == -9 and m8(d, n=need - 1) == -9 and m8(d, ws=ctypes.c_void_p(4104)) == -6
+    assert B.matmul8_workspace_bytes(B.make_matmul8_desc(m=16, n=256, k=16384, dtype="f16", message=True)) >= need
+    for m, n, k in ((0, 256, 16384), (16, 0, 16384), (4096, 4096, 16384), (16, 256, 1024), (16, 256, 0)):
+        assert B.matmul8_workspace_bytes(B.make_matmul8_desc(m=m, n=n, k=k, dtype="f16")) == 0
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    away = SimpleNamespace(cuda_stream=0, device_index=1)
+    z = torch.zeros
+    codes, one = z(4, 64, dtype=torch.int8), z(4)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        B.quant8(B.make_quant8_desc(rows=4, cols=64, dtype="f32"), z(4, 64), row_codes=codes, row_scales=one, stream=away)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        B.matmul8(B.make_matmul8_desc(m=4, n=4, k=64, dtype="f32"), codes, one, codes, one, z(4, 4), stream=away)
+    d = B.make_ffn8_desc(m=4, f=4, k=64, dtype="f32", gated=False)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        B.ffn8(d, codes, one, codes, one, z(4, 4), stream=away)
+    with pytest.raises(ValueError, match="the stream is of cuda:1"):
+        B.ffn8_grad(d, z(4, 4), z(4, 4), z(4, 4), stream=away)
 
 
 def test_the_plain_quantiser_by_hand():
