@@ -18,9 +18,10 @@
  *
  * General rules for every entry point
  *   - Every data pointer is DEVICE memory on the current HIP device, owned by the
- *     caller before, during and after the call.  The codec calls allocate no device
- *     memory, keep no state between calls and may be made from several host threads
- *     at once.  Descriptors and job lists are HOST memory and are read before the
+ *     caller before, during and after the call.  The calls allocate no device
+ *     memory (a workspace, where one is needed, is the caller's), keep no state
+ *     between calls and may be made from several host threads at once, each with
+ *     workspaces of its own.  Descriptors and job lists are HOST memory and are read before the
  *     call returns.  Three things are stateful, and say so where they are declared:
  *     the launch-shape knobs (process-wide atomics, aqsgd_set_launch_shape), the
  *     request to time the next launch (per host thread, aqsgd_profile_next_launch)
@@ -44,8 +45,8 @@
  *     check is checked before any work is enqueued; on error nothing is enqueued.
  *     NOT checked: sample ids outside [0, n_samples) (out-of-bounds accesses),
  *     duplicate ids within one call (two rows of the call race on one row of
- *     m_buf: undefined results, all accesses in bounds), non-finite inputs
- *     (undefined results), buffers smaller than the descriptor says.
+ *     m_buf: undefined results, all accesses in bounds), non-finite inputs of the
+ *     codec (undefined results), buffers smaller than the descriptor says.
  *     aqsgd_check_ids() checks the first two on the device.  AQSGD_ERR_LAUNCH
  *     reports the status of the call's own launches (or that host memory ran out,
  *     before any): where a message or a job list takes several, those before the
