@@ -21,10 +21,13 @@ __device__ __forceinline__ uint32_t row_from(int32_t n0, int32_t c, int32_t n) {
 // What is left of the sums once they lie in LDS as rows of 32-bit integers: a lane takes four columns of every few
 // rows, so that its scales and bias are read once and a row leaves in whole lines.  COLS virtual columns from n0 on.
 //
-// STREAM: a large product's results go past the caches, in which they would take the room of the rows of a and b that
-// other tiles still need: 4096 x 12800 x 1600 gated, with what the backward pass needs, 125.4 us with ordinary stores,
-// 106.6 so; 16384 x 16384 x 4096 float32 998 and 927.  Small ones wait for memory then: 48 x 304 x 368 4.0 and 4.3.
-template <int KIND, int DT, int COLS, bool STREAM>
+// STREAM: the results of large tiles go past the caches, in which they would take the room of the rows of a and b that
+// other tiles still need, if rows of results are whole sectors of 32 bytes, so that no two waves share one: with ordinary
+// stores and so, 4096 x 12800 x 1600 float16 gated, with what the backward pass needs, 124 us and 103; 8192 x 8192 x 2048
+// float32 159 and 135, with 8200 columns 184 and 158; 2048 x 2048 x 1024 11.9 and 10.7; where sectors are shared, 5000 x
+// 5001 x 512 bfloat16 27.7 and 33.5, 4096 x 6401 x 1600 float16 49.9 and 56.  Results of small tiles would
+// only wait for memory then: 48 x 304 x 368 4.0 and 4.3.
+template <int KIND, int DT, int COLS>
 struct Finish {
     static constexpr int wide = (KIND == kGated ? COLS / 2 : COLS) / 4;       // lanes to a row
     static constexpr int step_rows = kWave / wide;                            // rows a wave takes at a time
@@ -132,7 +135,7 @@ struct Finish {
         }
         return v;
     }
-    template <bool FULL>
+    template <bool FULL, bool STREAM>
     __device__ __forceinline__ void put(void* base, int64_t at, const f32x4_t& v) const {
         if (FULL || left >= 4) {
             store4<DT, STREAM>(base, at, v);
@@ -170,14 +173,14 @@ struct Finish {
         return s;
     }
     // FULL: the row and the four columns exist.
-    template <bool FULL, int PARTS = 1>
+    template <bool FULL, int PARTS, bool STREAM>
     __device__ __forceinline__ void row(int32_t m, float a_step, const f32x4_t& there, const int32_t* sums, int pitch = 0) const {
         if (!FULL && (m >= p.m || left <= 0)) return;
         i32x4_t u = {0, 0, 0, 0};
         if constexpr (KIND == kGated) u = sum_of<PARTS>(sums + place + 16, pitch);
-        finish<FULL>(m, a_step, there, sum_of<PARTS>(sums + place, pitch), u);
+        finish<FULL, STREAM>(m, a_step, there, sum_of<PARTS>(sums + place, pitch), u);
     }
-    template <bool FULL>
+    template <bool FULL, bool STREAM>
     __device__ __forceinline__ void finish(int32_t m, float a_step, const f32x4_t& there, const i32x4_t& sum, const i32x4_t& sum_u) const {
         f32x4_t v = scaled(sum, a_step, step, bias);
         if constexpr (KIND == kGated) {
@@ -185,21 +188,21 @@ struct Finish {
             f32x4_t h;
 #pragma unroll
             for (int e = 0; e < 4; ++e) h[e] = activation(p.act, v[e]) * u[e];
-            put<FULL>(p.out, static_cast<int64_t>(m) * half + n, h);
+            put<FULL, STREAM>(p.out, static_cast<int64_t>(m) * half + n, h);
             if (p.pre) {
-                put<FULL>(p.pre, static_cast<int64_t>(m) * p.n + n, v);
-                put<FULL>(p.pre, static_cast<int64_t>(m) * p.n + half + n, u);
+                put<FULL, STREAM>(p.pre, static_cast<int64_t>(m) * p.n + n, v);
+                put<FULL, STREAM>(p.pre, static_cast<int64_t>(m) * p.n + half + n, u);
             }
         } else {
             const int64_t at = static_cast<int64_t>(m) * p.n + n;
             if constexpr (KIND == kActivation) {
-                if (p.pre) put<FULL>(p.pre, at, v);
+                if (p.pre) put<FULL, STREAM>(p.pre, at, v);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = activation(p.act, v[e]);
             } else {
                 v += there;
             }
-            put<FULL>(p.out, at, v);
+            put<FULL, STREAM>(p.out, at, v);
         }
     }
 };
@@ -294,7 +297,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
         bring(0, 0);
         bring(min(1, steps - 1), 1);
     }
-    if (t < S::bm) a_steps[t] = Finish<KIND, DT, 16 * TN, true>::step_of_a(a_scale);
+    if (t < S::bm) a_steps[t] = Finish<KIND, DT, 16 * TN>::step_of_a(a_scale);
     if (t < S::bn) {
         b_steps[t] = b_scale / kCodeHalf;
         b_bias[t] = b_add;
@@ -379,7 +382,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
     }
     barrier_but_last<0>();                               // the last fragments have been read, the last loads are in
 
-    using F = Finish<KIND, DT, TN * 16, true>;
+    using F = Finish<KIND, DT, TN * 16>;
     F finish(p, n0 + wn, lane);
     finish.take_scales(b_steps + wn, b_bias + wn);
     if constexpr (KIND == kMessage) finish.take_ones(b_ones + wn, WM, S::bn);
@@ -390,8 +393,8 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
     const bool full = m0 + wm + 16 * TM <= p.m && n0 + wn + 16 * TN <= (KIND == kGated ? p.n & ~31 : p.n);     // h is whole sixteens there
     const int mine = lane / F::wide;
     const bool busy = F::step_rows * F::wide == kWave || mine < F::step_rows;
-    const auto store = [&](auto adds) {
-        constexpr bool ADD = decltype(adds)::value;
+    const auto store = [&](auto adds, auto streams) {
+        constexpr bool ADD = decltype(adds)::value, STREAM = decltype(streams)::value;
 #pragma unroll
         for (int i0 = 0; i0 < TM; i0 += kStoreBlocks) {
 #pragma unroll
@@ -410,21 +413,42 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, int32_t m0, i
 #pragma unroll
                         for (int u = 0; u < ahead; ++u) {
                             const int r = (t + u) * F::step_rows;
-                            finish.template row<true>(first + r, a_step[r], there[u], own + (mine + r) * S::pitch);
+                            finish.template row<true, 1, STREAM>(first + r, a_step[r], there[u], own + (mine + r) * S::pitch);
                         }
                     }
                 }
             } else {
+                // several rows' sums at a time (12072 x 944 x 136 13.5 us, one at a time 13.7; the gated product is 2 % slower so)
+                constexpr int most = KIND == kGated ? 1 : 4, few = ahead < most ? ahead : most;
 #pragma unroll 1
-                for (int r = 0; r < rows; r += F::step_rows) {
-                    if (!busy || mine + r >= rows) continue;
-                    finish.template row<false>(first + r, a_step[r], finish.template added<false, ADD>(first + r), own + (mine + r) * S::pitch);
+                for (int t = 0; t < turns; t += few) {
+                    f32x4_t there[few];
+                    i32x4_t sum[few], sum_u[few] = {};
+                    float step[few];
+#pragma unroll
+                    for (int u = 0; u < few; ++u) {
+                        const int r = (t + u) * F::step_rows, at = min(r, rows - 1 - mine);
+                        there[u] = finish.template added<false, ADD>(first + r);
+                        sum[u] = *reinterpret_cast<const i32x4_t*>(own + (mine + at) * S::pitch + finish.place);
+                        if constexpr (KIND == kGated) sum_u[u] = *reinterpret_cast<const i32x4_t*>(own + (mine + at) * S::pitch + finish.place + 16);
+                        step[u] = a_step[at];
+                    }
+#pragma unroll
+                    for (int u = 0; u < few; ++u) {
+                        const int r = (t + u) * F::step_rows;
+                        if (busy && mine + r < rows && first + r < p.m && finish.left > 0) finish.template finish<false, STREAM>(first + r, step[u], there[u], sum[u], sum_u[u]);
+                    }
                 }
             }
         }
     };
-    if ((KIND == kPlain || KIND == kMessage) && p.add) store(std::true_type());
-    else store(std::false_type());
+    if ((KIND == kPlain || KIND == kMessage) && p.add) {
+        if (p.stream) store(std::true_type(), std::true_type());
+        else store(std::true_type(), std::false_type());
+    } else {
+        if (p.stream) store(std::false_type(), std::true_type());
+        else store(std::false_type(), std::false_type());
+    }
 }
 
 // Tile t of a grid of tiles: they go down in bands of kBand tile rows, so that the tiles an XCD works on at a time
@@ -550,7 +574,7 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
     Frags x, y;
     load(x, begin + wave);
     // what the end needs is asked for now
-    using F = Finish<KIND, DT, 16 * J, false>;
+    using F = Finish<KIND, DT, 16 * J>;
     constexpr int lanes_rows = kWave * W / F::wide, turns = (16 * R + lanes_rows - 1) / lanes_rows;
     F finish(p, n0, lane);
     if (!SLICED) finish.ask_scales(n0 + 16 * J <= (KIND == kGated ? p.n & ~31 : p.n));         // h is whole sixteens there
@@ -604,7 +628,7 @@ __global__ __launch_bounds__(64 * W, (SplitShape<KIND, R, J>::waves)) void produ
         const int r = static_cast<int>(threadIdx.x) / F::wide + t * lanes_rows;
         if (r >= 16 * R) continue;
         const bool adds = (KIND == kPlain || KIND == kMessage) && p.add;
-        finish.template row<false, W>(m0 + r, F::step_of_a(a_step[t]), adds ? finish.template added<false, true>(m0 + r) : f32x4_t{0, 0, 0, 0},
+        finish.template row<false, W, false>(m0 + r, F::step_of_a(a_step[t]), adds ? finish.template added<false, true>(m0 + r) : f32x4_t{0, 0, 0, 0},
                                       sums + r * S::pitch, slab);
     }
 }
@@ -615,7 +639,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs p, 
     const uint32_t fours = (static_cast<uint32_t>(p.n) + 3) / 4, i = blockIdx.x * 256 + threadIdx.x;
     const int32_t m = static_cast<int32_t>(i / fours), n = static_cast<int32_t>(i % fours) * 4;
     if (m >= p.m) return;
-    using F = Finish<KIND, DT, 256, false>;
+    using F = Finish<KIND, DT, 256>;
     F finish(p, n, 0);
     finish.ask_scales(n + 4 <= p.n);
     const float a_scale = p.a_scales[m];
@@ -628,7 +652,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductArgs p, 
     }
     if constexpr (KIND == kMessage) finish.take_ones(reinterpret_cast<const int32_t*>(&ones), 1, 0);
     finish.settle_scales();
-    finish.template finish<false>(m, F::step_of_a(a_scale), there, sum, sum);
+    finish.template finish<false, false>(m, F::step_of_a(a_scale), there, sum, sum);
 }
 
 template <int KIND, int DT, int R, int J, int W>

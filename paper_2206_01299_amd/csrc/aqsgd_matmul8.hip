@@ -145,6 +145,11 @@ Choice choose(ProductKind kind, const ProductShape& p) {
     return c;
 }
 
+bool whole_sectors(ProductKind kind, const ProductArgs& p) {
+    const int64_t width = static_cast<int64_t>(kind == kGated ? p.n / 2 : p.n) * (p.dtype == AQSGD_F32 ? 4 : 2);
+    return width % 32 == 0 && ((reinterpret_cast<uintptr_t>(p.out) | reinterpret_cast<uintptr_t>(p.pre)) & 31) == 0;
+}
+
 // The slices' sums in the workspace: rows of whole tiles.
 Slices slices_of(const Choice& c, const ProductShape& p) {
     Slices s = {nullptr, 1, 0, 0};
@@ -165,7 +170,9 @@ int64_t product_workspace_bytes(ProductKind kind, const ProductShape& p) {
     return s.count > 1 ? static_cast<int64_t>(s.count) * (p.m + 1) * s.pitch * 4 : 0;
 }
 
-hipError_t launch_product(ProductKind kind, const ProductArgs& p, void* workspace, hipStream_t stream) {
+hipError_t launch_product(ProductKind kind, const ProductArgs& q, void* workspace, hipStream_t stream) {
+    ProductArgs p = q;
+    p.stream = whole_sectors(kind, q);
     const ProductShape shape{p.m, p.n, p.k};
     const Choice c = choose(kind, shape);
     if (c.split >= 0) {

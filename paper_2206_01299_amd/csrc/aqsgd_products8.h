@@ -120,6 +120,7 @@ struct ProductArgs {
     int64_t lda, ldb;          // bytes
     int32_t m, n, k;           // n: rows of b
     int32_t dtype, act;
+    bool stream;               // rows of results are whole sectors of memory
 };
 
 struct ProductShape { int32_t m, n, k; };
