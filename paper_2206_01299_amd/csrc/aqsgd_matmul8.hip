@@ -32,18 +32,17 @@ uint32_t tiles(int64_t n, int64_t side) { return static_cast<uint32_t>((n + side
 // What a call takes on an idle MI355X, in microseconds, for each kernel: a tile alone, and what every 256 tiles add, a
 // part of it only with every full round of the CUs; both straight lines in k (thousands).  Fitted to 550 products with
 // m, n up to 16384 and k from 16 to 16384, drawn evenly over their logarithms, and 98 whose sides are powers of two or
-// the widths of models, each timed with every kernel in a captured graph: the mean distance is 7 to 12 %, and the
+// the widths of models, each timed with every kernel in a captured graph: the mean distance is 7 to 10 %, and the
 // kernel that the lines pick is 1 % slower on average than the best one (30 % at worst).  Sides measured (us):
-// 1 x 6400 x 1600 4.9 with 16 x 16, 6.6 with 64 x 64, 12.7 with 128 x 128; 512 x 512 x 4096 10.4 with 32 x 32, 17.9
-// with 16 x 16 and with 64 x 64; 4349 x 449 x 688 7.8 with 128 x 64, 10.2 with 128 x 128, 14.1 with 32 x 32; one of those
-// that the lines miss: 777 x 1001 x 1333 10.0 with 128 x 64, which they take, 8.3 with 64 x 64; 1024 x 4096 x 1024 11.6 with 128 x 128, 18.5 with 256 x
-// 256, 27 with 64 x 64; 7373 x 7896 x 383 55.8 with 128 x 128, 77.9 with 128 x 64, whose rows of results are half as
-// long, so it is left out from 1024 tiles on.
+// 512 x 512 x 4096 10.7 with 32 x 32, 17.9 with 16 x 16, 18.5 with 64 x 64; 1024 x 4096 x 1024 9.2 with 128 x 64, 10.7 with
+// 128 x 128, 16.7 with 256 x 256, 27.0 with 64 x 64; 7373 x 7896 x 383 54.0 with 128 x 128, 77.9 with 128 x 64, whose rows
+// of results are half as long, so it is left out from 1024 tiles on; one that the lines miss: 777 x 1001 x 1333 9.5 with
+// 128 x 64, which they take, 8.3 with 64 x 64.
 struct Line { int rows, cols; float alone, alone_k, more, more_k, rounds; };
 constexpr Line kSplitLines[] = {            // by SplitTile
-    {64, 64, 4.17f, 2.47f, 2.71f, 3.32f, 0.67f}, {64, 32, 3.57f, 1.62f, 1.63f, 2.51f, 0.62f}, {32, 32, 3.31f, 1.10f, 0.60f, 1.54f, 0.59f},
-    {16, 16, 3.40f, 0.49f, 0.57f, 0.73f, 0.59f}, {16, 32, 3.33f, 0.87f, 0.54f, 1.12f, 0.55f}};
-constexpr Line kTile128Line = {128, 128, 5.81f, 4.29f, 2.54f, 3.67f, 0.72f}, kTile128x64Line = {128, 64, 4.11f, 3.16f, 0.92f, 1.19f, 0.12f};
+    {64, 64, 4.16f, 2.47f, 2.68f, 3.32f, 0.66f}, {64, 32, 3.56f, 1.61f, 1.62f, 2.54f, 0.61f}, {32, 32, 3.29f, 1.09f, 0.60f, 1.55f, 0.58f},
+    {16, 16, 3.38f, 0.49f, 0.56f, 0.73f, 0.59f}, {16, 32, 3.33f, 0.86f, 0.54f, 1.13f, 0.56f}};
+constexpr Line kTile128Line = {128, 128, 5.54f, 4.29f, 2.38f, 3.82f, 0.68f}, kTile128x64Line = {128, 64, 3.84f, 3.16f, 0.96f, 1.30f, 0.25f};
 
 float cost(const Line& l, const ProductShape& p, int slices = 1) {
     const float k = 0.001f * static_cast<float>(p.k) / static_cast<float>(slices);
