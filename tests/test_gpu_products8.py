@@ -20,7 +20,7 @@ MARK = 77                               # what memory holds that a call must lea
 @pytest.fixture(scope="module", autouse=True)
 def _library():
     if not torch.cuda.is_available():
-        pytest.fail("these tests need the MI355X; run them with -m gpu on the GPU box")
+        pytest.fail("these tests need an MI355X")
     B.lib()
 
 
@@ -653,6 +653,145 @@ def test_the_time_of_a_call_of_two_launches():
         call()
         torch.cuda.synchronize()
         assert 0.001 < start.elapsed_time(stop) < 5.0
+
+
+# ---- every kernel ------------------------------------------------------------------------------
+# Sizes at which the choice takes each of the kernels of larger products, small ones as far as that goes: rows of results
+# that are whole sectors of 32 bytes and others, columns and rows that end inside a tile, k that ends in either half of
+# a step.  The 64-bit products are the device's own here; sums of codes are whole numbers, exact in them.
+
+TILES = [(97, 4129, 1808), (161, 2816, 1264), (33, 4160, 224), (4125, 33, 160), (65, 5195, 176), (65, 5312, 176), (1803, 4369, 160),
+         (1539, 5088, 144), (2327, 5615, 160), (2309, 5664, 224), (3093, 4901, 1008), (5447, 2848, 896), (3597, 5637, 240),
+         (1283, 1632, 9456), (5401, 3979, 240), (5935, 3648, 240), (1281, 5989, 224), (1667, 4704, 208), (1539, 5913, 160), (1569, 5792, 176),
+         (2821, 4095, 144), (2339, 4832, 160)]
+GATED = [(4131, 49, 1856), (161, 1408, 1264), (33, 2077, 160), (33, 2080, 224), (65, 2533, 160), (67, 2560, 160), (1557, 2499, 160),
+         (1797, 2240, 144), (2069, 2693, 176), (2311, 2464, 176), (5385, 1417, 976), (5941, 1312, 992), (4613, 2197, 256), (4651, 2208, 240),
+         (1667, 2337, 192), (1671, 2368, 208)]
+
+
+def device_codes(rows, k, gen):
+    t = torch.zeros((rows, R.stride(k)), dtype=torch.int8, device="cuda")
+    t[:, :k] = torch.randint(-127, 128, (rows, k), generator=gen, device="cuda", dtype=torch.int8)
+    return t, torch.rand(rows, generator=gen, device="cuda") * 0.02 + 0.01
+
+
+def device_projections(a, sa, b, sb, k, message=False):
+    """R.projections on the device."""
+    ai, bi = a[:, :k].double(), b[:, :k].double()
+    steps = (sa.double() / (127.5 if message else 127.0))[:, None] * (sb.double() / 127.0)[None, :]
+    if message:
+        whole, ones = (ai - 128) @ bi.t().contiguous(), bi.sum(dim=1)[None, :]
+        sums = whole + 0.5 * ones
+        off = 5 * sums.abs() + 3 * (whole.abs() + 0.5 * ones.abs())
+    else:
+        sums = ai @ bi.t().contiguous()
+        off = 5 * sums.abs()
+    return sums * steps, off * R.U * steps
+
+
+def device_act(x, kind):
+    if kind == "silu":
+        return x / (1.0 + torch.exp(-x))
+    if kind == "gelu":
+        return 0.5 * x * (1.0 + torch.erf(x / 2 ** 0.5))
+    return 0.5 * x * (1.0 + torch.tanh((2.0 / np.pi) ** 0.5 * (x + 0.044715 * x ** 3)))
+
+
+def device_close(got, want, off, dtype, tag):
+    """R.close on the device."""
+    miss = (got.double() - want).abs() - 1.0001 * (off + R.HALF_STEP[dtype] * (want.abs() + off) + R.TINY[dtype])
+    bad = ~(miss <= 0)
+    assert not bad.any(), f"{tag}: {int(bad.sum())} of {bad.numel()} values too far off, first at {bad.nonzero()[0].tolist()}"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", TILES)
+def test_products_by_every_kernel(dtype, m, n, k):
+    """Plain, added to in place, of a message, and through an activation."""
+    gen = torch.Generator(device="cuda").manual_seed(m * n + k)
+    td, tag = B.DTYPE_NAME[dtype], f"{dtype} {m}x{n}x{k}"
+    a, sa = device_codes(m, k, gen)
+    b, sb = device_codes(n, k, gen)
+    bias = torch.randn(n, generator=gen, device="cuda").to(td)
+    out = Framed((m, n), td, 128)
+    p, off = device_projections(a, sa, b, sb, k)
+    d = B.make_matmul8_desc(m=m, n=n, k=k, dtype=dtype)
+    B.matmul8(d, a, sa, b, sb, out.t, bias=bias)
+    device_close(out.t, p + bias.double(), off + R.U * (p + bias.double()).abs(), dtype, tag)
+    before = torch.randn((m, n), generator=gen, device="cuda").to(td)
+    out.t.copy_(before)
+    B.matmul8(d, a, sa, b, sb, out.t, add=out.t)
+    want = p + before.double()
+    device_close(out.t, want, off + R.U * want.abs(), dtype, tag + " added")
+    act = ACTS[(m + n) % 3]
+    h, pre = Framed((m, n), td, 128), Framed((m, n), td, 160)
+    B.ffn8(B.make_ffn8_desc(m=m, f=n, k=k, dtype=dtype, act=act, gated=False), a, sa, b, sb, h.t, bias=bias, pre=pre.t)
+    y = p + bias.double()
+    yoff = off + R.U * y.abs()
+    device_close(pre.t, y, yoff, dtype, tag + " pre")
+    device_close(h.t, device_act(y, act), R.STEEPEST * yoff + R.VALUE_OFF * y.abs(), dtype, tag + " " + act)
+    levels = torch.randint(0, 256, (m, k), generator=gen, device="cuda", dtype=torch.uint8)
+    p, off = device_projections(levels, sa, b, sb, k, message=True)
+    B.matmul8(B.make_matmul8_desc(m=m, n=n, k=k, dtype=dtype, message=True), levels, sa, b, sb, out.t)
+    device_close(out.t, p, off, dtype, tag + " message")
+    torch.cuda.synchronize()
+    for f in (out, h, pre):
+        f.check(tag)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,f,k", GATED)
+def test_gated_blocks_by_every_kernel(dtype, m, f, k):
+    gen = torch.Generator(device="cuda").manual_seed(m * f + k)
+    td, act, tag = B.DTYPE_NAME[dtype], ACTS[(m + f) % 3], f"{dtype} {m}x{f}x{k}"
+    a, sa = device_codes(m, k, gen)
+    b, sb = device_codes(2 * f, k, gen)
+    bias = torch.randn(2 * f, generator=gen, device="cuda").to(td)
+    h, pre = Framed((m, f), td, 128), Framed((m, 2 * f), td, 128)
+    B.ffn8(B.make_ffn8_desc(m=m, f=f, k=k, dtype=dtype, act=act), a, sa, b, sb, h.t, bias=bias, pre=pre.t)
+    p, off = device_projections(a, sa, b, sb, k)
+    p = p + bias.double()
+    off = off + R.U * p.abs()
+    device_close(pre.t, p, off, dtype, tag + " pre")
+    g, goff = device_act(p[:, :f], act), R.STEEPEST * off[:, :f] + R.VALUE_OFF * p[:, :f].abs()
+    u, uoff = p[:, f:], off[:, f:]
+    device_close(h.t, g * u, g.abs() * uoff + u.abs() * goff + goff * uoff + R.U * (g * u).abs(), dtype, f"{tag} {act}")
+    alone = torch.empty((m, f), dtype=td, device="cuda")
+    B.ffn8(B.make_ffn8_desc(m=m, f=f, k=k, dtype=dtype, act=act), a, sa, b, sb, alone, bias=bias)
+    assert torch.equal(alone, h.t)
+    torch.cuda.synchronize()
+    h.check(tag)
+    pre.check(tag)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n,k", [(863, 33, 19264), (1033, 1, 16704), (515, 1, 16560), (1, 1, 10496), (1, 1035, 16384), (33, 896, 19376),
+                                   (35, 384, 16720)])
+def test_long_sums_in_slices(dtype, m, n, k):
+    assert B.matmul8_workspace_bytes(B.make_matmul8_desc(m=m, n=n, k=k, dtype=dtype)) > 0
+    run_matmul8(m, n, k, dtype, bias=True, add=True, in_place=True)
+    run_matmul8(m, n, k, dtype, message=True, workspace=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(65601, 3), (33001, 131), (262200, 3), (1048700, 1)])
+def test_quant8_of_many_rows(dtype, rows, cols):
+    """Tiles of 128 rows, one, two and eight to a workgroup."""
+    x = activations(np.random.default_rng([rows, cols]), rows, cols)
+    run_quant8(x, dtype)
+    run_quant8(x, dtype, by_rows=False, sums=False, pad=cols % 2)
+    if cols == 3:
+        run_quant8(x, dtype, rounding=1, seed=rows)
+        run_quant8(x, dtype, rounding=1, seed=rows, by_rows=False, sums=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_quant8_draws_of_rows_or_columns_alone(dtype):
+    for cols in (40, 200, 900, 1500, 5001, 12000, 20000):
+        run_quant8(activations(np.random.default_rng(cols), 5, cols), dtype, rounding=1, seed=cols, by_cols=False, sums=False)
+    run_quant8(activations(np.random.default_rng(1), 300, 150), dtype, rounding=1, seed=9, by_rows=False, sums=False)
+    run_quant8(activations(np.random.default_rng(1), 300, 150), dtype, by_rows=False, sums=False)
+    run_quant8(activations(np.random.default_rng(2), 700, 150), dtype, by_rows=True, by_cols=False)
 
 
 # ---- the largest -------------------------------------------------------------------------------
