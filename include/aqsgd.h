@@ -322,7 +322,8 @@ int aqsgd_grad_topk_dequant(const aqsgd_desc* desc, int32_t keep, const uint8_t*
  *   col_sums    out  float[cols], or NULL: sums of the columns of x itself, in binary32 (the
  *               gradient of a bias); the same bits on every call
  *   workspace   aqsgd_quant8_workspace_bytes() bytes of device memory, 16-byte aligned, free
- *               for other use once the call's work has run; NULL where that is 0
+ *               for other use once the call's work has run; NULL where that is 0 or
+ *               rows alone are asked for
  * x and the float arrays need their element's alignment.  AQSGD_ERR_WORKSPACE if
  * workspace_bytes is less than asked for.
  */
