@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void ffn8_grad_kernel(const Ffn8GradArgs a, ui
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             float value, slope;
-            activation_slope(ACT, g[e], value, slope);
+            activation_slope<DT>(ACT, g[e], value, slope);
             g[e] = GATED ? d[e] * u[e] * slope : d[e] * slope;
             u[e] = d[e] * value;
         }

@@ -187,7 +187,7 @@ struct Finish {
             const f32x4_t u = scaled(sum_u, a_step, step_u, bias_u);
             f32x4_t h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = activation(p.act, v[e]) * u[e];
+            for (int e = 0; e < 4; ++e) h[e] = activation<DT>(p.act, v[e]) * u[e];
             put<FULL, STREAM>(p.out, static_cast<int64_t>(m) * half + n, h);
             if (p.pre) {
                 put<FULL, STREAM>(p.pre, static_cast<int64_t>(m) * p.n + n, v);
@@ -198,7 +198,7 @@ struct Finish {
             if constexpr (KIND == kActivation) {
                 if (p.pre) put<FULL, STREAM>(p.pre, at, v);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = activation(p.act, v[e]);
+                for (int e = 0; e < 4; ++e) v[e] = activation<DT>(p.act, v[e]);
             } else {
                 v += there;
             }

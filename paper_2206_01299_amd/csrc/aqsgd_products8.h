@@ -57,31 +57,61 @@ __device__ __forceinline__ void store4(void* base, int64_t idx, const f32x4_t& v
     }
 }
 
+// A whole number as an integer by the instruction itself, which takes a NaN to 0 (a conversion from C++ would leave that
+// open).
+__device__ __forceinline__ int32_t integer_of(float x) {
+    int32_t k;
+    asm("v_cvt_i32_f32 %0, %1" : "=v"(k) : "v"(x));
+    return k;
+}
+
 // ---- activations ---------------------------------------------------------------------------
 constexpr float kSqrtHalf = 0.70710678118654752f;          // 1 / sqrt(2)
 constexpr float kDensity = 0.39894228040143268f;           // 1 / sqrt(2 pi)
 constexpr float kTanhSlope = 1.5957691216057308f;          // 2 sqrt(2 / pi)
 
-// p = 1 / (1 + exp(-x)) and q = 1 - p, both without a difference of nearly equal numbers and without an
-// exponential that overflows.  The hardware's exponential and reciprocal are off by an ulp at most; the rounding
-// of x log2(e) puts e off by |x| half steps more, which e itself outweighs: p and q are off by 4 half steps of 1.
+// exp(x) of an x that is not above 0, a NaN included, for results of type DT.  The hardware's exponential is good to an ulp
+// and ends at 2^-126; x log2(e) rounded in front of it puts the result off by |x| half steps of binary32.  float32 results are to
+// be right to an ulp, subnormal ones too: the exponential takes only the fraction of x log2(e), formed of two parts of log2(e).
+// bfloat16 has 2^-126 and what is below it as well, but |x| half steps of binary32 (88 at most) are nothing next to one of
+// its own: the square of exp(x / 2).  What float16 can hold ends long before either.  ffn8 4096 x 6400 x 1600 gated,
+// float16 with silu, 101.6 us, with the float32 form 106.2; ffn8_grad of that size not gated, bfloat16, 28.7 and 29.9.
+template <int DT>
+__device__ __forceinline__ float exp_below(float x) {
+    if constexpr (DT == AQSGD_F32) {
+        x = x < -150.0f ? -150.0f : x;        // 0 from there on; a NaN stays
+        const float whole = rintf(x * 1.44269502f), part = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269502f, -whole));
+        return ldexpf(__builtin_amdgcn_exp2f(part), integer_of(whole));
+    } else if constexpr (DT == AQSGD_BF16) {
+        const float half = __builtin_amdgcn_exp2f(x * 0.72134752044448170f);
+        return half * half;
+    } else {
+        return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
+    }
+}
+
+// p = 1 / (1 + exp(-x)) and q = 1 - p, both without a difference of nearly equal numbers and without an exponential that
+// overflows: the exponential, a sum, the hardware's reciprocal and a product, 10 half steps of p and q (float32).
+template <int DT>
 __device__ __forceinline__ void sigmoids(float x, float& p, float& q) {
-    const float e = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269504088896341f), r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
+    const float e = exp_below<DT>(-fabsf(x)), r = __builtin_amdgcn_rcpf(1.0f + e), er = e * r;
     p = x >= 0.0f ? r : er;
     q = x >= 0.0f ? er : r;                   // a NaN gives e, r and er NaN
 }
 
-// (1 + tanh(y / 2)) / 2 is the sigmoid of y.
+// (1 + tanh(y / 2)) / 2 is the sigmoid of y; y's own roundings (five half steps) put its tail off by 5 |y| half steps.
 __device__ __forceinline__ float tanh_argument(float x) { return kTanhSlope * (x + 0.044715f * x * x * x); }
 
+template <int DT>
 __device__ __forceinline__ float activation(int act, float x) {
     if (act == AQSGD_ACT_GELU) return 0.5f * x * (1.0f + erff(x * kSqrtHalf));
     float p, q;
-    sigmoids(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
+    sigmoids<DT>(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
     return x * p;
 }
 
 // The activation's value and slope.
+template <int DT>
 __device__ __forceinline__ void activation_slope(int act, float x, float& value, float& slope) {
     if (act == AQSGD_ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(x * kSqrtHalf));
@@ -90,7 +120,7 @@ __device__ __forceinline__ void activation_slope(int act, float x, float& value,
         return;
     }
     float p, q;
-    sigmoids(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
+    sigmoids<DT>(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
     value = x * p;
     if (act == AQSGD_ACT_SILU) {
         slope = p + value * q;

@@ -28,13 +28,11 @@ __device__ __forceinline__ CodeScale code_scale(uint32_t bits) {
 }
 
 // Code of one value.  x * inv is within an ulp of [-127, 127], so a nearest code needs no clamp; where inv is 0 an
-// infinity or a NaN makes the product a NaN, which the conversion takes to 0 (one from C++ would leave that open;
-// the conversion that rounds down by itself does not do so for every NaN).
+// infinity or a NaN makes the product a NaN, which the conversion takes to 0 (the one that rounds down by itself does not
+// do so for every NaN).
 template <int ROUND>
 __device__ __forceinline__ int32_t code_of(float x, float inv, float r) {
-    const float y = floorf(x * inv + r);
-    int32_t k;
-    asm("v_cvt_i32_f32 %0, %1" : "=v"(k) : "v"(y));
+    int32_t k = integer_of(floorf(x * inv + r));
     if constexpr (ROUND == AQSGD_ROUND_STOCHASTIC) k = min(max(k, -127), 127);
     return k;
 }
