@@ -97,3 +97,29 @@ def test_gradients_of_what_is_far_below_zero(dtype, act):
     # a tail below 2^-114, times x at most 80 of it in a slope: all of them are far below 2^-100 |x|
     assert np.isfinite(got).all()
     assert (np.abs(got - want) <= 2.0 ** -100 * np.abs(np.concatenate([v, v])) + R.TINY[dtype]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gelu_is_right_relative_to_its_value(dtype):
+    """The erf form below 0 is x times a tail of the normal distribution.  float32: exp(-x^2 / 2) from an exact square (the
+    exponential 6 half steps, the square's second part 1); t = 1 / (1 + c |x|) (a sum 1, a reciprocal 2), which the tail
+    follows with a factor of 2.4 at most (7 in all); the polynomial (3.1 by its partial sums, 1 its own distance); two products
+    and that with x (3): 21.1.  Subnormal densities are off by steps of 2^-149 (4 with the product), times |x|.  16 bits: the
+    exponent's square, product and constant are rounded, half a step of x^2 / 2 each, once more where it is a square."""
+    rng = np.random.default_rng(6)
+    x = held(np.concatenate([np.linspace(-14.5, 14.5, 40001), rng.uniform(-0.8, -0.7, 500), -(10.0 ** rng.uniform(-8, 0, 500)),
+                             10.0 ** rng.uniform(0, 4, 500), [0.0, -0.0, -5.0, -5.5, -6.0, -13.5, -14.2]]), dtype)
+    v = x.astype(np.float64)
+    below, phi = 0.5 * erfc(-v / np.sqrt(2)), np.exp(-0.5 * v * v) / np.sqrt(2 * np.pi)
+    more = 0.0 if dtype == "f32" else R.U * (1.5 * np.minimum(v * v, 400) + 8)
+    # above 0 it is 1 less a tail, rounded once
+    cdf_off = (23 * R.U + more) * 0.5 * erfc(np.abs(v) / np.sqrt(2)) + np.where(v < 0, 0, R.U) + 4 * LEAST
+    if dtype == "f16":
+        cdf_off = cdf_off + np.where(np.abs(v) > 13, 2.0 ** -125, 0.0)               # the exponential ends there
+    value_off = np.abs(v) * cdf_off + R.U * np.abs(v) * below
+    within(block(x, "gelu", dtype), v * below, value_off, x, dtype, "gelu")
+    slope, value = gradients(x, "gelu", dtype)
+    within(value, v * below, value_off, x, dtype, "gelu's value")
+    # x times a density (exponential 6, second part 1, its factor and two products 3), added
+    bell_off = np.abs(v) * ((12 * R.U + more) * phi + 4 * LEAST + (2.0 ** -125 * (np.abs(v) > 13) if dtype == "f16" else 0))
+    within(slope, below + v * phi, cdf_off + bell_off + R.U * np.abs(below + v * phi), x, dtype, "gelu's slope")
