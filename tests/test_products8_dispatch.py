@@ -9,6 +9,7 @@ from pathlib import Path
 import pytest
 
 import test_gpu_products8 as T
+import test_gpu_products8_columns as C
 import test_gpu_products8_pipeline as L
 
 ROOT = Path(__file__).resolve().parent.parent
@@ -86,6 +87,35 @@ def test_every_product_kernel_is_taken_by_a_size_that_the_gpu_tests_run(client):
              for what, kind, of in (("m", 0, plain), ("m", 1, message), ("f", 0, act), ("f", 1, gated)) for size in of]
     taken = {kernel for launches in client(*calls) for _, _, kernel in launches}
     for name in ("product_tile_kernel", "product_split_kernel", "product_join_kernel"):
+        here = compiled(name)
+        assert len(here) > 1
+        missing = here - taken
+        assert not missing, f"{len(missing)} of {len(here)} without a size: {sorted(missing)[:5]}"
+
+
+ROWS, COLS, SUMS, DRAWS = 1, 2, 4, 8
+
+
+def test_the_wide_matrices_take_whole_tiles_of_128_rows(client):
+    """Several spans of columns, one tile and two to a workgroup."""
+    for (rows, cols), each in zip(C.WIDE, (1, 2)):
+        for which in (ROWS | COLS | SUMS, COLS | SUMS, ROWS | COLS | DRAWS):
+            launches, = client(("q", 0, which, rows, cols, cols))
+            assert len(launches) == 2 and re.match(rf"quant8_tiles_kernel<0, {which >> 3}, {'true' if which & ROWS else 'false'}, 2>", launches[1][2])
+            assert launches[1][0] == -(-cols // 128) * -(-rows // (128 * each)) and cols > 256
+
+
+def test_every_kernel_of_the_quantiser_is_taken_by_a_size_that_the_gpu_tests_run(client):
+    runs = {which: T.SIZES + sizes(T.test_quant8_of_many_rows, "rows,cols") for which in (ROWS | COLS | SUMS, ROWS, COLS)}
+    runs[ROWS | COLS | SUMS] = runs[ROWS | COLS | SUMS] + C.WIDE + C.SUMS
+    runs[COLS | SUMS] = runs[ROWS | SUMS] = runs[SUMS] = C.SUMS
+    runs[ROWS | COLS] = C.WIDE
+    runs[ROWS | COLS | DRAWS] = sizes(T.test_quant8_stochastic, "rows,cols") + C.WIDE
+    runs[COLS | DRAWS] = [(300, 150)] + [s for s in sizes(T.test_quant8_of_many_rows, "rows,cols") if s[1] == 3]
+    runs[ROWS | DRAWS] = [(5, cols) for cols in (40, 200, 900, 1500, 5001, 12000, 20000)]
+    calls = [("q", dtype, which, r, c, c) for dtype in TYPES.values() for which, of in runs.items() for r, c in of]
+    taken = {kernel for launches in client(*calls) for _, _, kernel in launches}
+    for name in ("quant8_rows_kernel", "quant8_short_kernel", "quant8_maxima_kernel", "quant8_tiles_kernel"):
         here = compiled(name)
         assert len(here) > 1
         missing = here - taken
