@@ -65,10 +65,13 @@ float streams(const ProductShape& p, int cols) {
 }
 
 // Tiles of 256 rows, one workgroup to a CU.  A tile of w columns takes 8 us and (0.45 + 0.0043 w) us for every 128
-// of k, with all CUs at work (power bounds them then).  Where whole tiles leave CUs idle in the last round, the last
-// columns go as narrower ones, launched behind the others: 4096 x 6400 x 1600, 400 tiles of 256 columns 54.2 us,
-// 256 of them and 240 of 160 columns 52.5, 192 of 192 columns 50.8; 4096 x 12800 x 1600 gated, 800 tiles 114.9 us,
-// 768 of them and 128 of 64 columns 102.7; 6144 x 1536 x 8192 added to, 144 tiles 110.7 us, 240 of 160 columns 98.0.
+// of k, with all CUs at work.  Where whole tiles leave CUs idle in the last round, the last
+// columns go as narrower ones, launched behind the others.  Measured with operands from memory: a message of 4096 x 1600
+// times 6400, float16, 400 tiles of 256 columns 56.7 us, 256 of them and 240 of 160 columns 53.1, 192 of 192 columns 53.5;
+// 4096 x 12800 x 1600 gated float16, 800 tiles 113.2, 768 of them and 128 of 64 columns 102.2, 64 of 128 columns 106.0;
+// 6144 x 1536 x 8192 float32 added to, 144 tiles 111.5, 240 of 160 columns 98.0, 192 of 192 columns 103.0.  One that the lines
+// miss: tiles of 96 and 160 columns have no whole number of rows to a wave's store and end row by row, which the line
+// does not know; with the last product's sums in the caches already, 160 columns take 79.0 us, 192 columns 75.5.
 constexpr uint32_t kCus = 256;
 float tile256_time(int blocks, float steps) { return 8.0f + steps * (0.45f + 0.0043f * 32.0f * static_cast<float>(blocks)); }
 
