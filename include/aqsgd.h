@@ -392,7 +392,7 @@ int aqsgd_matmul8(const aqsgd_matmul8_desc* desc, const void* a_codes, const flo
  * aqsgd_ffn8_grad, the backward pass to the projections, in binary32 from the stored ones:
  *     dpre[:, :f] = dtype(dh * pre[:, f:] * act'(pre[:, :f])),  dpre[:, f:] = dtype(dh * act(pre[:, :f]))
  * or  dpre = dtype(dh * act'(pre));  from there aqsgd_quant8 and aqsgd_matmul8 lead on.
- *   dh   in [m, f],  pre in [m, w],  dpre out [m, w] (may be pre itself), of desc.dtype; k is ignored
+ *   dh   in [m, f],  pre in [m, w],  dpre out [m, w] (may be pre itself), of desc.dtype; k as above, not read
  * Alignment and limits as for aqsgd_matmul8.  An activation outside the list: AQSGD_ERR_DTYPE.
  */
 typedef enum {
