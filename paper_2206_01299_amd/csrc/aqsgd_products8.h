@@ -124,15 +124,30 @@ __device__ __forceinline__ void normal_tail(float x, float& tail, float& bell) {
     tail = bell * (t * v);
 }
 
-// The normal distribution's function at x.
-__device__ __forceinline__ float normal_below(float x, float tail) { return x < 0.0f ? tail : 1.0f - tail; }
+// The normal distribution's function at x.  float32: 1/2 and a series in odd powers up to |x| = 1 (fitted as the tail, 7e-10;
+// 3.5e-8 with rounded coefficients), where most of what a layer computes lies and the tail's roundings would be seen: the
+// slope's 2-norm error on normal numbers is 4.0e-8 with it, 5.8e-8 without, for 48.7 us of 4096 x 6400 not gated either way.
+template <int DT>
+__device__ __forceinline__ float normal_below(float x, float tail) {
+    const float far = x < 0.0f ? tail : 1.0f - tail;
+    if constexpr (DT == AQSGD_F32) {
+        const float w = x * x;
+        float v = fmaf(w, -7.65400637e-06f, 0.000113485825f);
+        v = fmaf(w, v, -0.00118632941f);
+        v = fmaf(w, v, 0.00997332297f);
+        v = fmaf(w, v, -0.0664903596f);
+        v = fmaf(w, v, 0.398942292f);
+        return fabsf(x) < 1.0f ? fmaf(x, v, 0.5f) : far;
+    }
+    return far;
+}
 
 template <int DT>
 __device__ __forceinline__ float activation(int act, float x) {
     if (act == AQSGD_ACT_GELU) {
         float tail, bell;
         normal_tail<DT>(x, tail, bell);
-        return x * normal_below(x, tail);
+        return x * normal_below<DT>(x, tail);
     }
     float p, q;
     sigmoids<DT>(act == AQSGD_ACT_SILU ? x : tanh_argument(x), p, q);
@@ -145,7 +160,7 @@ __device__ __forceinline__ void activation_slope(int act, float x, float& value,
     if (act == AQSGD_ACT_GELU) {
         float tail, bell;
         normal_tail<DT>(x, tail, bell);
-        const float below = normal_below(x, tail);
+        const float below = normal_below<DT>(x, tail);
         value = x * below;
         slope = below + x * (kDensity * bell);
         return;
