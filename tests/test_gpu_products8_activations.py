@@ -123,3 +123,20 @@ def test_gelu_is_right_relative_to_its_value(dtype):
     # x times a density (exponential 6, second part 1, its factor and two products 3), added
     bell_off = np.abs(v) * ((12 * R.U + more) * phi + 4 * LEAST + (2.0 ** -125 * (np.abs(v) > 13) if dtype == "f16" else 0))
     within(slope, below + v * phi, cdf_off + bell_off + R.U * np.abs(below + v * phi), x, dtype, "gelu's slope")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_activations_of_no_numbers(dtype, act):
+    """A NaN stays one, in the value and in the slope, an infinity is its own value, and what stands beside them is as without
+    them.  Below, an infinity times 0 is a NaN, as in the formulas."""
+    x = held(np.linspace(-8, 8, 67), dtype)
+    x[[5, 20, 40, 66]] = np.nan, np.inf, -np.inf, np.nan
+    ordinary = held(np.linspace(-8, 8, 67), dtype)
+    plain = np.isfinite(x)
+    for values, alone in ((block(x, act, dtype), block(ordinary, act, dtype)),
+                          (gradients(x, act, dtype)[1], gradients(ordinary, act, dtype)[1])):
+        assert np.isnan(values[[5, 40, 66]]).all() and values[20] == np.inf
+        assert np.array_equal(values[plain], alone[plain])
+    slope, alone = gradients(x, act, dtype)[0], gradients(ordinary, act, dtype)[0]
+    assert np.isnan(slope[[5, 66]]).all() and np.array_equal(slope[plain], alone[plain])
