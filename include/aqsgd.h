@@ -416,6 +416,137 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
                     void* stream);
 
 /*
+ * Layer norm: what stands in front of a stage's 8-bit products, over the residual stream.
+ *
+ * For every row of x [rows, cols], s = x, or s = dtype(x + residual):
+ *     mean = RN( sum s / cols ),  d = RN(s - mean),  rstd = RN( 1 / sqrt( sum d^2 / cols + eps ) )
+ *     y    = dtype( RN( RN( RN(d * rstd) * weight ) + bias ) )
+ * with the sums, quotients and the root in binary64, everything else in binary32.  Without a weight
+ * its factor is left out, without a bias its term.
+ *   x           in   [rows, cols], desc.ld elements from one row to the next
+ *   residual    in   [rows, cols] dense, or NULL; added to x in binary32
+ *   weight      in   [cols], or NULL;  bias in [cols], or NULL; of desc.dtype
+ *   sum         out  [rows, cols] dense: s, or NULL; only with a residual (else AQSGD_ERR_NULL)
+ *   y           out  [rows, cols] dense, or NULL
+ *   mean, rstd  out  float[rows], or both NULL: what the backward pass reads
+ *   row_codes   out  int8 [rows, aqsgd_quant8_stride(cols)], row_scales out float[rows]: what aqsgd_quant8
+ *               (nearest) makes of the rows of y, whether y itself is stored or not; both or neither NULL
+ * sum and y may each be x itself (ld == cols) or residual itself, but not the same one of them; no output may
+ * overlap an input or another output otherwise.  A row with an infinity or a NaN in it gives NaN, the others
+ * nothing of it.
+ *
+ * aqsgd_layernorm_grad, the backward pass.  With x the normalised s (of the call above: sum, where
+ * there was a residual), xh = (x - mean) * rstd and g = dy * weight, in binary32:
+ *     dx      = dtype( rstd * (g - sum g / cols - xh * sum (g * xh) / cols)  (+ add) )
+ *     dweight = sum over the rows of dy * xh,  dbias = sum over the rows of dy
+ * desc.accumulate: dweight and dbias are added to what is there (earlier micro-batches').  Sums are formed
+ * in an order that the sizes alone fix: every call gives the same bits.
+ *   dy          in   [rows, cols] dense;  x in, as above;  mean, rstd in float[rows]
+ *   weight      in   [cols], or NULL for 1;  add in [rows, cols] dense, or NULL: the gradient that arrives along
+ *               the residual stream
+ *   dx          out  [rows, cols] dense; may be dy or add itself, and must not overlap an input otherwise
+ *   dweight     out  float[cols], or NULL;  dbias out float[cols], or NULL
+ *   workspace   aqsgd_layernorm_grad_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use
+ *               once the call's work has run; not read where neither dweight nor dbias is asked for
+ * 0 rows: dweight and dbias are 0, or stay as they are with accumulate; nothing else is written.  codes are
+ * 16-byte aligned, the rest needs its element's alignment.  AQSGD_ERR_SHAPE: no columns, an eps that is negative or
+ * not finite; AQSGD_ERR_WORKSPACE as for aqsgd_quant8.
+ */
+typedef struct {
+    int64_t rows, cols;   /* of x; cols at least 1                                     */
+    int64_t ld;           /* elements between the rows of x, at least cols             */
+    int32_t dtype;        /* aqsgd_dtype of x, residual, weight, bias, sum, y, dy, add, dx */
+    int32_t accumulate;   /* 0 or 1; aqsgd_layernorm does not read it                  */
+    double eps;           /* aqsgd_layernorm_grad does not read it                     */
+} aqsgd_layernorm_desc;
+
+int aqsgd_layernorm(const aqsgd_layernorm_desc* desc, const void* x, const void* residual, const void* weight,
+                    const void* bias, void* sum, void* y, float* mean, float* rstd, int8_t* row_codes,
+                    float* row_scales, void* stream);
+size_t aqsgd_layernorm_grad_workspace_bytes(const aqsgd_layernorm_desc* desc);
+int aqsgd_layernorm_grad(const aqsgd_layernorm_desc* desc, const void* dy, const void* x, const float* mean,
+                         const float* rstd, const void* weight, const void* add, void* dx, float* dweight,
+                         float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * AdamW: one step of many tensors at once, with the moments in 32 or in 8 bits.
+ *
+ * For every element of every tensor, with t the step, one rounding to binary32 per written operation; the
+ * constants in quotes are computed in binary64 and rounded once:
+ *     g = grad  (or  RN(grad * scale))
+ *     m = RN( RN("beta1" * m) + RN("1 - beta1" * g) )
+ *     v = RN( RN("beta2" * v) + RN(RN("1 - beta2" * g) * g) ),  r = RN(sqrt(v))
+ *     w = RN( RN("1 - lr * weight_decay" * w)
+ *             - RN( "lr / (1 - beta1^t)" * RN( m / RN( RN("1 / sqrt(1 - beta2^t)" * r) + "eps" ) ) ) )
+ * w is the binary32 master copy where there is one (param <- dtype(w)), else param itself.
+ *
+ * A tensor's state is one buffer of aqsgd_adamw_state_bytes() bytes, 16-byte aligned, all zero before the first
+ * step; its parts follow each other, each rounded up to whole 64 bytes (n elements, G = ceil(n / 256) groups):
+ *     state_bits 32   float m[n];  float v[n]
+ *     state_bits 8    int8 m codes[n];  uint8 r codes[n];  float m scales[G];  float r scales[G]
+ * In 8 bits the moments are held as codes with a scale for each group of 256 consecutive elements (the last may be
+ * shorter); the second one by its root r.  With s the group's max-abs and T = 127 (m, whose codes carry the sign) or
+ * 255 (r), a code k stands for RN(k^2 * RN(s / T^2)), v being RN(r * r): squares, because the steps' sizes shall
+ * follow the values'.  A new value x is held as
+ *     u = RN(|x| * RN(T^2 / s)),  k the largest whole number with k^2 <= u,
+ *     one more where u - k^2 >= RN(z * (2 k + 1));   z = 1/2 (the nearer neighbour, ties upwards), or
+ *     a draw in (0, 1] (stochastic: the value's expectation is u's),
+ * at most T; of r, what is not 0 gets at least 1.  s < 2^-100: scale 0, codes 0.  A group with an infinity or a NaN
+ * in it: scale NaN, codes 0, so it stays NaN.  This step's w is computed from m and r before they are so rounded.
+ * Draws: Philox4x32-10 with key rng_seed + t and counter (j / 4 as 64 bits, 0, 0), word j % 4, where j numbers the
+ * elements of all the call's tensors, each rounded up to whole groups, one behind the other in the list's order; m's z
+ * is ((word & 0xffff) + 1) / 65536, r's ((word >> 16) + 1) / 65536.
+ *
+ *   tensors  HOST memory, n_tensors of them, read before the call returns.  param [n] of desc.dtype; grad [n] of
+ *            desc.grad_dtype (that of the weights, or AQSGD_F32; else AQSGD_ERR_DTYPE); state; master float [n], or
+ *            NULL (all of a call's tensors have one, or none: else AQSGD_ERR_NULL; with desc.dtype AQSGD_F32 none
+ *            does).  A tensor of no elements is skipped, its pointers are not looked at.  NOT checked: tensors that
+ *            overlap each other (undefined results).
+ *   lr       device float, or NULL: takes the place of desc.lr
+ *   step     device int64, or NULL: takes the place of desc.step (below 1 counts as 1).  With these two a captured
+ *            call goes on with the training's values
+ *   scale    device float, or NULL: factor of the gradients (aqsgd_grad_norm).  One that is not finite makes the
+ *            call leave everything as it was: a step that is skipped
+ * param, grad and master need their element's alignment.  AQSGD_ERR_SHAPE: a negative count, a step below 1, betas
+ * outside [0, 1), an lr, eps or weight_decay that is negative or not finite; AQSGD_ERR_BITS: state_bits not 8 or 32.
+ *
+ * aqsgd_grad_norm: the 2-norm over all the tensors' gradients and the factor that clips them.
+ *     norm = sqrt( sum over all elements of grad^2 ) / loss_scale     (binary64, rounded to binary32 at the end)
+ *     result[0] = norm,  result[1] = min(1, max_norm / norm) / loss_scale, or NaN where norm is not finite
+ * Of the tensors only grad and n are looked at.  The order of the sum is fixed by the sizes alone: the same bits on every call.
+ *   grad_dtype  aqsgd_dtype of every grad
+ *   max_norm    not negative, infinity for no clipping (else AQSGD_ERR_SHAPE)
+ *   loss_scale  device float, or NULL for 1;  result out float[2]
+ *   workspace   aqsgd_grad_norm_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use once the
+ *               call's work has run
+ */
+typedef struct {
+    void* param;
+    const void* grad;
+    void* state;
+    float* master;
+    int64_t n;            /* elements                                                  */
+    double weight_decay;
+} aqsgd_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;         /* t, from 1 on                                              */
+    int32_t dtype;        /* aqsgd_dtype of the weights                                */
+    int32_t grad_dtype;   /* aqsgd_dtype of the gradients                              */
+    int32_t state_bits;   /* 32 or 8                                                   */
+    int32_t rounding;     /* aqsgd_round of states in 8 bits; weights go to nearest    */
+    uint64_t rng_seed;    /* key of the stochastic rounding                            */
+} aqsgd_adamw_desc;
+
+size_t aqsgd_adamw_state_bytes(const aqsgd_adamw_desc* desc, int64_t n);
+int aqsgd_adamw(const aqsgd_adamw_desc* desc, const aqsgd_adamw_tensor* tensors, int32_t n_tensors, const float* lr,
+                const int64_t* step, const float* scale, void* stream);
+size_t aqsgd_grad_norm_workspace_bytes(const aqsgd_adamw_tensor* tensors, int32_t n_tensors);
+int aqsgd_grad_norm(int32_t grad_dtype, const aqsgd_adamw_tensor* tensors, int32_t n_tensors, double max_norm,
+                    const float* loss_scale, float* result, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Tiers below HBM for the previous messages (the implementation notes of Section 3.3
  * and Appendix G: m(xi) lives in host memory or on an SSD, is brought to the GPU before
  * the forward pass of its sample and goes back after the update, both behind the

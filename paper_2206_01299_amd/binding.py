@@ -43,7 +43,9 @@ EXPORTS = ("aqsgd_codes_bytes", "aqsgd_scales_count", "aqsgd_encode", "aqsgd_dec
            "aqsgd_tier_acquire", "aqsgd_tier_release", "aqsgd_tier_drain", "aqsgd_tier_destroy",
            "aqsgd_topk_bitmap_bytes", "aqsgd_topk_codes_bytes", "aqsgd_grad_topk_quant",
            "aqsgd_grad_topk_dequant", "aqsgd_quant8_stride", "aqsgd_quant8_workspace_bytes", "aqsgd_quant8",
-           "aqsgd_matmul8_workspace_bytes", "aqsgd_matmul8", "aqsgd_ffn8", "aqsgd_ffn8_grad", "aqsgd_check_ids", "aqsgd_set_launch_shape",
+           "aqsgd_matmul8_workspace_bytes", "aqsgd_matmul8", "aqsgd_ffn8", "aqsgd_ffn8_grad",
+           "aqsgd_layernorm", "aqsgd_layernorm_grad_workspace_bytes", "aqsgd_layernorm_grad", "aqsgd_adamw_state_bytes",
+           "aqsgd_adamw", "aqsgd_grad_norm_workspace_bytes", "aqsgd_grad_norm", "aqsgd_check_ids", "aqsgd_set_launch_shape",
            "aqsgd_profile_next_launch", "aqsgd_strerror", "aqsgd_version")
 
 
@@ -82,6 +84,25 @@ class Ffn8Desc(ctypes.Structure):
     """Mirror of ``aqsgd_ffn8_desc``."""
     _fields_ = [("m", ctypes.c_int64), ("f", ctypes.c_int64), ("k", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("act", ctypes.c_int32), ("gated", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class LayernormDesc(ctypes.Structure):
+    """Mirror of ``aqsgd_layernorm_desc``."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("accumulate", ctypes.c_int32), ("eps", ctypes.c_double)]
+
+
+class AdamwTensor(ctypes.Structure):
+    """Mirror of ``aqsgd_adamw_tensor``."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("state", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
+class AdamwDesc(ctypes.Structure):
+    """Mirror of ``aqsgd_adamw_desc``."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_int64), ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32), ("rounding", ctypes.c_int32), ("rng_seed", ctypes.c_uint64)]
 
 
 ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
@@ -156,6 +177,21 @@ def lib() -> ctypes.CDLL:
         L.aqsgd_ffn8.argtypes = [fp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.aqsgd_ffn8_grad.restype = ctypes.c_int
         L.aqsgd_ffn8_grad.argtypes = [fp, vp, vp, vp, vp]
+        np_, tp, ap = ctypes.POINTER(LayernormDesc), ctypes.POINTER(AdamwTensor), ctypes.POINTER(AdamwDesc)
+        L.aqsgd_layernorm.restype = ctypes.c_int
+        L.aqsgd_layernorm.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.aqsgd_layernorm_grad_workspace_bytes.restype = size
+        L.aqsgd_layernorm_grad_workspace_bytes.argtypes = [np_]
+        L.aqsgd_layernorm_grad.restype = ctypes.c_int
+        L.aqsgd_layernorm_grad.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.aqsgd_adamw_state_bytes.restype = size
+        L.aqsgd_adamw_state_bytes.argtypes = [ap, ctypes.c_int64]
+        L.aqsgd_adamw.restype = ctypes.c_int
+        L.aqsgd_adamw.argtypes = [ap, tp, ctypes.c_int32, vp, vp, vp, vp]
+        L.aqsgd_grad_norm_workspace_bytes.restype = size
+        L.aqsgd_grad_norm_workspace_bytes.argtypes = [tp, ctypes.c_int32]
+        L.aqsgd_grad_norm.restype = ctypes.c_int
+        L.aqsgd_grad_norm.argtypes = [ctypes.c_int32, tp, ctypes.c_int32, ctypes.c_double, vp, vp, vp, size, vp]
         L.aqsgd_tier_create.restype = ctypes.c_int
         L.aqsgd_tier_create.argtypes = [ctypes.POINTER(vp), vp, vp, vp, ctypes.c_int64, ctypes.c_int64,
                                         ctypes.c_int32, ctypes.c_int32]
@@ -220,7 +256,7 @@ def _load_native():
         warnings.warn(f"{NATIVE_PATH.name} cannot be loaded ({e}): calls go through ctypes, which costs the host some "
                       "9 us a call instead of 4; build it with `python -m paper_2206_01299_amd.build`", RuntimeWarning)
         return _Ctypes()
-    mod.setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS})
+    mod.setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, LayernormDesc, AdamwDesc, {n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in EXPORTS})
     return mod
 
 
@@ -699,6 +735,197 @@ def ffn8_grad(desc: Ffn8Desc, dh, pre, dpre, *, stream=None) -> None:
     w = f * (2 if desc.gated else 1)
     _raise(lib().aqsgd_ffn8_grad(ctypes.byref(desc), _here("dh", dh, td, (m, f)), _here("pre", pre, td, (m, w)),
                                  _here("dpre", dpre, td, (m, w)), _stream(stream)))
+
+
+# ---- layer norm and the weights' update ------------------------------------------------------
+
+def make_layernorm_desc(*, rows: int, cols: int, dtype, ld: int | None = None, eps: float = 1e-5,
+                        accumulate: bool = False) -> LayernormDesc:
+    return LayernormDesc(rows, cols, cols if ld is None else ld, _code(DTYPE_CODE, dtype), int(accumulate), eps)
+
+
+def layernorm_grad_workspace_bytes(desc: LayernormDesc) -> int:
+    return int(lib().aqsgd_layernorm_grad_workspace_bytes(ctypes.byref(desc)))
+
+
+def _rows_of(what: str, t, dtype, rows: int, cols: int, ld: int) -> ctypes.c_void_p:
+    """The address of a device matrix whose rows are contiguous and ``ld`` elements apart."""
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{what} must be of shape {(rows, cols)}, got {tuple(t.shape)}")
+    if not t.is_cuda or (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != ld):
+        raise ValueError(f"{what} must be a device tensor whose rows are contiguous and {ld} elements apart")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the call is made on cuda:{torch.cuda.current_device()}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def layernorm(desc: LayernormDesc, x, *, residual=None, weight=None, bias=None, sum=None, y=None, mean=None, rstd=None,
+              row_codes=None, row_scales=None, stream=None) -> None:
+    """``aqsgd_layernorm``: ``y`` [rows, cols] of the rows of ``x`` (row stride ``desc.ld``), or of ``sum`` = ``x`` +
+    ``residual``; ``mean`` and ``rstd`` [rows] float32 for the backward pass; ``row_codes`` [rows, stride(cols)] int8 and
+    ``row_scales`` [rows] float32 as :func:`quant8` makes them of ``y``."""
+    rc = _native.layernorm(desc, x, residual, weight, bias, sum, y, mean, rstd, row_codes, row_scales, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
+    td, rows, cols = _TORCH_OF_CODE[desc.dtype], desc.rows, desc.cols
+    _raise(lib().aqsgd_layernorm(
+        ctypes.byref(desc), _rows_of("x", x, td, rows, cols, desc.ld), _here("residual", residual, td, (rows, cols)),
+        _here("weight", weight, td, (cols,)), _here("bias", bias, td, (cols,)), _here("sum", sum, td, (rows, cols)),
+        _here("y", y, td, (rows, cols)), _here("mean", mean, torch.float32, (rows,)), _here("rstd", rstd, torch.float32, (rows,)),
+        _here("row_codes", row_codes, torch.int8, (rows, quant8_stride(cols))),
+        _here("row_scales", row_scales, torch.float32, (rows,)), _stream(stream)))
+
+
+def layernorm_grad(desc: LayernormDesc, dy, x, mean, rstd, dx, *, weight=None, add=None, dweight=None, dbias=None,
+                   workspace=None, stream=None) -> None:
+    """``aqsgd_layernorm_grad``: ``dx`` [rows, cols] (plus ``add``) and the sums ``dweight`` and ``dbias`` [cols] float32
+    from ``dy`` and what the forward pass normalised (``x``, row stride ``desc.ld``) and kept."""
+    rc = _native.layernorm_grad(desc, dy, x, mean, rstd, dx, weight, add, dweight, dbias, workspace, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
+    if desc.dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    _check_stream(stream)
+    td, rows, cols = _TORCH_OF_CODE[desc.dtype], desc.rows, desc.cols
+    args = [_here("dy", dy, td, (rows, cols)), _rows_of("x", x, td, rows, cols, desc.ld), _here("mean", mean, torch.float32, (rows,)),
+            _here("rstd", rstd, torch.float32, (rows,)), _here("weight", weight, td, (cols,)), _here("add", add, td, (rows, cols)),
+            _here("dx", dx, td, (rows, cols)), _here("dweight", dweight, torch.float32, (cols,)),
+            _here("dbias", dbias, torch.float32, (cols,))]
+    need = layernorm_grad_workspace_bytes(desc) if dweight is not None or dbias is not None else 0
+    ws, nbytes = _workspace(need, workspace, dx, stream)
+    _raise(lib().aqsgd_layernorm_grad(ctypes.byref(desc), *args, ws, nbytes, _stream(stream)))
+
+
+def make_adamw_desc(*, dtype, grad_dtype=None, state_bits: int = 32, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, step: int = 1, rounding: int = NEAREST, rng_seed: int = 0) -> AdamwDesc:
+    """``grad_dtype``: the weights' where it is not given."""
+    code = _code(DTYPE_CODE, dtype)
+    return AdamwDesc(lr, beta1, beta2, eps, step, code, code if grad_dtype is None else _code(DTYPE_CODE, grad_dtype), state_bits,
+                     rounding, rng_seed & 0xFFFFFFFFFFFFFFFF)
+
+
+def adamw_state_bytes(desc: AdamwDesc, n: int) -> int:
+    """Bytes of the state (zeros before the first step) of a tensor of ``n`` elements."""
+    return int(lib().aqsgd_adamw_state_bytes(ctypes.byref(desc), n))
+
+
+def adamw_state_views(desc: AdamwDesc, state, n: int) -> tuple:
+    """The parts of a tensor's state: ``(m, v)`` float32 [n], or in 8 bits ``(m codes int8 [n], r codes uint8 [n], m scales
+    float32 [groups], r scales float32 [groups])``."""
+    def up(k):
+        return -(-k // 64) * 64
+    _want(state, "state", torch.uint8, adamw_state_bytes(desc, n), exact=True)
+    if desc.state_bits == 32:
+        return state[:4 * n].view(torch.float32), state[up(4 * n):][:4 * n].view(torch.float32)
+    p, groups = up(n), 4 * -(-n // 256)
+    return (state[:n].view(torch.int8), state[p:p + n], state[2 * p:][:groups].view(torch.float32),
+            state[2 * p + up(groups):][:groups].view(torch.float32))
+
+
+class AdamwTensors:
+    """The tensors of :func:`adamw` and :func:`grad_norm` calls, checked once and kept alive: what a program builds
+    before its first step.  ``whole``: with weights and states, not gradients alone."""
+
+    def __init__(self, array, kind: tuple, whole: bool, device: int, held):
+        self.array, self.kind, self.whole, self.device, self.held = array, kind, whole, device, held
+
+    def __len__(self) -> int:
+        return len(self.array)
+
+
+def _kind_of(desc: AdamwDesc) -> tuple:
+    return desc.dtype, desc.grad_dtype, desc.state_bits
+
+
+def adamw_tensors(desc: AdamwDesc, *, grads, params=None, states=None, masters=None, weight_decays=None) -> AdamwTensors:
+    """``params`` (any shapes, contiguous), ``grads`` of the same shapes, ``states`` (uint8, :func:`adamw_state_bytes` each),
+    ``masters`` (float32 copies of 16-bit weights) and ``weight_decays`` (numbers), each a sequence with an entry a
+    tensor.  ``grads`` alone serve :func:`grad_norm`."""
+    grads = list(grads)
+    whole = params is not None
+    lists = {"params": params, "states": states, "masters": masters, "weight_decays": weight_decays}
+    lists = {k: list(v) for k, v in lists.items() if v is not None}
+    if whole != ("states" in lists) or (not whole and lists):
+        raise ValueError("weights need states, and states, copies and decays need weights")
+    for name, v in lists.items():
+        if len(v) != len(grads):
+            raise ValueError(f"{name} must be as many as grads, {len(grads)}, got {len(v)}")
+    if desc.dtype not in _TORCH_OF_CODE or desc.grad_dtype not in _TORCH_OF_CODE:
+        raise AqsgdError(-4, strerror(-4))
+    pt, gt = _TORCH_OF_CODE[desc.dtype], _TORCH_OF_CODE[desc.grad_dtype]
+    array, written = (AdamwTensor * len(grads))(), []
+    for i, g in enumerate(grads):
+        e = array[i]
+        e.n, e.grad = g.numel(), _here(f"grads[{i}]", g, gt, g.shape)
+        if not whole:
+            continue
+        p, s = lists["params"][i], lists["states"][i]
+        e.param = _here(f"params[{i}]", p, pt, g.shape)
+        e.state = _here(f"states[{i}]", s, torch.uint8, (adamw_state_bytes(desc, e.n),))
+        written += [(e.param, p.nbytes, "params", i), (e.state, s.nbytes, "states", i)]
+        if masters is not None:
+            m = lists["masters"][i]
+            e.master = _here(f"masters[{i}]", m, torch.float32, g.shape)
+            written.append((e.master, m.nbytes, "masters", i))
+        if weight_decays is not None:
+            e.weight_decay = lists["weight_decays"][i]
+    written = sorted(w for w in written if w[1])
+    for a, b in zip(written, written[1:]):
+        if a[0] + a[1] > b[0]:
+            raise ValueError(f"{a[2]}[{a[3]}] and {b[2]}[{b[3]}] overlap")
+    return AdamwTensors(array, _kind_of(desc), whole, torch.cuda.current_device(), (grads, lists))
+
+
+def _check_tensors(tensors: AdamwTensors) -> None:
+    if tensors.device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{tensors.device}, the call is made on cuda:{torch.cuda.current_device()}")
+
+
+def adamw(desc: AdamwDesc, tensors: AdamwTensors, *, lr=None, step=None, scale=None, stream=None) -> None:
+    """``aqsgd_adamw``: one step of ``tensors`` (:func:`adamw_tensors` with a descriptor of the same types and state
+    bits; ``desc.step`` and ``desc.lr`` may change from call to call).  ``lr`` float32, ``step`` int64 and ``scale``
+    float32: device tensors of one element that are read when the call's work runs."""
+    rc = _native.adamw(desc, tensors, lr, step, scale, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
+    _check_stream(stream)
+    _check_tensors(tensors)
+    if not tensors.whole:
+        raise ValueError("the list holds gradients alone")
+    if _kind_of(desc) != tensors.kind:
+        raise ValueError("the list was made for other types or state bits than the descriptor's")
+    args = []
+    for t, what, dt in ((lr, "lr", torch.float32), (step, "step", torch.int64), (scale, "scale", torch.float32)):
+        if t is not None:
+            _want(t, what, dt, 1, exact=True)
+        args.append(_here(what, t, dt, t.shape) if t is not None else None)
+    _raise(lib().aqsgd_adamw(ctypes.byref(desc), tensors.array, len(tensors), *args, _stream(stream)))
+
+
+def grad_norm_workspace_bytes(tensors: AdamwTensors) -> int:
+    return int(lib().aqsgd_grad_norm_workspace_bytes(tensors.array, len(tensors)))
+
+
+def grad_norm(tensors: AdamwTensors, result, *, max_norm: float = float("inf"), loss_scale=None, workspace=None, stream=None) -> None:
+    """``aqsgd_grad_norm``: ``result`` [2] float32 takes the 2-norm over all gradients and the factor for :func:`adamw`
+    (``scale=result[1:]``) that clips them to ``max_norm`` and takes ``loss_scale`` (a float32 device tensor of one
+    element) out of them."""
+    rc = _native.grad_norm(tensors, result, max_norm, loss_scale, workspace, stream)
+    if rc is not None:
+        return _raise(rc) if rc else None
+    _check_stream(stream)
+    _check_tensors(tensors)
+    if loss_scale is not None:
+        _want(loss_scale, "loss_scale", torch.float32, 1, exact=True)
+    args = [_here("loss_scale", loss_scale, torch.float32, loss_scale.shape) if loss_scale is not None else None,
+            _here("result", result, torch.float32, (2,))]
+    ws, nbytes = _workspace(grad_norm_workspace_bytes(tensors), workspace, result, stream)
+    _raise(lib().aqsgd_grad_norm(tensors.kind[1], tensors.array, len(tensors), float(max_norm), *args, ws, nbytes, _stream(stream)))
 
 
 def check_ids(sample_ids, n_samples: int, flag, stream=None) -> None:

@@ -1,0 +1,557 @@
+// Kernels of aqsgd_layernorm and aqsgd_layernorm_grad.
+//
+// Both read a row once into the registers of a team of lanes (a fraction of a wave, a wave, or a workgroup of up to
+// 1024), which forms the row's sums between the load and the store.  What bounds them is memory.  The forward pass sums in
+// binary64, so that mean and rstd are the definition's binary32 numbers whatever the order, and codes that hang on them do
+// not change with the launch.  Lanes take pieces of 16 bytes side by side.
+#pragma once
+
+#include <optional>
+
+#include "aqsgd_norms.h"
+#include "aqsgd_quant8.h"
+
+namespace aqsgd {
+
+template <int DT> constexpr int kPiece = 16 / ElemBytes<DT>::value;            // elements of a piece
+
+template <int DT>
+__device__ __forceinline__ void piece_values(const u32x4_t& r, float (&f)[kPiece<DT>]) {
+    if constexpr (DT == AQSGD_F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(r[e]);
+    } else {
+        unpack_raw<DT>(Raw<DT>{r}, f);
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4_t values_piece(const float (&f)[kPiece<DT>]) {
+    if constexpr (DT == AQSGD_F32) return u32x4_t{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    else return pack_raw<DT>(f).v;
+}
+
+// The piece from column c on of a row that starts at element `at`.  Rows have at least a piece's elements; a lane whose
+// piece lies across or behind the row's end reads the row's last elements instead, and moves those it has down in
+// registers (RAGGED: pieces across the end exist); what does not exist is 0.
+template <int DT>
+__device__ __forceinline__ u32x4_t load_piece(const void* base, int64_t at, int32_t c, int32_t cols) {
+    return *reinterpret_cast<const u32x4_any_t*>(element_at<DT>(base, at + min(c, cols - kPiece<DT>)));
+}
+
+template <int DT>
+__device__ __forceinline__ u32x4_t mended_piece(u32x4_t r, int32_t c, int32_t cols) {
+    const int down = c + kPiece<DT> - cols;              // elements that do not exist
+    if (down <= 0) return r;
+    if (down >= kPiece<DT>) return u32x4_t{0, 0, 0, 0};
+    if constexpr (DT == AQSGD_F32) {
+        if (down & 2) r = u32x4_t{r[2], r[3], 0, 0};
+        if (down & 1) r = u32x4_t{r[1], r[2], r[3], 0};
+    } else {
+        if (down & 4) r = u32x4_t{r[2], r[3], 0, 0};
+        if (down & 2) r = u32x4_t{r[1], r[2], r[3], 0};
+        if (down & 1) r = u32x4_t{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16, r[3] >> 16};
+    }
+    return r;
+}
+
+// A value as the type holds it.
+template <int DT>
+__device__ __forceinline__ float rounded_to(float f) {
+    if constexpr (DT == AQSGD_F16) return static_cast<float>(static_cast<_Float16>(f));
+    else if constexpr (DT == AQSGD_BF16) return bf16_bits_to_f32(f32_to_bf16_bits(f));
+    return f;
+}
+
+template <int DT>
+__device__ __forceinline__ char* element_at(void* base, int64_t i) {
+    return static_cast<char*>(base) + i * ElemBytes<DT>::value;
+}
+
+// Stores what exists of a piece.
+template <int DT, bool RAGGED>
+__device__ __forceinline__ void store_piece_of(void* base, int64_t at, int32_t c, int32_t cols, const u32x4_t& r) {
+    if (c + kPiece<DT> <= cols || (!RAGGED && c < cols)) {
+        *reinterpret_cast<u32x4_any_t*>(element_at<DT>(base, at + c)) = r;
+        return;
+    }
+    if constexpr (RAGGED) {
+#pragma unroll
+        for (int e = 0; e < kPiece<DT> - 1; ++e) {
+            if (c + e >= cols) continue;
+            if constexpr (DT == AQSGD_F32) static_cast<uint32_t*>(base)[at + c + e] = r[e];
+            else static_cast<uint16_t*>(base)[at + c + e] = static_cast<uint16_t>(r[e >> 1] >> (16 * (e & 1)));
+        }
+    }
+}
+
+// ---- sums over a team, the same bits in all of its lanes ---------------------------------------
+template <int CTRL> __device__ __forceinline__ float dpp_moved(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int CTRL> __device__ __forceinline__ double dpp_moved(double v) {
+    const int lo = __double2loint(v), hi = __double2hiint(v);
+    return __hiloint2double(__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xf, 0xf, false), __builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xf, 0xf, false));
+}
+
+template <int LANES, typename T>
+__device__ __forceinline__ T lanes_sum(T v) {
+    if constexpr (LANES >= 2) v += dpp_moved<0xB1>(v);     // quad_perm [1,0,3,2]
+    if constexpr (LANES >= 4) v += dpp_moved<0x4E>(v);     // quad_perm [2,3,0,1]
+    if constexpr (LANES >= 8) v += dpp_moved<0x141>(v);    // row_half_mirror
+    if constexpr (LANES >= 16) v += dpp_moved<0x140>(v);   // row_mirror
+    if constexpr (LANES >= 32) v += __shfl_xor(v, 16, kWave);
+    if constexpr (LANES >= 64) v += __shfl_xor(v, 32, kWave);
+    return v;
+}
+
+// `part`: a word for each of the workgroup's waves, not in use otherwise since the last barrier.
+template <int TEAM, typename T>
+__device__ __forceinline__ T team_sum(T v, T* part) {
+    if constexpr (TEAM <= kWave) {
+        return lanes_sum<TEAM>(v);
+    } else {
+        v = lanes_sum<kWave>(v);
+        if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
+        __syncthreads();
+        const T* of = part + threadIdx.x / TEAM * (TEAM / kWave);
+        T sum = of[0];
+#pragma unroll
+        for (int w = 1; w < TEAM / kWave; ++w) sum += of[w];
+        return sum;
+    }
+}
+
+template <int TEAM>
+__device__ __forceinline__ uint32_t team_top(uint32_t v, uint32_t* part) {
+    v = __float_as_uint(team_max<(TEAM < kWave ? TEAM : kWave)>(__uint_as_float(v)));
+    if constexpr (TEAM > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < TEAM / kWave; ++w) v = max(v, part[w]);
+    }
+    return v;
+}
+
+struct TeamSpace {                       // of a workgroup that is one team
+    double first[16], second[16];
+    uint32_t top[16];
+};
+
+__device__ __forceinline__ float inverse_deviation(double squares, int32_t cols, double eps) {
+    return static_cast<float>(1.0 / sqrt(squares / cols + eps));
+}
+
+// ---- forward -----------------------------------------------------------------------------------
+template <int DT, int TEAM, int CPL, bool RAGGED>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(const LayernormArgs a) {
+    constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM, V = kPiece<DT>;
+    __shared__ TeamSpace space;
+    const int lane = threadIdx.x % TEAM;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows) {
+        const bool here = first + threadIdx.x / TEAM < a.rows;
+        const int64_t row = here ? first + threadIdx.x / TEAM : a.rows - 1;          // the last row again: its lanes store nothing
+        constexpr bool kEarly = TEAM <= 256;              // weight and bias are asked for with the row; a team of 1024 has no registers for them
+        u32x4_t held[CPL], w[kEarly ? CPL : 1], b[kEarly ? CPL : 1];
+        const auto column = [&](int i) { return (i * TEAM + lane) * V; };
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) held[i] = load_piece<DT>(a.x, row * a.ld, column(i), a.cols);
+        if (a.residual) {
+            u32x4_t more[CPL];
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) more[i] = load_piece<DT>(a.residual, row * a.cols, column(i), a.cols);
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                float f[V], r[V];
+                piece_values<DT>(held[i], f);
+                piece_values<DT>(more[i], r);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] += r[e];
+                held[i] = values_piece<DT>(f);
+            }
+        }
+        if constexpr (kEarly) {
+            if (a.weight) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) w[i] = load_piece<DT>(a.weight, 0, column(i), a.cols);
+            }
+            if (a.bias) {
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) b[i] = load_piece<DT>(a.bias, 0, column(i), a.cols);
+            }
+        }
+        double total = 0.0;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            held[i] = mended_piece<DT>(held[i], column(i), a.cols);
+            float f[V];
+            piece_values<DT>(held[i], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) total += static_cast<double>(f[e]);
+        }
+        if (a.sum && here) {
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) store_piece_of<DT, RAGGED>(a.sum, row * a.cols, column(i), a.cols, held[i]);
+        }
+        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) / a.cols);
+        double squares = 0.0;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            float f[V];
+            piece_values<DT>(held[i], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const double d = static_cast<double>(column(i) + (RAGGED ? e : 0) < a.cols ? f[e] - mean : 0.0f);
+                squares = fma(d, d, squares);
+            }
+        }
+        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.cols, a.eps);
+        if (a.mean && here && lane == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            float f[V], more[V];
+            piece_values<DT>(held[i], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = (f[e] - mean) * rstd;
+            if (a.weight) {
+                piece_values<DT>(mended_piece<DT>(kEarly ? w[kEarly ? i : 0] : load_piece<DT>(a.weight, 0, column(i), a.cols), column(i), a.cols), more);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = f[e] * more[e];
+            }
+            if (a.bias) {
+                piece_values<DT>(mended_piece<DT>(kEarly ? b[kEarly ? i : 0] : load_piece<DT>(a.bias, 0, column(i), a.cols), column(i), a.cols), more);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = f[e] + more[e];
+            }
+            // zeros behind the row's end: codes' rows have them, and they are no maximum
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = column(i) + (RAGGED ? e : 0) < a.cols ? f[e] : 0.0f;
+            held[i] = values_piece<DT>(f);
+            if (a.y && here) store_piece_of<DT, RAGGED>(a.y, row * a.cols, column(i), a.cols, held[i]);
+        }
+        if (a.codes) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) {
+                float f[V];
+                piece_values<DT>(held[i], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) top = max(top, magnitude_bits(f[e]));
+            }
+            const CodeScale s = code_scale(team_top<TEAM>(top, space.top));
+            if (here) {
+                if (lane == 0) a.scales[row] = s.scale;
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) {
+                    if (column(i) >= a.code_stride) continue;
+                    float f[V];
+                    piece_values<DT>(held[i], f);
+                    uint32_t k[V / 4];
+#pragma unroll
+                    for (int q = 0; q < V / 4; ++q) {
+                        int32_t c[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[e] = code_of<AQSGD_ROUND_NEAREST>(f[4 * q + e], s.inv, 0.5f);
+                        k[q] = pack_codes(c[0], c[1], c[2], c[3]);
+                    }
+                    int8_t* to = a.codes + row * a.code_stride + column(i);
+                    if constexpr (V == 8) *reinterpret_cast<u32x2_t*>(to) = u32x2_t{k[0], k[1]};
+                    else *reinterpret_cast<uint32_t*>(to) = k[0];
+                }
+            }
+        }
+        if constexpr (TEAM > kWave) __syncthreads();      // the words of `space` are free again
+    }
+}
+
+// Rows of any width, narrower than a piece or wider than a workgroup holds: read element by element, once for each sum
+// and once more for the result.
+template <int DT, int TEAM>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_any_kernel(const LayernormArgs a) {
+    constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM;
+    __shared__ TeamSpace space;
+    const int lane = threadIdx.x % TEAM;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows) {
+        const int64_t row = first + threadIdx.x / TEAM;
+        const bool here = row < a.rows;
+        const int64_t at = row * a.cols;
+        const int32_t cols = here ? a.cols : 0;
+        const auto value = [&](int32_t c) {              // as it is stored, for `sum` may be x or the residual
+            float f = load_elem<DT>(a.x, row * a.ld + c);
+            if (a.residual) f = rounded_to<DT>(f + load_elem<DT>(a.residual, at + c));
+            return f;
+        };
+        const auto again = [&](int32_t c) { return a.sum ? load_elem<DT>(a.sum, at + c) : value(c); };
+        double total = 0.0, squares = 0.0;
+        for (int32_t c = lane; c < cols; c += TEAM) {
+            const float f = value(c);
+            if (a.sum) store_elem<DT>(a.sum, at + c, f);
+            total += static_cast<double>(f);
+        }
+        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) / a.cols);
+        for (int32_t c = lane; c < cols; c += TEAM) {
+            const double d = static_cast<double>(again(c) - mean);
+            squares = fma(d, d, squares);
+        }
+        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.cols, a.eps);
+        if (a.mean && here && lane == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+        const auto result = [&](int32_t c) {
+            float y = (again(c) - mean) * rstd;
+            if (a.weight) y = y * load_elem<DT>(a.weight, c);
+            if (a.bias) y = y + load_elem<DT>(a.bias, c);
+            return rounded_to<DT>(y);
+        };
+        uint32_t top = 0;
+        if (a.codes)                                      // before y is stored: it may be what `again` reads
+            for (int32_t c = lane; c < cols; c += TEAM) top = max(top, magnitude_bits(result(c)));
+        CodeScale s = {};
+        if (a.codes) s = code_scale(team_top<TEAM>(top, space.top));
+        if (a.codes && here && lane == 0) a.scales[row] = s.scale;
+        if (a.codes || a.y) {
+            const int64_t end = !here ? 0 : a.codes ? a.code_stride : a.cols;
+            for (int64_t c = lane; c < end; c += TEAM) {
+                const float y = c < a.cols ? result(static_cast<int32_t>(c)) : 0.0f;
+                if (a.codes) a.codes[row * a.code_stride + c] = static_cast<int8_t>(code_of<AQSGD_ROUND_NEAREST>(y, s.inv, 0.5f));
+                if (a.y && c < a.cols) store_elem<DT>(a.y, at + c, y);
+            }
+        }
+        if constexpr (TEAM > kWave) __syncthreads();
+    }
+}
+
+// ---- backward ----------------------------------------------------------------------------------
+// The workspace: sums of blocks of rows, for the weight [blocks, cols] and for the bias [blocks, cols].
+struct GradPlan {
+    int team, cpl;                        // 0: rows of any width
+    int64_t blocks;                       // workgroups, and sums of each column
+};
+
+constexpr int kWideTeam = 1024;
+
+template <int DT>
+inline GradPlan grad_plan(int64_t rows, int64_t cols) {
+    const int64_t pieces = (cols + kPiece<DT> - 1) / kPiece<DT>;
+    GradPlan p = {0, 0, 0};
+    if (cols >= kPiece<DT> && pieces <= (DT == AQSGD_F32 ? 4096 : 2048)) {
+        p.team = pieces <= 16 ? 16 : pieces <= 256 ? 64 : pieces <= 1024 ? 256 : 512;
+        const int64_t per = (pieces + p.team - 1) / p.team;
+        p.cpl = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 ? 4 : 8;
+    }
+    const int64_t teams = p.team ? 512 / p.team : 1;
+    const int64_t want = p.team ? (rows + teams - 1) / teams : (rows + 63) / 64;
+    p.blocks = want < 256 ? want : 256;
+    return p;
+}
+
+// A workgroup of 512 lanes takes every blocks-th set of rows and keeps the columns' sums in registers.
+template <int DT, int TEAM, int CPL, bool RAGGED>
+__global__ __launch_bounds__(512) void layernorm_grad_kernel(const LayernormGradArgs a, const int64_t blocks) {
+    constexpr int kTeams = 512 / TEAM, V = kPiece<DT>;
+    __shared__ float part[2][2][16];
+    __shared__ float joined[kTeams > 1 ? kTeams : 1][kTeams > 1 ? TEAM * V : 1];
+    const int lane = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    const auto column = [&](int i) { return (i * TEAM + lane) * V; };
+    float dw[CPL][V] = {}, db[CPL][V] = {};
+    u32x4_t w[CPL];
+    if (a.weight) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) w[i] = mended_piece<DT>(load_piece<DT>(a.weight, 0, column(i), a.cols), column(i), a.cols);
+    }
+    int turn = 0;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams; first < a.rows; first += blocks * kTeams, turn ^= 1) {
+        const bool here = first + team < a.rows;
+        const int64_t row = here ? first + team : a.rows - 1;
+        u32x4_t x[CPL], dy[CPL], more[CPL];
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) x[i] = load_piece<DT>(a.x, row * a.ld, column(i), a.cols);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) dy[i] = load_piece<DT>(a.dy, row * a.cols, column(i), a.cols);
+        if (a.add) {
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) more[i] = load_piece<DT>(a.add, row * a.cols, column(i), a.cols);
+        }
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float along = 0.0f, across = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            x[i] = mended_piece<DT>(x[i], column(i), a.cols);
+            dy[i] = mended_piece<DT>(dy[i], column(i), a.cols);          // 0 behind the end, so that its sums are too
+            float xf[V], g[V], wf[V];
+            piece_values<DT>(x[i], xf);
+            piece_values<DT>(dy[i], g);
+            if (a.weight) piece_values<DT>(w[i], wf);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (column(i) + (RAGGED ? e : 0) >= a.cols) continue;
+                const float xh = (xf[e] - mean) * rstd, gw = a.weight ? g[e] * wf[e] : g[e];
+                along += gw;
+                across += gw * xh;
+                if (here) {
+                    dw[i][e] += g[e] * xh;
+                    db[i][e] += g[e];
+                }
+            }
+        }
+        along = team_sum<TEAM>(along, part[turn][0]) / a.cols;
+        across = team_sum<TEAM>(across, part[turn][1]) / a.cols;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            float xf[V], g[V], wf[V], af[V];
+            piece_values<DT>(x[i], xf);
+            piece_values<DT>(dy[i], g);
+            if (a.weight) piece_values<DT>(w[i], wf);
+            if (a.add) piece_values<DT>(mended_piece<DT>(more[i], column(i), a.cols), af);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xh = (xf[e] - mean) * rstd, gw = a.weight ? g[e] * wf[e] : g[e];
+                g[e] = rstd * (gw - along - xh * across);
+                if (a.add) g[e] += af[e];
+            }
+            if (here) store_piece_of<DT, RAGGED>(a.dx, row * a.cols, column(i), a.cols, values_piece<DT>(g));
+        }
+    }
+    if (!a.workspace) return;
+    float* to = a.workspace + static_cast<int64_t>(blockIdx.x) * a.cols;
+    const auto leave = [&](float (&sums)[CPL][V], float* at) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            if constexpr (kTeams > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < V; ++e) joined[team][lane * V + e] = sums[i][e];
+                __syncthreads();
+                for (int c = threadIdx.x; c < TEAM * V; c += TEAM * kTeams) {
+                    float s = joined[0][c];
+#pragma unroll
+                    for (int t = 1; t < kTeams; ++t) s += joined[t][c];
+                    if (i * TEAM * V + c < a.cols) at[i * TEAM * V + c] = s;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (column(i) + e < a.cols) at[column(i) + e] = sums[i][e];
+            }
+        }
+    };
+    if (a.dweight) leave(dw, to);
+    if (a.dbias) leave(db, to + blocks * a.cols);
+}
+
+// Rows of any width: the columns' sums by a launch of their own, in front of the one that may write dx over dy.
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_grad_columns_kernel(const LayernormGradArgs a, const int64_t blocks) {
+    for (int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; c < a.cols; c += static_cast<int64_t>(gridDim.x) * 256) {
+        float dw = 0.0f, db = 0.0f;
+        for (int64_t row = blockIdx.y; row < a.rows; row += blocks) {
+            const float g = load_elem<DT>(a.dy, row * a.cols + c);
+            dw += g * ((load_elem<DT>(a.x, row * a.ld + c) - a.mean[row]) * a.rstd[row]);
+            db += g;
+        }
+        float* to = a.workspace + static_cast<int64_t>(blockIdx.y) * a.cols + c;
+        if (a.dweight) to[0] = dw;
+        if (a.dbias) to[blocks * a.cols] = db;
+    }
+}
+
+template <int DT, int TEAM>
+__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_grad_any_kernel(const LayernormGradArgs a) {
+    constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM;
+    __shared__ float part[2][2][16];
+    const int lane = threadIdx.x % TEAM;
+    int turn = 0;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows, turn ^= 1) {
+        const int64_t row = first + threadIdx.x / TEAM, at = row * a.cols;
+        const int32_t cols = row < a.rows ? a.cols : 0;
+        const float mean = cols ? a.mean[row] : 0.0f, rstd = cols ? a.rstd[row] : 0.0f;
+        const auto hat = [&](int32_t c) { return (load_elem<DT>(a.x, row * a.ld + c) - mean) * rstd; };
+        const auto weighted = [&](int32_t c) {
+            const float g = load_elem<DT>(a.dy, at + c);
+            return a.weight ? g * load_elem<DT>(a.weight, c) : g;
+        };
+        float along = 0.0f, across = 0.0f;
+        for (int32_t c = lane; c < cols; c += TEAM) {
+            const float g = weighted(c);
+            along += g;
+            across += g * hat(c);
+        }
+        along = team_sum<TEAM>(along, part[turn][0]) / a.cols;
+        across = team_sum<TEAM>(across, part[turn][1]) / a.cols;
+        for (int32_t c = lane; c < cols; c += TEAM) {
+            float g = rstd * (weighted(c) - along - hat(c) * across);
+            if (a.add) g += load_elem<DT>(a.add, at + c);
+            store_elem<DT>(a.dx, at + c, g);
+        }
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------------------
+template <int DT>
+hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
+    const auto go = [&](void (*kernel)(const LayernormArgs), int team) {
+        const int threads = team < 256 ? 256 : team;
+        const int64_t per = threads / team, blocks = (a.rows + per - 1) / per, most = (int64_t{1} << 30) / threads;
+        return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(static_cast<unsigned>(threads)), stream, a);
+    };
+    const int64_t pieces = (a.cols + kPiece<DT> - 1) / kPiece<DT>;
+    const bool ragged = a.cols % kPiece<DT> != 0;
+#define AQSGD_NORM(TEAM, CPL) \
+    return ragged ? go(layernorm_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_kernel<DT, TEAM, CPL, false>, TEAM)
+    if (a.cols < kPiece<DT>) return go(layernorm_any_kernel<DT, 64>, 64);
+    if (pieces <= 16) AQSGD_NORM(16, 1);
+    if (pieces <= 64) AQSGD_NORM(64, 1);
+    if (pieces <= 128) AQSGD_NORM(64, 2);
+    if (pieces <= 256) AQSGD_NORM(64, 4);
+    if (pieces <= 512) AQSGD_NORM(256, 2);
+    if (pieces <= 1024) AQSGD_NORM(256, 4);
+    if (pieces <= 2048) AQSGD_NORM(1024, 2);
+    if (pieces <= 4096) AQSGD_NORM(1024, 4);
+#undef AQSGD_NORM
+    return go(layernorm_any_kernel<DT, kWideTeam>, kWideTeam);
+}
+
+hipError_t launch_layernorm_join(const LayernormGradArgs& a, int64_t blocks, hipStream_t stream);
+
+template <int DT>
+hipError_t launch_layernorm_grad_as(const LayernormGradArgs& a, hipStream_t stream) {
+    const GradPlan p = grad_plan<DT>(a.rows, a.cols);
+    const bool sums = a.dweight || a.dbias, ragged = a.cols % kPiece<DT> != 0;
+    std::optional<ProfileSpan> span;
+    if (sums && a.rows > 0) span.emplace();
+    hipError_t err = hipSuccess;
+    const auto go = [&](void (*kernel)(const LayernormGradArgs, const int64_t)) {
+        return launch_kernel(kernel, dim3(static_cast<unsigned>(p.blocks)), dim3(512), stream, a, p.blocks);
+    };
+#define AQSGD_NORM(TEAM, CPL) \
+    else if (p.team == TEAM && p.cpl == CPL) err = ragged ? go(layernorm_grad_kernel<DT, TEAM, CPL, true>) : go(layernorm_grad_kernel<DT, TEAM, CPL, false>);
+    if (a.rows == 0) {}
+    AQSGD_NORM(16, 1) AQSGD_NORM(64, 1) AQSGD_NORM(64, 2) AQSGD_NORM(64, 4) AQSGD_NORM(256, 2) AQSGD_NORM(256, 4)
+    AQSGD_NORM(512, 4)
+    else if (DT == AQSGD_F32 && p.cpl == 8) {
+        if constexpr (DT == AQSGD_F32) err = ragged ? go(layernorm_grad_kernel<DT, 512, 8, true>) : go(layernorm_grad_kernel<DT, 512, 8, false>);
+    }
+#undef AQSGD_NORM
+    else {
+        if (sums) {
+            const int64_t across = (a.cols + 255) / 256;
+            err = launch_kernel(layernorm_grad_columns_kernel<DT>, dim3(static_cast<unsigned>(across < 4096 ? across : 4096), static_cast<unsigned>(p.blocks)), dim3(256),
+                                stream, a, p.blocks);
+            if (err != hipSuccess) return err;
+        }
+        const bool narrow = a.cols < kPiece<DT>;
+        const int64_t per = narrow ? 4 : 1, blocks = (a.rows + per - 1) / per, most = int64_t{1} << 20;
+        err = launch_kernel(narrow ? layernorm_grad_any_kernel<DT, 64> : layernorm_grad_any_kernel<DT, kWideTeam>,
+                            dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(narrow ? 256u : unsigned{kWideTeam}), stream, a);
+    }
+    if (!sums || err != hipSuccess) return err;
+    if (span) span->last();
+    return launch_layernorm_join(a, p.blocks, stream);
+}
+
+}  // namespace aqsgd

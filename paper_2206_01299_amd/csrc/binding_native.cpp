@@ -52,6 +52,12 @@ struct Api {
     decltype(&aqsgd_matmul8) matmul8;
     decltype(&aqsgd_ffn8) ffn8;
     decltype(&aqsgd_ffn8_grad) ffn8_grad;
+    decltype(&aqsgd_layernorm) layernorm;
+    decltype(&aqsgd_layernorm_grad_workspace_bytes) layernorm_grad_workspace_bytes;
+    decltype(&aqsgd_layernorm_grad) layernorm_grad;
+    decltype(&aqsgd_adamw) adamw;
+    decltype(&aqsgd_grad_norm_workspace_bytes) grad_norm_workspace_bytes;
+    decltype(&aqsgd_grad_norm) grad_norm;
 };
 Api g_api;
 PyTypeObject* g_desc_type = nullptr;      // the binding's ctypes mirrors of aqsgd_desc and aqsgd_job
@@ -59,6 +65,8 @@ PyTypeObject* g_job_type = nullptr;
 PyTypeObject* g_quant8_type = nullptr;    // and of the descriptors of the 8-bit operators
 PyTypeObject* g_matmul8_type = nullptr;
 PyTypeObject* g_ffn8_type = nullptr;
+PyTypeObject* g_layernorm_type = nullptr; // and of those of the layer norm and the weights' update
+PyTypeObject* g_adamw_type = nullptr;
 
 // The memory of a ctypes structure of exactly this type, while the view lives.
 class View {
@@ -306,19 +314,11 @@ bool known_type(int32_t dtype, c10::ScalarType& type) {
 }
 
 // A call of these operators: tensors of exact shapes on the current device; None where one may be left out.
-template <typename Desc>
-struct Call8 {
-    Desc d = {};
-    c10::ScalarType type = c10::ScalarType::Float;
+struct Placed {
     bool ok = false;
     int device;
 
-    Call8(PyObject* desc, PyTypeObject* mirror) : device(c10::hip::current_device()) {
-        View v(desc, mirror, sizeof(Desc));
-        if (!v) return;
-        std::memcpy(&d, v.template as<Desc>(), sizeof d);
-        ok = known_type(d.dtype, type);
-    }
+    Placed() : device(c10::hip::current_device()) {}
     const at::Tensor* on_device(PyObject* o, c10::ScalarType t) {
         if (!ok || !THPVariable_CheckExact(o)) { ok = false; return nullptr; }
         const at::Tensor& x = THPVariable_Unpack(o);
@@ -368,14 +368,31 @@ struct Call8 {
     }
 };
 
+template <typename Desc>
+struct Call8 : Placed {
+    Desc d = {};
+    c10::ScalarType type = c10::ScalarType::Float;
+
+    Call8(PyObject* desc, PyTypeObject* mirror) {
+        View v(desc, mirror, sizeof(Desc));
+        if (!v) return;
+        std::memcpy(&d, v.template as<Desc>(), sizeof d);
+        ok = known_type(d.dtype, type);
+    }
+    // A matrix whose rows are contiguous and ld elements apart.
+    const void* rows(PyObject* o, int64_t n, int64_t cols, int64_t ld) {
+        const at::Tensor* x = on_device(o, type);
+        ok = x && x->dim() == 2 && x->size(0) == n && x->size(1) == cols && (cols <= 1 || x->stride(1) == 1) &&
+             (n <= 1 || cols == 0 || x->stride(0) == ld);
+        return ok ? x->data_ptr() : nullptr;
+    }
+};
+
 AQSGD_ENTRY(py_quant8, 9, {
     Call8<aqsgd_quant8_desc> c(p[0], g_quant8_type);
     const auto f32 = c10::ScalarType::Float; const auto i8 = c10::ScalarType::Char;
-    const at::Tensor* x = c.on_device(p[1], c.type);
-    c.ok = x && x->dim() == 2 && x->size(0) == c.d.rows && x->size(1) == c.d.cols && (c.d.cols <= 1 || x->stride(1) == 1) &&
-           (c.d.rows <= 1 || c.d.cols == 0 || x->stride(0) == c.d.ld);
+    const void* at = c.rows(p[1], c.d.rows, c.d.cols, c.d.ld);
     if (!c.ok) Py_RETURN_NONE;
-    const void* at = x->data_ptr();
     const int64_t across = static_cast<int64_t>(g_api.quant8_stride(c.d.cols)); const int64_t down = static_cast<int64_t>(g_api.quant8_stride(c.d.rows));
     auto* rc = static_cast<int8_t*>(c.matrix(p[2], i8, c.d.rows, across, true)); auto* rs = static_cast<float*>(c.vector(p[3], f32, c.d.rows, true));
     auto* cc = static_cast<int8_t*>(c.matrix(p[4], i8, c.d.cols, down, true)); auto* cs = static_cast<float*>(c.vector(p[5], f32, c.d.cols, true));
@@ -423,6 +440,108 @@ AQSGD_ENTRY(py_ffn8_grad, 5, {
     void* dh = c.matrix(p[1], c.type, c.d.m, c.d.f); void* pre = c.matrix(p[2], c.type, c.d.m, w); void* dpre = c.matrix(p[3], c.type, c.d.m, w);
     void* s = c.stream(p[4]);
     return launch(c, [&] { return g_api.ffn8_grad(&c.d, dh, pre, dpre, s); });
+})
+
+// ---- layer norm and the weights' update ----------------------------------------------------
+AQSGD_ENTRY(py_layernorm, 12, {
+    Call8<aqsgd_layernorm_desc> c(p[0], g_layernorm_type);
+    if (!c.ok) Py_RETURN_NONE;
+    const auto f32 = c10::ScalarType::Float; const int64_t n = c.d.rows; const int64_t k = c.d.cols;
+    const void* x = c.rows(p[1], n, k, c.d.ld); void* res = c.matrix(p[2], c.type, n, k, true);
+    void* w = c.vector(p[3], c.type, k, true); void* b = c.vector(p[4], c.type, k, true);
+    void* sum = c.matrix(p[5], c.type, n, k, true); void* y = c.matrix(p[6], c.type, n, k, true);
+    auto* mean = static_cast<float*>(c.vector(p[7], f32, n, true)); auto* rstd = static_cast<float*>(c.vector(p[8], f32, n, true));
+    auto* codes = static_cast<int8_t*>(c.matrix(p[9], c10::ScalarType::Char, n, static_cast<int64_t>(g_api.quant8_stride(k)), true));
+    auto* scales = static_cast<float*>(c.vector(p[10], f32, n, true)); void* s = c.stream(p[11]);
+    return launch(c, [&] { return g_api.layernorm(&c.d, x, res, w, b, sum, y, mean, rstd, codes, scales, s); });
+})
+
+AQSGD_ENTRY(py_layernorm_grad, 12, {
+    Call8<aqsgd_layernorm_desc> c(p[0], g_layernorm_type);
+    if (!c.ok) Py_RETURN_NONE;
+    const auto f32 = c10::ScalarType::Float; const int64_t n = c.d.rows; const int64_t k = c.d.cols;
+    void* dy = c.matrix(p[1], c.type, n, k); const void* x = c.rows(p[2], n, k, c.d.ld);
+    auto* mean = static_cast<float*>(c.vector(p[3], f32, n)); auto* rstd = static_cast<float*>(c.vector(p[4], f32, n));
+    void* dx = c.matrix(p[5], c.type, n, k); void* w = c.vector(p[6], c.type, k, true); void* add = c.matrix(p[7], c.type, n, k, true);
+    auto* dw = static_cast<float*>(c.vector(p[8], f32, k, true)); auto* db = static_cast<float*>(c.vector(p[9], f32, k, true));
+    size_t bytes; void* ws = c.workspace(p[10], c.ok && (dw || db) ? g_api.layernorm_grad_workspace_bytes(&c.d) : 0, bytes);
+    void* s = c.stream(p[11]);
+    return launch(c, [&] { return g_api.layernorm_grad(&c.d, dy, x, mean, rstd, w, add, dx, dw, db, ws, bytes, s); });
+})
+
+// The binding's list of tensors: its array's memory while this lives, on the current device.
+class List {
+public:
+    List(PyObject* o, Placed& c) {
+        PyObject* array = attribute(o, "array");
+        PyObject* device = attribute(o, "device");
+        PyObject* whole_flag = attribute(o, "whole");
+        kind_ = attribute(o, "kind");
+        ok_ = array && device && whole_flag && kind_ && PyLong_Check(device) && PyLong_AsLong(device) == c.device &&
+              PyTuple_CheckExact(kind_) && PyTuple_GET_SIZE(kind_) == 3 && PyObject_GetBuffer(array, &view_, PyBUF_SIMPLE) == 0;
+        whole = whole_flag == Py_True;
+        held_ = ok_;
+        PyErr_Clear();
+        Py_XDECREF(array);
+        Py_XDECREF(device);
+        Py_XDECREF(whole_flag);
+        ok_ = ok_ && view_.len % static_cast<Py_ssize_t>(sizeof(aqsgd_adamw_tensor)) == 0;
+        c.ok = ok_;
+    }
+    ~List() {
+        if (held_) PyBuffer_Release(&view_);
+        Py_XDECREF(kind_);
+    }
+    List(const List&) = delete;
+    List& operator=(const List&) = delete;
+    const aqsgd_adamw_tensor* tensors() const { return static_cast<const aqsgd_adamw_tensor*>(view_.buf); }
+    int32_t count() const { return static_cast<int32_t>(view_.len / static_cast<Py_ssize_t>(sizeof(aqsgd_adamw_tensor))); }
+    long kind(Py_ssize_t i) const { return PyLong_AsLong(PyTuple_GET_ITEM(kind_, i)); }
+    bool whole = false;
+
+private:
+    static PyObject* attribute(PyObject* o, const char* name) {
+        PyObject* v = PyObject_GetAttrString(o, name);
+        if (!v) PyErr_Clear();
+        return v;
+    }
+    Py_buffer view_;
+    PyObject* kind_ = nullptr;
+    bool held_ = false, ok_ = false;
+};
+
+// A device tensor of one element, or None.
+template <typename T>
+T* one_value(Placed& c, PyObject* o, c10::ScalarType t) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor* x = c.on_device(o, t);
+    c.ok = x && x->numel() == 1;
+    return c.ok ? static_cast<T*>(x->data_ptr()) : nullptr;
+}
+
+AQSGD_ENTRY(py_adamw, 6, {
+    Call8<aqsgd_adamw_desc> c(p[0], g_adamw_type);
+    if (!c.ok) Py_RETURN_NONE;
+    List list(p[1], c);
+    if (!c.ok || !list.whole || list.kind(0) != c.d.dtype || list.kind(1) != c.d.grad_dtype || list.kind(2) != c.d.state_bits) Py_RETURN_NONE;
+    const auto* lr = one_value<float>(c, p[2], c10::ScalarType::Float);
+    const auto* step = one_value<int64_t>(c, p[3], c10::ScalarType::Long);
+    const auto* scale = one_value<float>(c, p[4], c10::ScalarType::Float);
+    void* s = c.stream(p[5]);
+    return launch(c, [&] { return g_api.adamw(&c.d, list.tensors(), list.count(), lr, step, scale, s); });
+})
+
+AQSGD_ENTRY(py_grad_norm, 6, {
+    Placed c;
+    List list(p[0], c);
+    if (!c.ok || !PyFloat_CheckExact(p[2])) Py_RETURN_NONE;
+    const auto f32 = c10::ScalarType::Float;
+    auto* result = static_cast<float*>(c.vector(p[1], f32, 2)); const double most = PyFloat_AS_DOUBLE(p[2]);
+    const auto* loss_scale = one_value<float>(c, p[3], f32);
+    size_t bytes; void* ws = c.workspace(p[4], c.ok ? g_api.grad_norm_workspace_bytes(list.tensors(), list.count()) : 0, bytes);
+    void* s = c.stream(p[5]);
+    const int32_t type = static_cast<int32_t>(list.kind(1));
+    return launch(c, [&] { return g_api.grad_norm(type, list.tensors(), list.count(), most, loss_scale, result, ws, bytes, s); });
 })
 
 // ---- jobs -------------------------------------------------------------------------------
@@ -504,18 +623,19 @@ AQSGD_ENTRY(py_run_jobs, 2, {
     return PyLong_FromLong(status);
 })
 
-// setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, {name: address}): called once by binding.py after it has loaded
-// the library.
+// setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, LayernormDesc, AdamwDesc, {name: address}): called once by
+// binding.py after it has loaded the library.
 PyObject* py_setup(PyObject*, PyObject* const* p, Py_ssize_t np) {
-    bool types = np == 6;
-    for (Py_ssize_t i = 0; types && i < 5; ++i) types = PyType_Check(p[i]);
-    if (!types || !PyDict_Check(p[5])) {
-        PyErr_SetString(PyExc_TypeError, "setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, addresses)");
+    constexpr Py_ssize_t kTypes = 7;
+    bool types = np == kTypes + 1;
+    for (Py_ssize_t i = 0; types && i < kTypes; ++i) types = PyType_Check(p[i]);
+    if (!types || !PyDict_Check(p[kTypes])) {
+        PyErr_SetString(PyExc_TypeError, "setup(Desc, Job, Quant8Desc, Matmul8Desc, Ffn8Desc, LayernormDesc, AdamwDesc, addresses)");
         return nullptr;
     }
 #define AQSGD_TAKE(name)                                                              \
     {                                                                                 \
-        PyObject* a = PyDict_GetItemString(p[5], "aqsgd_" #name);                     \
+        PyObject* a = PyDict_GetItemString(p[kTypes], "aqsgd_" #name);                \
         void* f = a ? PyLong_AsVoidPtr(a) : nullptr;                                  \
         if (!f) {                                                                     \
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_KeyError, "aqsgd_" #name);   \
@@ -529,11 +649,15 @@ PyObject* py_setup(PyObject*, PyObject* const* p, Py_ssize_t np) {
     AQSGD_TAKE(encode_lowbit) AQSGD_TAKE(decode_lowbit) AQSGD_TAKE(grad_topk_quant)
     AQSGD_TAKE(grad_topk_dequant) AQSGD_TAKE(run_jobs) AQSGD_TAKE(quant8_stride) AQSGD_TAKE(quant8_workspace_bytes)
     AQSGD_TAKE(quant8) AQSGD_TAKE(matmul8_workspace_bytes) AQSGD_TAKE(matmul8) AQSGD_TAKE(ffn8) AQSGD_TAKE(ffn8_grad)
+    AQSGD_TAKE(layernorm) AQSGD_TAKE(layernorm_grad_workspace_bytes) AQSGD_TAKE(layernorm_grad) AQSGD_TAKE(adamw)
+    AQSGD_TAKE(grad_norm_workspace_bytes) AQSGD_TAKE(grad_norm)
 #undef AQSGD_TAKE
-    for (Py_ssize_t i = 0; i < 5; ++i) Py_INCREF(p[i]);
+    for (Py_ssize_t i = 0; i < kTypes; ++i) Py_INCREF(p[i]);
     g_quant8_type = reinterpret_cast<PyTypeObject*>(p[2]);
     g_matmul8_type = reinterpret_cast<PyTypeObject*>(p[3]);
     g_ffn8_type = reinterpret_cast<PyTypeObject*>(p[4]);
+    g_layernorm_type = reinterpret_cast<PyTypeObject*>(p[5]);
+    g_adamw_type = reinterpret_cast<PyTypeObject*>(p[6]);
     g_desc_type = reinterpret_cast<PyTypeObject*>(p[0]);
     g_job_type = reinterpret_cast<PyTypeObject*>(p[1]);
     Py_RETURN_NONE;
@@ -547,6 +671,7 @@ PyMethodDef methods[] = {
     AQSGD_METHOD(grad_topk_dequant), AQSGD_METHOD(encode_job), AQSGD_METHOD(decode_job),
     AQSGD_METHOD(grad_quant_job), AQSGD_METHOD(grad_dequant_job), AQSGD_METHOD(run_jobs),
     AQSGD_METHOD(quant8), AQSGD_METHOD(matmul8), AQSGD_METHOD(ffn8), AQSGD_METHOD(ffn8_grad),
+    AQSGD_METHOD(layernorm), AQSGD_METHOD(layernorm_grad), AQSGD_METHOD(adamw), AQSGD_METHOD(grad_norm),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "The binding's per-call work (see binding.py).", -1, methods,

@@ -1,0 +1,399 @@
+"""AdamW and the gradients' norm on the GPU: weights and states bit for bit as the header's binary32 steps give them."""
+import math
+import threading
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import norms_reference as N
+import products8_reference as R
+from paper_2206_01299_amd import binding as B
+from test_gpu_norms import typed
+from test_gpu_products8 import DTYPES, MARK, Framed, stored
+
+TYPES = [("f32", "f32"), ("f16", "f32"), ("f16", "f16"), ("bf16", "f32"), ("bf16", "bf16")]
+KINDS = [(32, 0), (8, 0), (8, 1)]                                               # state bits, rounding
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    if not torch.cuda.is_available():
+        pytest.fail("these tests need an MI355X")
+    B.lib()
+
+
+class Program:
+    """Some tensors with their plain counterparts, stepped side by side."""
+
+    def __init__(self, sizes, dtype, grad_dtype, bits, rounding=0, master=False, seed=0, lead=64, decays=True, **settings):
+        self.rng = np.random.default_rng([seed, len(sizes)])
+        self.dtype, self.grad_dtype, self.bits, self.master = dtype, grad_dtype, bits, master
+        self.settings = {"lr": 1e-2, "beta1": 0.9, "beta2": 0.99, "eps": 1e-8, **settings}
+        self.desc = B.make_adamw_desc(dtype=dtype, grad_dtype=grad_dtype, state_bits=bits, rounding=rounding, rng_seed=seed + 77, **self.settings)
+        self.seed = seed + 77 if rounding else None
+        pt, gt = B.DTYPE_NAME[dtype], B.DTYPE_NAME[grad_dtype]
+        size = torch.empty(0, dtype=pt).element_size()
+        w = [self.rng.standard_normal(n).astype(np.float32) for n in sizes]
+        self.params = [Framed((n,), pt, lead if lead == 64 else lead * size) for n in sizes]
+        self.masters = [Framed((n,), torch.float32) for n in sizes] if master else None
+        self.grads = [Framed((n,), gt, lead if lead == 64 else lead * torch.empty(0, dtype=gt).element_size()) for n in sizes]
+        self.states = [Framed((N.state_bytes(n, bits),), torch.uint8) for n in sizes]
+        for i, x in enumerate(w):
+            self.params[i].t.copy_(torch.from_numpy(x))
+            if master:
+                self.masters[i].t.copy_(torch.from_numpy(x))
+            self.states[i].t.zero_()
+        self.weights = [x if master else typed(dtype)(x) for x in w]
+        self.plain = [N.State(n, bits) for n in sizes]
+        self.decays = [0.01 * (i % 3) if decays else 0.0 for i in range(len(sizes))]
+        self.list = B.adamw_tensors(self.desc, params=[f.t for f in self.params], grads=[f.t for f in self.grads],
+                                    states=[f.t for f in self.states], masters=[f.t for f in self.masters] if master else None,
+                                    weight_decays=self.decays)
+
+    def draw(self, scale=1.0):
+        for f in self.grads:
+            f.t.copy_(torch.from_numpy(scale * self.rng.standard_normal(f.t.numel()) * np.exp(self.rng.standard_normal(f.t.numel()))))
+
+    def step(self, step, scale=None, **kw):
+        self.desc.step = step
+        given = None if scale is None else torch.tensor(scale, device="cuda")
+        B.adamw(self.desc, self.list, scale=given, **kw)
+        self.follow(step, scale)
+
+    def follow(self, step, scale=None, lr=None):
+        first = 0
+        for i, (f, s) in enumerate(zip(self.grads, self.plain)):
+            new = N.adamw(self.weights[i], f.t.float().cpu().numpy(), s, **{**self.settings, **({} if lr is None else {"lr": lr})}, step=step,
+                          decay=self.decays[i], scale=scale, seed=self.seed, first=first)
+            self.weights[i] = new if self.master else typed(self.dtype)(new)
+            first += N.up(s.n, 256)
+
+    def check(self, tag=""):
+        torch.cuda.synchronize()
+        for i, s in enumerate(self.plain):
+            where = f"{self.dtype}/{self.grad_dtype} {self.bits} bits {tag}: tensor {i} of {s.n}"
+            for f in (self.params[i], self.grads[i], self.states[i], *([self.masters[i]] if self.master else [])):
+                f.check(where)
+            got = B.adamw_state_views(self.desc, self.states[i].t, s.n)
+            for name, a, b in zip("mv" if self.bits == 32 else ("m codes", "r codes", "m scales", "r scales"), got, s.parts()):
+                a = a.cpu().numpy()
+                bad = np.flatnonzero(~((a == b) | (np.isnan(a.astype(np.float32)) & np.isnan(b.astype(np.float32)))))
+                assert bad.size == 0, f"{where}: {name} differs at {bad[:3]}: {a[bad[:3]]} instead of {b[bad[:3]]} ({bad.size} do)"
+            if self.master:
+                assert np.array_equal(self.masters[i].t.cpu().numpy(), self.weights[i], equal_nan=True), f"{where}: master"
+            want = typed(self.dtype)(self.weights[i])
+            assert np.array_equal(self.params[i].t.float().cpu().numpy(), want, equal_nan=True), f"{where}: weights"
+
+
+SIZES = [1, 3, 0, 255, 256, 257, 2047, 2048, 2049, 5000, 4, 70001]
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+@pytest.mark.parametrize("dtype,grad_dtype", TYPES)
+def test_adamw(dtype, grad_dtype, bits, rounding):
+    p = Program(SIZES, dtype, grad_dtype, bits, rounding)
+    for step in range(1, 5):
+        p.draw()
+        p.step(step, scale=None if step % 2 else 0.25)
+        p.check(f"step {step}")
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+@pytest.mark.parametrize("dtype,grad_dtype", TYPES[1:])
+def test_adamw_with_a_binary32_copy(dtype, grad_dtype, bits, rounding):
+    p = Program(SIZES, dtype, grad_dtype, bits, rounding, master=True, lead=1, seed=3)
+    for step in (1, 2, 1000):
+        p.draw()
+        p.step(step, scale=3.0)
+        p.check(f"step {step}")
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+def test_adamw_of_more_tensors_than_a_launch_holds(bits, rounding):
+    sizes = [(37 * i) % 700 for i in range(150)]
+    p = Program(sizes, "f16", "f32", bits, rounding, seed=1)
+    for step in (1, 2):
+        p.draw()
+        p.step(step)
+        p.check(f"step {step}")
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+def test_adamw_of_many_groups(bits, rounding):
+    p = Program([1_000_003, 300_000], "bf16", "bf16", bits, rounding, seed=2)
+    p.draw()
+    p.step(1)
+    p.draw(1e-3)
+    p.step(2)
+    p.check()
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+def test_adamw_settings(bits, rounding):
+    for i, settings in enumerate((dict(beta1=0.0), dict(beta2=0.0, eps=0.0), dict(lr=0.0), dict(eps=1.0, beta2=0.9), dict(beta1=0.0, beta2=0.0, lr=3.0))):
+        p = Program([513, 40], "f32", "f32", bits, rounding, seed=10 + i, decays=False, **settings)
+        for step in (1, 2):
+            p.draw()
+            p.step(step)
+            p.check(str(settings))
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_adamw_of_gradients_that_are_no_ordinary_numbers(dtype, bits, rounding):
+    """Zeros from the first step on, subnormals, the largest, infinities and NaN: in 32 bits they stay with their element, in
+    8 with their group."""
+    big = {"f16": 65504.0, "bf16": 3e38, "f32": 3e38}[dtype]
+    tiny = {"f16": 2.0 ** -24, "bf16": 2.0 ** -133, "f32": 2.0 ** -149}[dtype]
+    p = Program([2000, 300], dtype, dtype, bits, rounding, seed=5)
+    for step in range(1, 4):
+        p.draw()
+        g = p.grads[0].t
+        g[:256] = 0.0
+        g[300:400] = tiny * step
+        g[512:768] = 1e-30
+        g[1024:1100] = big
+        if step == 2:
+            g[1300], g[1600], g[1999] = math.inf, math.nan, -math.inf
+        p.step(step)
+        p.check(f"step {step}")
+    codes = B.adamw_state_views(p.desc, p.states[0].t, 2000)
+    if bits == 8:
+        assert torch.isnan(codes[2][[1300 // 256, 1600 // 256, 1999 // 256]]).all() and torch.isfinite(codes[2][[0, 1, 2]]).all()
+    assert torch.isfinite(p.params[1].t).all()
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+def test_a_factor_that_is_not_finite_skips_the_step(bits, rounding):
+    p = Program([700, 70], "f16", "f32", bits, rounding, master=True)
+    p.draw()
+    p.step(1, scale=0.5)
+    frames = [f.raw.clone() for f in (*p.params, *p.masters, *p.states)]
+    for bad in (math.nan, math.inf, -math.inf):
+        p.draw()
+        p.desc.step = 2
+        B.adamw(p.desc, p.list, scale=torch.tensor(bad, device="cuda"))
+        torch.cuda.synchronize()
+        for f, before in zip((*p.params, *p.masters, *p.states), frames):
+            assert torch.equal(f.raw, before)
+    p.draw()
+    p.step(2, scale=0.5)
+    p.check()
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
+def test_steps_of_a_captured_call_go_on(bits, rounding):
+    """lr, step and scale on the device: replays with new values, eager work between them, against the plain steps."""
+    p = Program([513, 5000, 40], "bf16", "f32", bits, rounding, master=True, seed=4)
+    lr, step, scale = torch.tensor([0.0], device="cuda"), torch.tensor(0, device="cuda"), torch.tensor(1.0, device="cuda")
+    result, ws = torch.empty(2, device="cuda"), torch.empty(B.grad_norm_workspace_bytes(p.list), dtype=torch.uint8, device="cuda")
+    p.draw()
+    lr.fill_(1e-3); step.fill_(1)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.grad_norm(p.list, result, max_norm=1.0, loss_scale=scale, workspace=ws)
+        B.adamw(p.desc, p.list, lr=lr, step=step, scale=result[1:])
+    for t in (1, 2, 3, 50, 100_000):
+        p.draw(float(t))
+        lr.fill_(0.01 / t); step.fill_(t); scale.fill_(2.0 ** (t % 7))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        norm = math.sqrt(sum((f.t.double() ** 2).sum().item() for f in p.grads)) / 2.0 ** (t % 7)
+        got = result.cpu().numpy()
+        assert abs(got[0] - norm) <= 2 * N.U * norm and abs(got[1] - min(1.0, 1.0 / norm) / 2.0 ** (t % 7)) <= 2 * N.U * got[1]
+        p.follow(t, scale=got[1], lr=float(lr.item()))
+        p.check(f"replay at step {t}")
+        again = torch.empty(2, device="cuda")
+        B.grad_norm(p.list, again, max_norm=1.0, loss_scale=scale)
+        assert torch.equal(again, result)
+
+
+def test_a_step_below_one_on_the_device_counts_as_one():
+    p = Program([300], "f32", "f32", 32)
+    p.draw()
+    B.adamw(p.desc, p.list, step=torch.tensor([-5], device="cuda"))
+    p.follow(1)
+    p.check()
+
+
+def test_streams_and_both_ways_of_the_binding(monkeypatch):
+    side = torch.cuda.Stream()
+    programs = [Program([513, 5000, 40], "f16", "f16", 8, 1, seed=6) for _ in range(4)]
+    for i, p in enumerate(programs):
+        if i == 2:
+            monkeypatch.setattr(B, "_native", B._Ctypes())
+        p.draw()
+        torch.cuda.synchronize()
+        if i == 0:
+            p.step(1)
+        elif i == 1:
+            p.step(1, stream=side)
+        else:
+            with torch.cuda.stream(side if i == 3 else torch.cuda.current_stream()):
+                p.step(1, scale=None)
+        result = torch.empty(2, device="cuda")
+        torch.cuda.synchronize()
+        B.grad_norm(p.list, result, max_norm=3, stream=side)
+        torch.cuda.synchronize()
+        p.check(f"way {i}")
+        p.result = result
+    for p in programs[1:]:
+        assert torch.equal(p.result, programs[0].result)
+
+
+def test_calls_of_two_threads_at_once():
+    programs = [Program([513, 70001, 40], "bf16", "f32", 8, 1, seed=8 + i) for i in range(2)]
+    errors = []
+
+    def work(p):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for step in range(1, 5):
+                    p.draw()
+                    p.step(step)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:                                              # told to the test's own thread
+            errors.append(e)
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(p,)) for p in programs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for p in programs:
+        p.check()
+
+
+def test_lists_without_elements():
+    d = B.make_adamw_desc(dtype="f32")
+    empty = torch.empty(0, device="cuda")
+    for n in (0, 3):
+        made = B.adamw_tensors(d, params=[empty] * n, grads=[empty] * n, states=[torch.empty(0, dtype=torch.uint8, device="cuda")] * n)
+        B.adamw(d, made)
+        result = torch.full((2,), 7.0, device="cuda")
+        B.grad_norm(made, result, max_norm=1.0, loss_scale=torch.tensor(4.0, device="cuda"))
+        assert result.tolist() == [0.0, 0.25]
+
+
+# ---- the norm ----------------------------------------------------------------------------------
+
+def grads_of(sizes, dtype, seed=0, scale=1.0):
+    rng = np.random.default_rng([seed, len(sizes)])
+    return [stored(scale * rng.standard_normal(n), dtype)[0] for n in sizes]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sizes", [[1], [3], [4095, 4096, 4097], [0, 5, 0, 70001], [(31 * i) % 900 for i in range(150)], [9_000_001], [5_000_000, 7, 3_000_001]])
+def test_grad_norm(dtype, sizes):
+    grads = grads_of(sizes, dtype)
+    made = B.adamw_tensors(B.make_adamw_desc(dtype=dtype), grads=grads)
+    want = math.sqrt(sum((g.double() ** 2).sum().item() for g in grads))
+    ws = Framed((B.grad_norm_workspace_bytes(made),), torch.uint8)
+    for most, loss in ((1.0, None), (math.inf, 8.0), (want / 3, 0.5), (want * 2, None), (0.0, 2.0)):
+        result = Framed((2,), torch.float32)
+        B.grad_norm(made, result.t, max_norm=most, loss_scale=None if loss is None else torch.tensor(loss, device="cuda"), workspace=ws.t)
+        torch.cuda.synchronize()
+        ws.check("workspace")
+        result.check("result")
+        inverse = 1.0 if loss is None else 1.0 / loss
+        got, norm = result.t.tolist(), want * inverse
+        # one rounding to binary32; sums in binary64 are off by far less than the other half step
+        assert abs(got[0] - norm) <= 2 * N.U * norm
+        assert abs(got[1] - min(1.0, most / norm) * inverse) <= 2 * N.U * abs(got[1])
+
+
+def test_grad_norm_of_what_is_no_ordinary_number():
+    for dtype, value in (("f32", 3e38), ("bf16", 3e38), ("f16", 65504.0), ("f32", 2.0 ** -149), ("f16", 2.0 ** -24)):
+        g = torch.full((5000,), value, dtype=B.DTYPE_NAME[dtype], device="cuda")
+        result = torch.empty(2, device="cuda")
+        B.grad_norm(B.adamw_tensors(B.make_adamw_desc(dtype=dtype), grads=[g]), result, max_norm=1.0,
+                    loss_scale=torch.tensor(256.0, device="cuda"))
+        want = g[0].double().item() * math.sqrt(5000) / 256
+        assert abs(result[0].item() - want) <= 2 * N.U * want + 2.0 ** -149
+        assert abs(result[1].item() - min(1.0, 1.0 / want) / 256) <= 2 * N.U / 256
+    for bad in (math.inf, math.nan, -math.inf):
+        g = torch.ones(5000, device="cuda")
+        g[4999] = bad
+        result = torch.empty(2, device="cuda")
+        B.grad_norm(B.adamw_tensors(B.make_adamw_desc(dtype="f32"), grads=[g]), result, max_norm=1.0)
+        assert not math.isfinite(result[0].item()) and math.isnan(result[1].item())
+
+
+def test_two_graphs_that_share_a_workspace():
+    lists = [B.adamw_tensors(B.make_adamw_desc(dtype="f16"), grads=grads_of(s, "f16", i)) for i, s in enumerate(([5000, 70001], [300_000]))]
+    ws = torch.empty(max(B.grad_norm_workspace_bytes(x) for x in lists), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for made in lists:
+        result, g = torch.empty(2, device="cuda"), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            B.grad_norm(made, result, workspace=ws)
+        graphs.append((g, made, result))
+    for _ in range(3):
+        for g, made, _ in graphs:
+            for t in made.held[0]:
+                t.copy_(torch.randn(t.shape, device="cuda"))
+            g.replay()
+        torch.cuda.synchronize()
+        for _, made, result in graphs:
+            want = math.sqrt(sum((t.double() ** 2).sum().item() for t in made.held[0]))
+            assert abs(result[0].item() - want) <= 2 * N.U * want and result[1].item() == 1.0
+
+
+# ---- the largest -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_tensor_whose_offsets_pass_32_bits(bits):
+    """2^31 + 300 weights: the first and the last groups are as a call on them alone gives."""
+    n, part = (1 << 31) + 300, 256 * 40
+    if torch.cuda.mem_get_info()[0] < (60 << 30):
+        pytest.skip("needs 50 GB")
+    d = B.make_adamw_desc(dtype="f16", state_bits=bits, step=3)
+    last = n // 256 * 256 - part
+    cuts = [(0, part), (last, n - last)]
+    w, g = torch.zeros(n, dtype=torch.float16, device="cuda"), torch.zeros(n, dtype=torch.float16, device="cuda")
+    state = torch.zeros(B.adamw_state_bytes(d, n), dtype=torch.uint8, device="cuda")
+    few = []
+    for at, k in cuts:
+        w[at:at + k] = torch.randn(k, device="cuda").half()
+        g[at:at + k] = torch.randn(k, device="cuda").half()
+        few.append((w[at:at + k].clone(), g[at:at + k].clone(), torch.zeros(B.adamw_state_bytes(d, k), dtype=torch.uint8, device="cuda")))
+    made = B.adamw_tensors(d, params=[w], grads=[g], states=[state])
+    for _ in range(2):
+        B.adamw(d, made)
+    result, want = torch.empty(2, device="cuda"), math.sqrt(sum((x[1].double() ** 2).sum().item() for x in few))
+    B.grad_norm(made, result)
+    assert abs(result[0].item() - want) <= 2 * N.U * want
+    for (at, k), (fw, fg, fs) in zip(cuts, few):
+        alone = B.adamw_tensors(d, params=[fw], grads=[fg], states=[fs])
+        for _ in range(2):
+            B.adamw(d, alone)
+        assert torch.equal(w[at:at + k], fw)
+        for view, whole in zip(B.adamw_state_views(d, fs, k), B.adamw_state_views(d, state, n)):
+            first = at if view.numel() == k else at // 256
+            assert torch.equal(whole[first:first + view.numel()], view)
+    del w, g, state, made
+    torch.cuda.empty_cache()
+
+
+def test_the_time_of_a_call_of_several_launches():
+    p = Program([700] * 150, "f32", "f32", 32)
+    p.draw()
+    result = torch.empty(2, device="cuda")
+    few = B.adamw_tensors(p.desc, params=[p.params[0].t], grads=[p.grads[0].t], states=[p.states[0].t])
+    for call in (lambda: B.adamw(p.desc, p.list), lambda: B.adamw(p.desc, few), lambda: B.grad_norm(p.list, result), lambda: B.grad_norm(few, result)):
+        call()
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record(); stop.record()                                       # makes the events
+        torch.cuda.synchronize()
+        B.profile_next_launch(start, stop)
+        call()
+        torch.cuda.synchronize()
+        assert 0.0005 < start.elapsed_time(stop) < 5.0
