@@ -15,26 +15,37 @@ int64_t layernorm_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols) {
     return 2 * p.blocks * cols * 4;
 }
 
-// Joins the blocks' sums of 64 columns: four lanes to a column, each every fourth block.  blockIdx.y: weight, bias.
-static __global__ __launch_bounds__(256) void layernorm_join_kernel(const LayernormGradArgs a, const int64_t blocks) {
-    __shared__ double part[4][64];
+// Joins the blocks' sums of 32 columns: 32 lanes to a column, each every 32nd block, all asked for at once.
+// blockIdx.y: weight, bias.
+constexpr int kJoinCols = 32, kJoinSlots = 32;
+
+static __global__ __launch_bounds__(kJoinCols * kJoinSlots) void layernorm_join_kernel(const LayernormGradArgs a, const int64_t blocks) {
+    __shared__ double part[kJoinSlots][kJoinCols];
     float* out = blockIdx.y == 0 ? a.dweight : a.dbias;
     if (!out) return;
     const float* from = a.workspace + blockIdx.y * blocks * a.cols;
-    const int lane = threadIdx.x & 63, slot = threadIdx.x >> 6;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    const int lane = threadIdx.x % kJoinCols, slot = threadIdx.x / kJoinCols;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + lane;
+    float v[256 / kJoinSlots];
+#pragma unroll
+    for (int i = 0; i < 256 / kJoinSlots; ++i) {
+        const int64_t b = slot + i * kJoinSlots;
+        v[i] = b < blocks && c < a.cols ? from[b * a.cols + c] : 0.0f;
+    }
+    const float before = slot == 0 && a.accumulate && c < a.cols ? out[c] : 0.0f;
     double s = 0.0;
-    if (c < a.cols)
-        for (int64_t b = slot; b < blocks; b += 4) s += static_cast<double>(from[b * a.cols + c]);
+#pragma unroll
+    for (int i = 0; i < 256 / kJoinSlots; ++i) s += static_cast<double>(v[i]);
     part[slot][lane] = s;
     __syncthreads();
     if (slot != 0 || c >= a.cols) return;
-    const float sum = static_cast<float>(part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane]);
-    out[c] = a.accumulate ? out[c] + sum : sum;
+#pragma unroll
+    for (int i = 1; i < kJoinSlots; ++i) s += part[i][lane];
+    out[c] = a.accumulate ? before + static_cast<float>(s) : static_cast<float>(s);
 }
 
 hipError_t launch_layernorm_join(const LayernormGradArgs& a, int64_t blocks, hipStream_t stream) {
-    return launch_kernel(layernorm_join_kernel, dim3(static_cast<unsigned>((a.cols + 63) / 64), 2), dim3(256), stream, a, blocks);
+    return launch_kernel(layernorm_join_kernel, dim3(static_cast<unsigned>((a.cols + kJoinCols - 1) / kJoinCols), 2), dim3(kJoinCols * kJoinSlots), stream, a, blocks);
 }
 
 hipError_t launch_layernorm(int dtype, const LayernormArgs& a, hipStream_t stream) {
