@@ -447,7 +447,7 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  *   dx          out  [rows, cols] dense; may be dy or add itself, and must not overlap an input otherwise
  *   dweight     out  float[cols], or NULL;  dbias out float[cols], or NULL
  *   workspace   aqsgd_layernorm_grad_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use
- *               once the call's work has run; not read where neither dweight nor dbias is asked for
+ *               once the call's work has run; NULL where that is 0 or neither dweight nor dbias is asked for
  * 0 rows: dweight and dbias are 0, or stay as they are with accumulate; nothing else is written.  codes are
  * 16-byte aligned, the rest needs its element's alignment.  AQSGD_ERR_SHAPE: no columns, an eps that is negative or
  * not finite; AQSGD_ERR_WORKSPACE as for aqsgd_quant8.

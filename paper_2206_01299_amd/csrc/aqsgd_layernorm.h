@@ -32,8 +32,8 @@ __device__ __forceinline__ u32x4_t values_piece(const float (&f)[kPiece<DT>]) {
     else return pack_raw<DT>(f).v;
 }
 
-// The piece from column c on of a row that starts at element `at`.  Rows have at least a piece's elements.  LAST: a lane's
-// last piece, which may lie across the row's end (RAGGED) or behind it; such a lane reads the row's last elements instead,
+// The piece from column c on of a row that starts at element `at`.  Rows have at least a piece's elements.  LAST: a piece
+// that may lie across the row's end (RAGGED) or behind it; such a lane reads the row's last elements instead,
 // and whole_piece moves those it has down in registers; what does not exist is 0.
 template <int DT, bool LAST>
 __device__ __forceinline__ u32x4_t load_piece(const void* base, int64_t at, int32_t c, int32_t cols) {
@@ -97,10 +97,10 @@ __device__ __forceinline__ int team_number() {
     return TEAM >= kWave ? __builtin_amdgcn_readfirstlane(t) : t;
 }
 
-// f(i, whether it is a lane's last) for each of a lane's pieces.
+// f(i, whether it may lie across or behind the row's end) for each of a lane's pieces: its last one, of eight the last four.
 template <typename F, int... I>
 __device__ __forceinline__ void each_of(F& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>(), std::bool_constant<I == sizeof...(I) - 1>()), ...);
+    (f(std::integral_constant<int, I>(), std::bool_constant<I == sizeof...(I) - 1 || (sizeof...(I) == 8 && I >= 4)>()), ...);
 }
 template <int CPL, typename F>
 __device__ __forceinline__ void each_piece(F&& f) { each_of(f, std::make_integer_sequence<int, CPL>()); }
@@ -189,7 +189,9 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows) {
         const bool here = first + team < a.rows;
         const int64_t row = here ? first + team : a.rows - 1;          // the last row again: its lanes store nothing
-        constexpr bool kEarly = TEAM <= 256;              // weight and bias are asked for with the row; a team of 1024 has no registers for them
+        // Weight and bias are asked for with the row where registers allow (4096 x 1600 float16 with residual and codes
+        // 13.0 us, 14.3 without; 16384 x 4096 float32, four pieces of 256 lanes, 102 so and 98.9 without).
+        constexpr bool kEarly = TEAM < 256 || (TEAM == 256 && CPL < 4);
         u32x4_t held[CPL], w[CPL], b[CPL];
         each_piece<CPL>([&](auto i, auto last) { held[i] = load_piece<DT, last>(a.x, row * a.ld, column(i), a.cols); });
         if (a.residual) {
@@ -351,26 +353,35 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_any_kernel(
 }
 
 // ---- backward ----------------------------------------------------------------------------------
-// The workspace: sums of blocks of rows, for the weight [blocks, cols] and for the bias [blocks, cols].
+// Three ways.  Many rows: a workgroup takes many and keeps the columns' sums of them, which a second launch joins.  Few rows,
+// or rows wider than a workgroup has lanes: the columns' sums by workgroups of their own, which read dy and x a second time.
+// Rows of any width: the same, element by element.
+enum GradWay { kGradBlocks, kGradColumns, kGradAny };
+
+constexpr int kWideTeam = 1024;
+constexpr int kGradLanes = 1024;          // of a workgroup that takes many rows
+constexpr int64_t kFewRows = 1024;
+
+// The workspace of the first way: sums of blocks of rows, for the weight [blocks, cols] and for the bias [blocks, cols].
 struct GradPlan {
-    int team, cpl;                        // 0: rows of any width
+    GradWay way;
+    int team;                             // lanes to a row
     int64_t blocks;                       // workgroups, and sums of each column
 };
 
-constexpr int kWideTeam = 1024;
-constexpr int kGradLanes = 1024;          // of a workgroup of the gradient
-
+// 1024 rows (us, both ways): 1600 float16 10.7 by blocks and 7.6 by columns, 4096 float32 19.7 and 19.7; 2048 rows: 13.0 and 12.8,
+// 32.4 and 38.5, 200 float16 7.3 and 9.5.  Without sums rows alone are left, which blocks would only hold up.
 template <int DT>
-inline GradPlan grad_plan(int64_t rows, int64_t cols) {
+inline GradPlan grad_plan(int64_t rows, int64_t cols, bool sums) {
     const int64_t pieces = (cols + kPiece<DT> - 1) / kPiece<DT>;
-    GradPlan p = {0, 0, 0};
-    if (cols >= kPiece<DT> && pieces <= (DT == AQSGD_F32 ? 4096 : 2048)) {
-        p.team = 16;
-        while (p.team < pieces && p.team < kGradLanes) p.team *= 2;
-        p.cpl = static_cast<int>((pieces + p.team - 1) / p.team);          // no lane's piece but its last one lies behind the end
-    }
-    const int64_t teams = p.team ? kGradLanes / p.team : 1;
-    const int64_t want = p.team ? (rows + teams - 1) / teams : (rows + 63) / 64;
+    GradPlan p = {kGradAny, 0, 0};
+    if (cols < kPiece<DT> || pieces > (DT == AQSGD_F32 ? 4096 : 2048)) return p;
+    p.way = kGradColumns;
+    if (!sums || rows <= kFewRows || pieces > kGradLanes) return p;
+    p.way = kGradBlocks;
+    p.team = 16;
+    while (p.team < pieces) p.team *= 2;
+    const int64_t teams = kGradLanes / p.team, want = (rows + teams - 1) / teams;
     p.blocks = want < 256 ? want : 256;
     return p;
 }
@@ -409,117 +420,215 @@ struct GradRow {
     }
 };
 
-// A workgroup takes every blocks-th set of rows, asks for the next one before it computes one, and keeps the columns' sums in
-// registers to its end.
-template <int DT, int TEAM, int CPL, bool RAGGED>
+// A workgroup takes every blocks-th set of rows, a piece a lane, asks for the next one before it computes one, and keeps the
+// columns' sums in registers to its end.
+template <int DT, int TEAM, bool RAGGED>
 __global__ __launch_bounds__(kGradLanes) void layernorm_grad_kernel(const LayernormGradArgs a, const int64_t blocks) {
     constexpr int kTeams = kGradLanes / TEAM, V = kPiece<DT>;
-    constexpr bool kAhead = CPL == 1;
     __shared__ float2 part[2][kGradLanes / kWave];
     __shared__ float joined[kTeams > 1 ? kTeams : 1][kTeams > 1 ? TEAM * V : 1];
     const int lane = threadIdx.x % TEAM, team = team_number<TEAM>();
-    const auto column = [&](int i) { return (i * TEAM + lane) * V; };
-    float dw[CPL][V] = {}, db[CPL][V] = {}, w[CPL][V];
+    const int32_t c = lane * V;
+    float dw[V] = {}, db[V] = {}, w[V];
     const int64_t stride = blocks * kTeams;
     const auto row_of = [&](int64_t first) { return min(first + team, a.rows - 1); };
     int64_t first = static_cast<int64_t>(blockIdx.x) * kTeams;
-    GradRow<DT, TEAM, CPL> now, next;
+    GradRow<DT, TEAM, 1> now, next;
     now.ask(a, row_of(first), lane);
     if (a.weight) {
-        u32x4_t raw[CPL];
-        each_piece<CPL>([&](auto i, auto last) { raw[i] = load_piece<DT, last>(a.weight, 0, column(i), a.cols); });
-        each_piece<CPL>([&](auto i, auto last) { piece_values<DT>(whole_piece<DT, last, RAGGED>(raw[i], column(i), a.cols), w[i]); });
+        piece_values<DT>(whole_piece<DT, true, RAGGED>(load_piece<DT, true>(a.weight, 0, c, a.cols), c, a.cols), w);
     } else {
 #pragma unroll
-        for (int i = 0; i < CPL; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) w[i][e] = 1.0f;
+        for (int e = 0; e < V; ++e) w[e] = 1.0f;
     }
     const float each = 1.0f / static_cast<float>(a.cols);
     int turn = 0;
     for (; first < a.rows; first += stride, turn ^= 1) {
         const bool here = first + team < a.rows, more = first + stride < a.rows;
         const int64_t row = row_of(first);
-        if (kAhead && more) next.ask(a, row_of(first + stride), lane);
+        if (more) next.ask(a, row_of(first + stride), lane);
         // Where there is no column or no row dy is 0, and with it whatever is summed.  x is then one of the row's, or the last
         // row's: finite, unless that row's own sums are NaN anyway.
-        const float mean = now.mean, rstd = now.rstd;
-        float along = 0.0f, across = 0.0f, xh[CPL][V], gw[CPL][V];
-        each_piece<CPL>([&](auto i, auto last) {
-            float g[V];
-            piece_values<DT>(whole_piece<DT, last, RAGGED>(now.x[i], column(i), a.cols), xh[i]);
-            piece_values<DT>(here ? whole_piece<DT, last, RAGGED>(now.dy[i], column(i), a.cols) : u32x4_t{0, 0, 0, 0}, g);
+        float along = 0.0f, across = 0.0f, g[V], xh[V], gw[V];
+        piece_values<DT>(whole_piece<DT, true, RAGGED>(now.x[0], c, a.cols), xh);
+        piece_values<DT>(here ? whole_piece<DT, true, RAGGED>(now.dy[0], c, a.cols) : u32x4_t{0, 0, 0, 0}, g);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                xh[i][e] = (xh[i][e] - mean) * rstd;
-                gw[i][e] = g[e] * w[i][e];
-                along += gw[i][e];
-                across = fmaf(gw[i][e], xh[i][e], across);
-                dw[i][e] = fmaf(g[e], xh[i][e], dw[i][e]);
-                db[i][e] += g[e];
-            }
-        });
+        for (int e = 0; e < V; ++e) {
+            xh[e] = (xh[e] - now.mean) * now.rstd;
+            gw[e] = g[e] * w[e];
+            along += gw[e];
+            across = fmaf(gw[e], xh[e], across);
+            dw[e] = fmaf(g[e], xh[e], dw[e]);
+            db[e] += g[e];
+        }
         team_sums<TEAM>(along, across, part[turn]);
         along *= each;
         across *= each;
-        each_piece<CPL>([&](auto i, auto last) {
-            float out[V];
-            if (a.add) {
-                piece_values<DT>(whole_piece<DT, last, RAGGED>(now.more[i], column(i), a.cols), out);
-            } else {
+        float out[V] = {};
+        if (a.add) piece_values<DT>(whole_piece<DT, true, RAGGED>(now.more[0], c, a.cols), out);
 #pragma unroll
-                for (int e = 0; e < V; ++e) out[e] = 0.0f;
-            }
-#pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = fmaf(rstd, fmaf(-xh[i][e], across, gw[i][e] - along), out[e]);
-            if (here) store_piece_of<DT, last, RAGGED>(a.dx, row * a.cols, column(i), a.cols, values_piece<DT>(out));
-        });
-        if (more) {
-            if constexpr (kAhead) now = next;
-            else now.ask(a, row_of(first + stride), lane);
-        }
+        for (int e = 0; e < V; ++e) out[e] = fmaf(now.rstd, fmaf(-xh[e], across, gw[e] - along), out[e]);
+        if (here) store_piece_of<DT, true, RAGGED>(a.dx, row * a.cols, c, a.cols, values_piece<DT>(out));
+        if (more) now = next;
     }
-    if (!a.workspace) return;
     float* to = a.workspace + static_cast<int64_t>(blockIdx.x) * a.cols;
-    const auto leave = [&](float (&sums)[CPL][V], float* at) {
+    const auto leave = [&](const float (&sums)[V], float* at) {
+        if constexpr (kTeams > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < CPL; ++i) {
-            if constexpr (kTeams > 1) {
-                __syncthreads();
+            for (int e = 0; e < V; ++e) joined[team][lane * V + e] = sums[e];
+            __syncthreads();
+            for (int k = threadIdx.x; k < TEAM * V; k += kGradLanes) {
+                float s = joined[0][k];
 #pragma unroll
-                for (int e = 0; e < V; ++e) joined[team][lane * V + e] = sums[i][e];
-                __syncthreads();
-                for (int c = threadIdx.x; c < TEAM * V; c += kGradLanes) {
-                    float s = joined[0][c];
-#pragma unroll
-                    for (int t = 1; t < kTeams; ++t) s += joined[t][c];
-                    if (i * TEAM * V + c < a.cols) at[i * TEAM * V + c] = s;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (column(i) + e < a.cols) at[column(i) + e] = sums[i][e];
+                for (int t = 1; t < kTeams; ++t) s += joined[t][k];
+                if (k < a.cols) at[k] = s;
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (c + e < a.cols) at[c + e] = sums[e];
         }
     };
     if (a.dweight) leave(dw, to);
     if (a.dbias) leave(db, to + blocks * a.cols);
 }
 
-// Rows of any width: the columns' sums by a launch of their own, in front of the one that may write dx over dy.
-template <int DT>
-__global__ __launch_bounds__(256) void layernorm_grad_columns_kernel(const LayernormGradArgs a, const int64_t blocks) {
-    for (int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; c < a.cols; c += static_cast<int64_t>(gridDim.x) * 256) {
-        float dw = 0.0f, db = 0.0f;
-        for (int64_t row = blockIdx.y; row < a.rows; row += blocks) {
-            const float g = load_elem<DT>(a.dy, row * a.cols + c);
-            dw += g * ((load_elem<DT>(a.x, row * a.ld + c) - a.mean[row]) * a.rstd[row]);
-            db += g;
+// The second way in one launch: the first workgroups take the columns, 64 bytes of every row, the others the rows; neither needs
+// the other's sums.  Where dx is dy itself the columns go first, in a launch of their own.
+constexpr int kFewLanes = 512, kFewPieces = 4, kFewSlots = kFewLanes / kFewPieces;      // pieces side by side, rows at a time
+
+template <int DT, bool RAGGED>
+__device__ __forceinline__ void columns_of_few(const LayernormGradArgs& a, int64_t block) {
+    constexpr int V = kPiece<DT>, kCols = kFewPieces * V, kGroups = kFewLanes / kCols, kAhead = 4;
+    __shared__ float part[2][kFewSlots][kCols + 1];
+    __shared__ float last[2][kGroups][kCols + 1];
+    const int slot = threadIdx.x / kFewPieces, across = threadIdx.x % kFewPieces;
+    const int32_t c = static_cast<int32_t>(block * kCols) + across * V;
+    float dw[V] = {}, db[V] = {};
+    for (int64_t first = slot; first < a.rows; first += kFewSlots * kAhead) {
+        u32x4_t x[kAhead], dy[kAhead];
+        float mean[kAhead], rstd[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = min(first + i * kFewSlots, a.rows - 1);
+            x[i] = load_piece<DT, true>(a.x, row * a.ld, c, a.cols);
+            dy[i] = load_piece<DT, true>(a.dy, row * a.cols, c, a.cols);
+            mean[i] = a.mean[row];
+            rstd[i] = a.rstd[row];
         }
-        float* to = a.workspace + static_cast<int64_t>(blockIdx.y) * a.cols + c;
-        if (a.dweight) to[0] = dw;
-        if (a.dbias) to[blocks * a.cols] = db;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (first + i * kFewSlots >= a.rows) break;
+            float xf[V], g[V];
+            piece_values<DT>(whole_piece<DT, true, RAGGED>(x[i], c, a.cols), xf);
+            piece_values<DT>(whole_piece<DT, true, RAGGED>(dy[i], c, a.cols), g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                dw[e] = fmaf(g[e], (xf[e] - mean[i]) * rstd[i], dw[e]);
+                db[e] += g[e];
+            }
+        }
     }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        part[0][slot][across * V + e] = dw[e];
+        part[1][slot][across * V + e] = db[e];
+    }
+    __syncthreads();
+    const int col = threadIdx.x % kCols, group = threadIdx.x / kCols;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kFewSlots / kGroups; ++i) sum += part[k][group * (kFewSlots / kGroups) + i][col];
+        last[k][group][col] = sum;
+    }
+    __syncthreads();
+    const int64_t at = block * kCols + col;
+    float* out = group == 0 ? a.dweight : group == 1 ? a.dbias : nullptr;
+    if (!out || at >= a.cols) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) sum += last[group][i][col];
+    out[at] = a.accumulate ? out[at] + sum : sum;
+}
+
+template <int DT, int TEAM, int CPL, bool RAGGED>
+__global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const LayernormGradArgs a, const uint32_t column_blocks) {
+    if (blockIdx.x < column_blocks) {
+        columns_of_few<DT, RAGGED>(a, blockIdx.x);
+        return;
+    }
+    constexpr int kTeams = kFewLanes / TEAM, V = kPiece<DT>;
+    __shared__ float2 part[2][kFewLanes / kWave];
+    const int lane = threadIdx.x % TEAM, team = team_number<TEAM>();
+    const auto column = [&](int i) { return (i * TEAM + lane) * V; };
+    const float each = 1.0f / static_cast<float>(a.cols);
+    const int64_t stride = static_cast<int64_t>(gridDim.x - column_blocks) * kTeams;
+    int turn = 0;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x - column_blocks) * kTeams + team; row < a.rows; row += stride, turn ^= 1) {
+        GradRow<DT, TEAM, CPL> now;
+        now.ask(a, row, lane);
+        u32x4_t w[CPL];
+        if (a.weight) each_piece<CPL>([&](auto i, auto last) { w[i] = load_piece<DT, last>(a.weight, 0, column(i), a.cols); });
+        float along = 0.0f, across = 0.0f, xh[CPL][V], gw[CPL][V];
+        each_piece<CPL>([&](auto i, auto last) {
+            piece_values<DT>(whole_piece<DT, last, RAGGED>(now.x[i], column(i), a.cols), xh[i]);
+            piece_values<DT>(whole_piece<DT, last, RAGGED>(now.dy[i], column(i), a.cols), gw[i]);
+            if (a.weight) {
+                float wf[V];
+                piece_values<DT>(whole_piece<DT, last, RAGGED>(w[i], column(i), a.cols), wf);
+#pragma unroll
+                for (int e = 0; e < V; ++e) gw[i][e] *= wf[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                xh[i][e] = (xh[i][e] - now.mean) * now.rstd;
+                along += gw[i][e];
+                across = fmaf(gw[i][e], xh[i][e], across);
+            }
+        });
+        team_sums<TEAM>(along, across, part[turn]);
+        along *= each;
+        across *= each;
+        each_piece<CPL>([&](auto i, auto last) {
+            float out[V] = {};
+            if (a.add) piece_values<DT>(whole_piece<DT, last, RAGGED>(now.more[i], column(i), a.cols), out);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = fmaf(now.rstd, fmaf(-xh[i][e], across, gw[i][e] - along), out[e]);
+            store_piece_of<DT, last, RAGGED>(a.dx, row * a.cols, column(i), a.cols, values_piece<DT>(out));
+        });
+    }
+}
+
+// Rows of any width.  The columns' sums, in binary64 for a lane adds as many rows as there are: 16 columns to a workgroup, 16
+// lanes to a column.
+constexpr int kAnyCols = 16;
+
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_grad_columns_kernel(const LayernormGradArgs a) {
+    __shared__ double part[2][16][kAnyCols];
+    const int col = threadIdx.x % kAnyCols, slot = threadIdx.x / kAnyCols;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kAnyCols + col;
+    double dw = 0.0, db = 0.0;
+    if (c < a.cols) {
+#pragma unroll 4
+        for (int64_t row = slot; row < a.rows; row += 16) {
+            const float g = load_elem<DT>(a.dy, row * a.cols + c);
+            dw += static_cast<double>(g * ((load_elem<DT>(a.x, row * a.ld + c) - a.mean[row]) * a.rstd[row]));
+            db += static_cast<double>(g);
+        }
+    }
+    part[0][slot][col] = dw;
+    part[1][slot][col] = db;
+    __syncthreads();
+    float* out = slot == 0 ? a.dweight : slot == 1 ? a.dbias : nullptr;
+    if (!out || c >= a.cols) return;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += part[slot][i][col];
+    out[c] = a.accumulate ? out[c] + static_cast<float>(sum) : static_cast<float>(sum);
 }
 
 template <int DT, int TEAM>
@@ -562,17 +671,18 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
         return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(static_cast<unsigned>(threads)), stream, a);
     };
     const int64_t pieces = (a.cols + kPiece<DT> - 1) / kPiece<DT>;
-    const bool ragged = a.cols % kPiece<DT> != 0, few = a.rows <= 256;
+    // Few rows of three or four pieces a lane are better shared by four waves: 256 rows of 1600 float16 3.7 us, with a wave to a row
+    // 4.4; 512 rows 4.3 and 4.7, 1024 rows 6.0 and 5.1.
+    const bool ragged = a.cols % kPiece<DT> != 0, few = a.rows <= 512;
 #define AQSGD_NORM(TEAM, CPL) \
     return ragged ? go(layernorm_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_kernel<DT, TEAM, CPL, false>, TEAM)
     if (a.cols < kPiece<DT>) return go(layernorm_any_kernel<DT, 64>, 64);
     if (pieces <= 16) AQSGD_NORM(16, 1);
     if (pieces <= 64) AQSGD_NORM(64, 1);
-    if (pieces <= 256 && few) AQSGD_NORM(256, 1);
     if (pieces <= 128) AQSGD_NORM(64, 2);
+    if (pieces <= 256 && few) AQSGD_NORM(256, 1);
     if (pieces <= 192) AQSGD_NORM(64, 3);
     if (pieces <= 256) AQSGD_NORM(64, 4);
-    if (pieces <= 1024 && few) AQSGD_NORM(1024, 1);
     if (pieces <= 512) AQSGD_NORM(256, 2);
     if (pieces <= 768) AQSGD_NORM(256, 3);
     if (pieces <= 1024) AQSGD_NORM(256, 4);
@@ -586,42 +696,73 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
 hipError_t launch_layernorm_join(const LayernormGradArgs& a, int64_t blocks, hipStream_t stream);
 
 template <int DT>
-hipError_t launch_layernorm_grad_as(const LayernormGradArgs& a, hipStream_t stream) {
-    const GradPlan p = grad_plan<DT>(a.rows, a.cols);
-    const bool sums = a.dweight || a.dbias, ragged = a.cols % kPiece<DT> != 0;
+hipError_t launch_layernorm_grad_columns(const LayernormGradArgs& a, hipStream_t stream) {
+    const int64_t pieces = (a.cols + kPiece<DT> - 1) / kPiece<DT>;
+    const bool ragged = a.cols % kPiece<DT> != 0, sums = a.dweight || a.dbias;
+    const uint32_t columns = sums ? static_cast<uint32_t>((pieces + kFewPieces - 1) / kFewPieces) : 0;
     std::optional<ProfileSpan> span;
-    if (sums && a.rows > 0) span.emplace();
-    hipError_t err = hipSuccess;
+    if (sums && a.dx == a.dy) span.emplace();
+    const auto go = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int team) {
+        const int64_t per = kFewLanes / team, want = (a.rows + per - 1) / per, most = int64_t{1} << 22;      // 2^31 lanes
+        const unsigned rows = static_cast<unsigned>(want < most ? want : most);
+        if (!span) return launch_kernel(kernel, dim3(columns + rows), dim3(kFewLanes), stream, a, columns);
+        const hipError_t err = launch_kernel(kernel, dim3(columns), dim3(kFewLanes), stream, a, columns);
+        if (err != hipSuccess) return err;
+        span->last();
+        return launch_kernel(kernel, dim3(rows), dim3(kFewLanes), stream, a, uint32_t{0});
+    };
+#define AQSGD_NORM(TEAM, CPL) \
+    if (pieces <= TEAM * CPL) \
+        return ragged ? go(layernorm_grad_few_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_grad_few_kernel<DT, TEAM, CPL, false>, TEAM);
+    AQSGD_NORM(64, 1) AQSGD_NORM(64, 2) AQSGD_NORM(64, 3) AQSGD_NORM(64, 4) AQSGD_NORM(512, 1) AQSGD_NORM(512, 2) AQSGD_NORM(512, 3)
+    if constexpr (DT == AQSGD_F32) {
+        if (pieces > 2048) AQSGD_NORM(512, 8)
+    }
+#undef AQSGD_NORM
+    return ragged ? go(layernorm_grad_few_kernel<DT, 512, 4, true>, 512) : go(layernorm_grad_few_kernel<DT, 512, 4, false>, 512);
+}
+
+template <int DT>
+hipError_t launch_layernorm_grad_blocks(const LayernormGradArgs& a, const GradPlan& p, hipStream_t stream) {
+    const bool ragged = a.cols % kPiece<DT> != 0;
+    ProfileSpan span;
     const auto go = [&](void (*kernel)(const LayernormGradArgs, const int64_t)) {
         return launch_kernel(kernel, dim3(static_cast<unsigned>(p.blocks)), dim3(kGradLanes), stream, a, p.blocks);
     };
-#define AQSGD_NORM(TEAM, CPL) \
-    else if (p.team == TEAM && p.cpl == CPL) err = ragged ? go(layernorm_grad_kernel<DT, TEAM, CPL, true>) : go(layernorm_grad_kernel<DT, TEAM, CPL, false>);
-    if (a.rows == 0) {}
-    AQSGD_NORM(16, 1) AQSGD_NORM(32, 1) AQSGD_NORM(64, 1) AQSGD_NORM(128, 1) AQSGD_NORM(256, 1) AQSGD_NORM(512, 1)
-    AQSGD_NORM(1024, 1) AQSGD_NORM(1024, 2)
-    else if (DT == AQSGD_F32 && p.team) {                // rows of 16-bit elements that are so wide would spill
-        if constexpr (DT == AQSGD_F32) {
-            if (p.cpl == 3) err = ragged ? go(layernorm_grad_kernel<DT, 1024, 3, true>) : go(layernorm_grad_kernel<DT, 1024, 3, false>);
-            else err = ragged ? go(layernorm_grad_kernel<DT, 1024, 4, true>) : go(layernorm_grad_kernel<DT, 1024, 4, false>);
-        }
-    }
+    hipError_t err = hipErrorInvalidValue;
+#define AQSGD_NORM(TEAM) \
+    if (p.team == TEAM) err = ragged ? go(layernorm_grad_kernel<DT, TEAM, true>) : go(layernorm_grad_kernel<DT, TEAM, false>);
+    AQSGD_NORM(16) AQSGD_NORM(32) AQSGD_NORM(64) AQSGD_NORM(128) AQSGD_NORM(256) AQSGD_NORM(512) AQSGD_NORM(1024)
 #undef AQSGD_NORM
-    else {
-        if (sums) {
-            const int64_t across = (a.cols + 255) / 256;
-            err = launch_kernel(layernorm_grad_columns_kernel<DT>, dim3(static_cast<unsigned>(across < 4096 ? across : 4096), static_cast<unsigned>(p.blocks)), dim3(256),
-                                stream, a, p.blocks);
-            if (err != hipSuccess) return err;
-        }
-        const bool narrow = a.cols < kPiece<DT>;
-        const int64_t per = narrow ? 4 : 1, blocks = (a.rows + per - 1) / per, most = int64_t{1} << 20;
-        err = launch_kernel(narrow ? layernorm_grad_any_kernel<DT, 64> : layernorm_grad_any_kernel<DT, kWideTeam>,
-                            dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(narrow ? 256u : unsigned{kWideTeam}), stream, a);
-    }
-    if (!sums || err != hipSuccess) return err;
-    if (span) span->last();
+    if (err != hipSuccess) return err;
+    span.last();
     return launch_layernorm_join(a, p.blocks, stream);
+}
+
+template <int DT>
+hipError_t launch_layernorm_grad_any(const LayernormGradArgs& a, hipStream_t stream) {
+    const bool sums = a.dweight || a.dbias, narrow = a.cols < kPiece<DT>;
+    std::optional<ProfileSpan> span;
+    if (sums) {
+        span.emplace();
+        const hipError_t err = launch_kernel(layernorm_grad_columns_kernel<DT>, dim3(static_cast<unsigned>((a.cols + kAnyCols - 1) / kAnyCols)), dim3(256), stream, a);
+        if (err != hipSuccess) return err;
+        span->last();
+    }
+    const int64_t per = narrow ? 4 : 1, blocks = (a.rows + per - 1) / per, most = int64_t{1} << 20;
+    return launch_kernel(narrow ? layernorm_grad_any_kernel<DT, 64> : layernorm_grad_any_kernel<DT, kWideTeam>,
+                         dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(narrow ? 256u : unsigned{kWideTeam}), stream, a);
+}
+
+template <int DT>
+hipError_t launch_layernorm_grad_as(const LayernormGradArgs& a, hipStream_t stream) {
+    if (a.rows == 0) return launch_layernorm_join(a, 0, stream);
+    const GradPlan p = grad_plan<DT>(a.rows, a.cols, a.dweight || a.dbias);
+    switch (p.way) {
+    case kGradBlocks:  return launch_layernorm_grad_blocks<DT>(a, p, stream);
+    case kGradColumns: return launch_layernorm_grad_columns<DT>(a, stream);
+    default:           return launch_layernorm_grad_any<DT>(a, stream);
+    }
 }
 
 }  // namespace aqsgd

@@ -11,7 +11,7 @@ AQSGD_EXTERN_LAYERNORM(AQSGD_F16)
 AQSGD_EXTERN_LAYERNORM(AQSGD_BF16)
 
 int64_t layernorm_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols) {
-    const GradPlan p = dtype == AQSGD_F32 ? grad_plan<AQSGD_F32>(rows, cols) : grad_plan<AQSGD_F16>(rows, cols);
+    const GradPlan p = dtype == AQSGD_F32 ? grad_plan<AQSGD_F32>(rows, cols, true) : grad_plan<AQSGD_F16>(rows, cols, true);
     return 2 * p.blocks * cols * 4;
 }
 

@@ -124,15 +124,14 @@ int aqsgd_layernorm_grad(const aqsgd_layernorm_desc* d, const void* dy, const vo
         const uintptr_t e = elem_bytes(d->dtype);
         if (!aligned(dy, e) || !aligned(x, e) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, e) || !aligned(add, e) || !aligned(dx, e))
             return AQSGD_ERR_ALIGN;
-        if (sums) {
-            if (!workspace || workspace_bytes < aqsgd_layernorm_grad_workspace_bytes(d)) return AQSGD_ERR_WORKSPACE;
-            if (!aligned(workspace, 16)) return AQSGD_ERR_ALIGN;
-        }
+        const size_t need = sums ? aqsgd_layernorm_grad_workspace_bytes(d) : 0;
+        if (need && (!workspace || workspace_bytes < need)) return AQSGD_ERR_WORKSPACE;
+        if (need && !aligned(workspace, 16)) return AQSGD_ERR_ALIGN;
     }
     LayernormGradArgs a;
     a.dy = dy; a.x = x; a.mean = mean; a.rstd = rstd; a.weight = weight; a.add = add; a.dx = dx;
     a.dweight = dweight; a.dbias = dbias;
-    a.workspace = sums ? static_cast<float*>(workspace) : nullptr;
+    a.workspace = static_cast<float*>(workspace);
     a.rows = d->rows; a.ld = d->ld;
     a.cols = static_cast<int32_t>(d->cols);
     a.accumulate = d->accumulate;

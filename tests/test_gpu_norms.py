@@ -209,15 +209,18 @@ def test_layernorm_grad(dtype, rows, cols):
     run_grad(rows, cols, dtype, weight=False, pad=8, db=False)
     run_grad(rows, cols, dtype, add=True, dw=False, db=False, place="add")
     run_grad(rows, cols, dtype, add=True, dw=False, place="dy", workspace=False)
-    first = [t.clone() for t in run_grad(rows, cols, dtype, add=True, place="dy")]
-    for a, b in zip(first, run_grad(rows, cols, dtype, add=True, place="add")):
-        assert torch.equal(a, b)                                               # the same bits on every call
+    for place in (None, "dy"):
+        first = [t.clone() for t in run_grad(rows, cols, dtype, add=True, place=place)]
+        for a, b in zip(first, run_grad(rows, cols, dtype, add=True, place="add" if place is None else place)):
+            assert torch.equal(a, b)                                           # the same bits on every call
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("rows,cols", [(1, 40), (2, 1600), (15, 1600), (16, 130), (511, 64), (513, 1600), (2049, 200), (4100, 1600), (70000, 24), (20000, 300)])
+@pytest.mark.parametrize("rows,cols", [(1, 40), (2, 1600), (15, 1600), (16, 130), (511, 64), (513, 1600), (1025, 40), (1024, 700), (1025, 1001), (2049, 200), (4100, 1600), (1030, 4096),
+                                       (1027, 8191), (1500, 130), (2000, 3001), (1025, 8200), (1100, 3), (70000, 24), (20000, 300)])
 def test_layernorm_grad_by_rows(dtype, rows, cols):
     run_grad(rows, cols, dtype, add=rows % 2 == 0, accumulate=rows % 3 == 0)
+    run_grad(rows, cols, dtype, add=rows % 2 == 1, place="dy", weight=rows % 3 == 0)
 
 
 def test_layernorm_grad_of_no_rows():
@@ -432,6 +435,32 @@ def test_rows_whose_offsets_pass_32_bits():
     B.layernorm_grad(d, y, x, mean, rstd, y)
     assert torch.equal(y[-3:], dx3)
     del x, y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("cols", [3, 8])
+def test_more_rows_than_a_grid_has_teams(cols):
+    """70 million short rows, a period of 999983 again and again: every period's results are the first one's."""
+    period, rows = 999983, 70_000_000
+    d = B.make_layernorm_desc(rows=rows, cols=cols, dtype="f16")
+    x = torch.randn((period, cols), device="cuda").half().repeat(rows // period + 1, 1)[:rows].contiguous()
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.layernorm(d, x, y=y, mean=mean, rstd=rstd)
+    few = B.make_layernorm_desc(rows=period, cols=cols, dtype="f16")
+    y1, m1, r1, dx1 = torch.empty_like(x[:period]), torch.empty(period, device="cuda"), torch.empty(period, device="cuda"), torch.empty_like(x[:period])
+    B.layernorm(few, x[:period], y=y1, mean=m1, rstd=r1)
+    dx, dw = torch.empty_like(x), torch.empty(cols, device="cuda")
+    B.layernorm_grad(few, x[:period], x[:period], m1, r1, dx1)
+    B.layernorm_grad(d, x, x, mean, rstd, dx)
+    for at in range(0, rows, period):
+        n = min(period, rows - at)
+        assert torch.equal(y[at:at + n], y1[:n]) and torch.equal(dx[at:at + n], dx1[:n]) and torch.equal(mean[at:at + n], m1[:n]), at
+    again = torch.empty_like(x)
+    B.layernorm_grad(d, x, x, mean, rstd, again, dbias=dw)
+    assert torch.equal(again, dx) or cols == 8                                # by blocks the sums are formed in another order
+    want, size = x.double().sum(dim=0), x.double().abs().sum(dim=0)
+    assert ((dw.double() - want).abs() <= (128 + rows // 128 + 64) * N.U * size).all()
+    del x, y, dx
     torch.cuda.empty_cache()
 
 

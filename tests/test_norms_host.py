@@ -79,7 +79,7 @@ def test_layernorm_refusals():
 
 
 def test_layernorm_grad_refusals():
-    d = row_desc()
+    d = row_desc(rows=4096)
     need = B.layernorm_grad_workspace_bytes(d)
     assert need > 0 and lg(None) == -1
     for change, status in BAD_ROWS:
@@ -92,6 +92,8 @@ def test_layernorm_grad_refusals():
                      ("dw", 4098), ("db", 4098), ("ws", 4104)):
         assert lg(d, **{name: ctypes.c_void_p(at)}) == -6, name
     assert lg(d, ws=NULL) == -9 and lg(d, n=need - 1) == -9
+    for few in (row_desc(), row_desc(rows=4096, cols=2 ** 20, ld=2 ** 20)):             # no block's sums to join
+        assert B.layernorm_grad_workspace_bytes(few) == 0
 
 
 def test_adamw_refusals():
