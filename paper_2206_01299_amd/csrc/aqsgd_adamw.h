@@ -1,17 +1,18 @@
 // Kernels of aqsgd_adamw: one step of many tensors in one launch.
 //
-// Every element is read and written once, so memory bounds the step.  A wave takes a group of 256 elements, four
-// neighbouring ones a lane: with states in 8 bits the group's new scale is a maximum over the wave, and everything
-// stays in registers between the loads and the stores.  A workgroup's tensor is found in the launch's table by one load
-// and a vote of the wave.
+// Every element is read and written once.  With states in 32 bits memory bounds the step; in 8 bits it is near what the
+// arithmetic takes (a root and a quotient for the step, two roots for the codes, and the draws).  Lanes take four
+// neighbouring elements at a time; with states in 8 bits half a wave takes a group, whose new scale is a maximum over its
+// lanes, and everything stays in registers between the loads and the stores.  A workgroup's tensor is found in the
+// launch's table by one load and a vote of the wave.
 #pragma once
 
 #include "aqsgd_norms.h"
 
 namespace aqsgd {
 
-constexpr int kUpdateWaves = 4, kUpdateGroups = 2;                        // waves of a workgroup, groups of a wave
-constexpr int64_t kUpdateSpan = int64_t{kStateGroup} * kUpdateWaves * kUpdateGroups;
+constexpr int kUpdateWaves = 4, kUpdatePieces = 2;                        // waves of a workgroup, pieces of four elements a lane
+constexpr int64_t kUpdateSpan = int64_t{4} * kWave * kUpdateWaves * kUpdatePieces;      // elements of a workgroup
 constexpr float kStateFloor = 0x1p-100f;                                  // a group below this is held as zeros: T^2 / s is finite from here on
 constexpr float kMTop = 127.0f, kRTop = 255.0f;
 
@@ -24,10 +25,10 @@ __host__ __device__ inline int64_t state_bytes(int64_t n, int bits) {
 
 typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
 
-// Four elements at any element's address, of which `count` exist.
-template <int DT>
+// Four elements at any element's address, of which `count` exist (FULL: all four).
+template <int DT, bool FULL>
 __device__ __forceinline__ void load_four(const void* base, int64_t i, int count, float (&f)[4]) {
-    if (count >= 4) {
+    if (FULL || count >= 4) {
         if constexpr (DT == AQSGD_F32) {
             const f32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any_t*>(static_cast<const float*>(base) + i));
 #pragma unroll
@@ -45,9 +46,9 @@ __device__ __forceinline__ void load_four(const void* base, int64_t i, int count
     for (int e = 0; e < 4; ++e) f[e] = e < count ? load_elem<DT>(base, i + e) : 0.0f;
 }
 
-template <int DT>
+template <int DT, bool FULL>
 __device__ __forceinline__ void store_four(void* base, int64_t i, int count, const float (&f)[4]) {
-    if (count >= 4) {
+    if (FULL || count >= 4) {
         if constexpr (DT == AQSGD_F32) {
             __builtin_nontemporal_store(f32x4_t{f[0], f[1], f[2], f[3]}, reinterpret_cast<f32x4_any_t*>(static_cast<float*>(base) + i));
         } else {
@@ -77,13 +78,24 @@ struct UpdateFactors {
     bool scaled;
 };
 
-__device__ __forceinline__ void step_element(const AdamwArgs& a, const UpdateFactors& k, float g, float& w, float& m, float& v, float& r) {
+// The moments of one element after this step.
+__device__ __forceinline__ void step_moments(const AdamwArgs& a, const UpdateFactors& k, float g, float& m, float& v) {
     if (k.scaled) g = g * k.scale;
     m = m * a.beta1f + g * a.rest1;
     v = v * a.beta2f + (g * a.rest2) * g;
-    r = sqrtf(v);
-    const float denominator = r * k.correct + a.eps;
-    w = w * k.decay - (m / denominator) * k.length;
+}
+
+__device__ __forceinline__ float stepped_weight(const AdamwArgs& a, const UpdateFactors& k, float w, float m, float r) {
+    return w * k.decay - (m / (r * k.correct + a.eps)) * k.length;
+}
+
+// The root of a v that is 0 or at least 2^-96 (or no finite number), rounded once: the hardware's is within an ulp, and the
+// residuals of its neighbours say which of the three it is; below, the residuals are no longer exact.
+__device__ __forceinline__ float root_of(float v) {
+    const float s = __builtin_amdgcn_sqrtf(v);
+    const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
+    float r = fmaf(-down, s, v) <= 0.0f ? down : s;
+    return fmaf(-up, s, v) > 0.0f ? up : r;
 }
 
 // ---- states in 8 bits ----------------------------------------------------------------------------
@@ -103,117 +115,207 @@ __device__ __forceinline__ HeldScale held_scale(uint32_t bits, float top) {
     return h;
 }
 
-// The code of one magnitude: the neighbour below u's root and the choice between it and the next.
-__device__ __forceinline__ float held_code(float x, const HeldScale& h, float top, float least, float z) {
-    const float u = x * h.inv;
-    float k = floorf(sqrtf(u));
-    if (k * k > u) k -= 1.0f;             // the root is rounded: it may be a whole number that u's own is just below
-    k = fminf(k, top);
-    if (u - k * k >= z * (2.0f * k + 1.0f)) k += 1.0f;
-    k = fminf(k, top);
-    return h.live && x > 0.0f ? fmaxf(k, least) : 0.0f;
+// The code of one magnitude of a live group: the whole number below u's root, and one more where the distance says so.  The
+// hardware's root may be off by an ulp, so that its whole part is one off where u is next to a square.  To the nearest that
+// changes nothing: from either side the distance leads to the same neighbour.  Draws ask for the right one: the
+// root is taken a little low, and raised where the next square is not above u.  No code passes T: u is at most
+// T^2 (1 + 2^-23), nearer to T^2 than any threshold (z (2 T + 1), z at least 2^-16).
+template <int ROUND>
+__device__ __forceinline__ float held_code(float x, float inv, float z) {
+    const float u = x * inv;
+    if constexpr (ROUND == AQSGD_ROUND_NEAREST) {
+        const float k = floorf(__builtin_amdgcn_sqrtf(u));
+        return fmaf(-k, k, u) >= k + 0.5f ? k + 1.0f : k;
+    } else {
+        float k = floorf(__builtin_amdgcn_sqrtf(u) * (1.0f - 0x1p-21f));
+        const float next = k + 1.0f;
+        k = next * next <= u ? next : k;
+        return fmaf(-k, k, u) >= z * fmaf(2.0f, k, 1.0f) ? k + 1.0f : k;
+    }
 }
 
-__device__ __forceinline__ uint32_t magnitude_of(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The largest of 32 lanes, in all of them.
+__device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
+    v = dpp_max_step<0xB1>(v);
+    v = dpp_max_step<0x4E>(v);
+    v = dpp_max_step<0x141>(v);
+    v = dpp_max_step<0x140>(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max(r[0], r[1]);
+}
+
+// A quotient by a constant, rounded once for every s whose quotient is a normal number (all 2^23 significands were tried, for
+// 127^2 and 255^2).
+template <int N>
+__device__ __forceinline__ float divided_by(float s) {
+    constexpr float inv = 1.0f / N;
+    const float q = s * inv;
+    return fmaf(fmaf(-static_cast<float>(N), q, s), inv, q);
+}
+
+// Half a wave's group, elements 4 l .. 4 l + 3 and 128 + 4 l .. of it a lane l.
+template <int DT, int GT, int ROUND, bool FULL>
+__device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwArgs& a, const UpdateFactors& k, uint64_t key, int64_t group, int l) {
+    const int64_t first = group * kStateGroup + l * 4;
+    int count[2];
+    float g[2][4], w[2][4], m[2][4], v[2][4], r[2][4];
+    uint32_t mc[2], rc[2];
+    char* const m_at = t.state + first;
+    char* const r_at = m_at + whole64(t.n);
+    float* const m_scale = reinterpret_cast<float*>(t.state + 2 * whole64(t.n)) + group;
+    float* const r_scale = m_scale + whole64(4 * state_groups(t.n)) / 4;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int64_t i = first + 128 * p, left = t.n - i;
+        count[p] = FULL || left >= 4 ? 4 : left > 0 ? static_cast<int>(left) : 0;
+        load_four<GT, FULL>(t.grad, i, count[p], g[p]);
+        if (t.master) load_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
+        else load_four<DT, FULL>(t.param, i, count[p], w[p]);
+        mc[p] = rc[p] = 0;
+        if (FULL || count[p] > 0) {
+            mc[p] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(m_at + 128 * p));
+            rc[p] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(r_at + 128 * p));
+        }
+    }
+    const float m_step = divided_by<127 * 127>(*m_scale), r_step = divided_by<255 * 255>(*r_scale);
+    bool small = false;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        mc[p] ^= 0x80808080u;                              // code + 128 as bytes
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float mk = static_cast<float>((mc[p] >> (8 * e)) & 0xffu) - 128.0f, rk = static_cast<float>((rc[p] >> (8 * e)) & 0xffu);
+            const float root = (rk * rk) * r_step;
+            m[p][e] = (mk * fabsf(mk)) * m_step;
+            v[p][e] = root * root;
+            step_moments(a, k, g[p][e], m[p][e], v[p][e]);
+            small = small || __float_as_uint(v[p][e]) - 1u < 0x0f800000u - 1u;        // between 0 and 2^-96
+        }
+    }
+    if (__any(small)) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[p][e] = sqrtf(v[p][e]);
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[p][e] = root_of(v[p][e]);
+    }
+    uint32_t m_top = 0, r_top = 0;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[p][e] = stepped_weight(a, k, w[p][e], m[p][e], r[p][e]);
+            if (!FULL && e >= count[p]) m[p][e] = r[p][e] = 0.0f;
+            m_top = max(m_top, __float_as_uint(m[p][e]) & 0x7fffffffu);
+            r_top = max(r_top, __float_as_uint(r[p][e]) & 0x7fffffffu);
+        }
+        const int64_t i = first + 128 * p;
+        if (t.master) store_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
+        store_four<DT, FULL>(t.param, i, count[p], w[p]);
+    }
+    const HeldScale ms = held_scale(half_wave_max(m_top), kMTop), rs = held_scale(half_wave_max(r_top), kRTop);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        float zm[4], zr[4];
+        if constexpr (ROUND == AQSGD_ROUND_STOCHASTIC) {
+            const uint64_t block = static_cast<uint64_t>(t.group0 + group) * (kStateGroup / 4) + static_cast<uint32_t>(32 * p + l);
+            uint32_t words[4];
+            philox4x32_10(static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), static_cast<uint32_t>(key),
+                          static_cast<uint32_t>(key >> 32), words);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                zm[e] = fmaf(static_cast<float>(words[e] & 0xffffu), 0x1p-16f, 0x1p-16f);
+                zr[e] = fmaf(static_cast<float>(words[e] >> 16), 0x1p-16f, 0x1p-16f);
+            }
+        }
+        mc[p] = rc[p] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float mk = held_code<ROUND>(fabsf(m[p][e]), ms.inv, zm[e]);
+            const float rk = fmaxf(held_code<ROUND>(r[p][e], rs.inv, zr[e]), r[p][e] > 0.0f ? 1.0f : 0.0f);
+            mc[p] = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(mk, m[p][e]) + 128.0f, e, mc[p]);
+            rc[p] = __builtin_amdgcn_cvt_pk_u8_f32(rk, e, rc[p]);
+        }
+        mc[p] = ms.live ? mc[p] ^ 0x80808080u : 0;
+        rc[p] = rs.live ? rc[p] : 0;
+        if (FULL || count[p] > 0) {
+            __builtin_nontemporal_store(mc[p], reinterpret_cast<uint32_t*>(m_at + 128 * p));
+            __builtin_nontemporal_store(rc[p], reinterpret_cast<uint32_t*>(r_at + 128 * p));
+        }
+    }
+    if (l == 0) {
+        *m_scale = ms.scale;
+        *r_scale = rs.scale;
+    }
+}
+
+// Four elements with states in 32 bits.
+template <int DT, int GT, bool FULL>
+__device__ __forceinline__ void adamw32_pieces(const UpdateTensor& t, const AdamwArgs& a, const UpdateFactors& k, int64_t first) {
+    int count[kUpdatePieces];
+    float g[kUpdatePieces][4], w[kUpdatePieces][4], m[kUpdatePieces][4], v[kUpdatePieces][4];
+    char* const v_at = t.state + whole64(4 * t.n);
+#pragma unroll
+    for (int p = 0; p < kUpdatePieces; ++p) {
+        const int64_t i = first + 4 * kWave * p, left = t.n - i;
+        count[p] = FULL || left >= 4 ? 4 : left > 0 ? static_cast<int>(left) : 0;
+        load_four<GT, FULL>(t.grad, i, count[p], g[p]);
+        if (t.master) load_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
+        else load_four<DT, FULL>(t.param, i, count[p], w[p]);
+        load_four<AQSGD_F32, FULL>(t.state, i, count[p], m[p]);
+        load_four<AQSGD_F32, FULL>(v_at, i, count[p], v[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < kUpdatePieces; ++p) {
+        const int64_t i = first + 4 * kWave * p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            step_moments(a, k, g[p][e], m[p][e], v[p][e]);
+            w[p][e] = stepped_weight(a, k, w[p][e], m[p][e], sqrtf(v[p][e]));
+        }
+        if (t.master) store_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
+        store_four<DT, FULL>(t.param, i, count[p], w[p]);
+        store_four<AQSGD_F32, FULL>(t.state, i, count[p], m[p]);
+        store_four<AQSGD_F32, FULL>(v_at, i, count[p], v[p]);
+    }
+}
 
 // ---- the kernel ----------------------------------------------------------------------------------
 template <int DT, int GT, int BITS, int ROUND>
 __global__ __launch_bounds__(kWave * kUpdateWaves) void adamw_kernel(const UpdateTable table, const AdamwArgs a) {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     UpdateFactors k;
     k.scaled = a.scale != nullptr;
     k.scale = k.scaled ? *a.scale : 1.0f;
     if (!(fabsf(k.scale) < __builtin_inff())) return;                     // a step that is skipped
     const int which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(table.first[lane] <= blockIdx.x)) - 1);
     const UpdateTensor& t = table.tensor[which];
-    int64_t now = a.step_at ? *a.step_at : a.step;
-    if (now < 1) now = 1;
-    const double lr = a.lr_at ? static_cast<double>(*a.lr_at) : a.lr;
-    k.decay = static_cast<float>(1.0 - lr * t.weight_decay);
-    k.length = static_cast<float>(lr / (1.0 - power_of(a.beta1, now)));
-    k.correct = static_cast<float>(1.0 / sqrt(1.0 - power_of(a.beta2, now)));
-    const uint64_t key = a.seed + static_cast<uint64_t>(now);
-    const int64_t span = static_cast<int64_t>(blockIdx.x - table.first[which]) * (kUpdateWaves * kUpdateGroups);
-#pragma unroll
-    for (int q = 0; q < kUpdateGroups; ++q) {
-        const int64_t group = span + wave * kUpdateGroups + q, i = group * kStateGroup + lane * 4;
-        if (group * kStateGroup >= t.n) return;
-        const int64_t left = t.n - i;
-        const int count = left >= 4 ? 4 : left > 0 ? static_cast<int>(left) : 0;
-        float g[4], w[4], m[4], v[4], r[4];
-        load_four<GT>(t.grad, i, count, g);
-        if (t.master) load_four<AQSGD_F32>(t.master, i, count, w);
-        else load_four<DT>(t.param, i, count, w);
-        char* const m_at = t.state;
-        char* const r_at = t.state + whole64(BITS == 32 ? 4 * t.n : t.n);
-        float* const m_scales = reinterpret_cast<float*>(t.state + 2 * whole64(t.n));
-        float* const r_scales = m_scales + whole64(4 * state_groups(t.n)) / 4;
-        if constexpr (BITS == 32) {
-            load_four<AQSGD_F32>(m_at, i, count, m);
-            load_four<AQSGD_F32>(r_at, i, count, v);
-        } else {
-            uint32_t mc = 0, rc = 0;
-            if (count > 0) {
-                mc = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(m_at + i));
-                rc = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(r_at + i));
-            }
-            const float m_step = m_scales[group] / (kMTop * kMTop), r_step = r_scales[group] / (kRTop * kRTop);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float mk = static_cast<float>(static_cast<int8_t>(mc >> (8 * e))), rk = static_cast<float>((rc >> (8 * e)) & 0xffu);
-                m[e] = (mk * fabsf(mk)) * m_step;
-                const float root = (rk * rk) * r_step;
-                v[e] = root * root;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) step_element(a, k, g[e], w[e], m[e], v[e], r[e]);
-        if (t.master) store_four<AQSGD_F32>(t.master, i, count, w);
-        store_four<DT>(t.param, i, count, w);
-        if constexpr (BITS == 32) {
-            store_four<AQSGD_F32>(m_at, i, count, m);
-            store_four<AQSGD_F32>(r_at, i, count, v);
-        } else {
-            uint32_t m_top = 0, r_top = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (e >= count) m[e] = r[e] = 0.0f;
-                m_top = max(m_top, magnitude_of(m[e]));
-                r_top = max(r_top, magnitude_of(r[e]));
-            }
-            const HeldScale ms = held_scale(__float_as_uint(team_max<kWave>(__uint_as_float(m_top))), kMTop);
-            const HeldScale rs = held_scale(__float_as_uint(team_max<kWave>(__uint_as_float(r_top))), kRTop);
-            float zm[4], zr[4];
-            if constexpr (ROUND == AQSGD_ROUND_STOCHASTIC) {
-                const uint64_t block = static_cast<uint64_t>((t.group0 + group) * (kStateGroup / 4) + lane);
-                uint32_t words[4];
-                philox4x32_10(static_cast<uint32_t>(block), static_cast<uint32_t>(block >> 32), static_cast<uint32_t>(key),
-                              static_cast<uint32_t>(key >> 32), words);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    zm[e] = static_cast<float>((words[e] & 0xffffu) + 1u) * 0x1p-16f;
-                    zr[e] = static_cast<float>((words[e] >> 16) + 1u) * 0x1p-16f;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) zm[e] = zr[e] = 0.5f;
-            }
-            uint32_t mc = 0, rc = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float mk = held_code(fabsf(m[e]), ms, kMTop, 0.0f, zm[e]);
-                mc |= (static_cast<uint32_t>(static_cast<int32_t>(m[e] < 0.0f ? -mk : mk)) & 0xffu) << (8 * e);
-                rc |= static_cast<uint32_t>(held_code(r[e], rs, kRTop, 1.0f, zr[e])) << (8 * e);
-            }
-            if (count > 0) {
-                __builtin_nontemporal_store(mc, reinterpret_cast<uint32_t*>(m_at + i));
-                __builtin_nontemporal_store(rc, reinterpret_cast<uint32_t*>(r_at + i));
-            }
-            if (lane == 0) {
-                m_scales[group] = ms.scale;
-                r_scales[group] = rs.scale;
-            }
-        }
+    k.decay = t.decay;
+    k.length = a.length;
+    k.correct = a.correct;
+    uint64_t key = a.key;
+    if (a.lr_at || a.step_at) {                                           // some 150 instructions in binary64, a fifth of a wave's
+        const int64_t now = a.step_at ? max(*a.step_at, int64_t{1}) : a.step;
+        const double lr = a.lr_at ? static_cast<double>(*a.lr_at) : a.lr;
+        k.decay = decay_factor(lr, t.weight_decay);
+        k.length = length_factor(lr, a.beta1, now);
+        k.correct = correct_factor(a.beta2, now);
+        key = a.seed + static_cast<uint64_t>(now);
+    }
+    const int64_t begin = static_cast<int64_t>(blockIdx.x - table.first[which]) * kUpdateSpan + wave * (4 * kWave * kUpdatePieces);
+    const int64_t left = t.n - begin;                                     // for the wave, which takes 512 elements
+    if (left <= 0) return;
+    if constexpr (BITS == 32) {
+        if (left >= 4 * kWave * kUpdatePieces) adamw32_pieces<DT, GT, true>(t, a, k, begin + 4 * lane);
+        else adamw32_pieces<DT, GT, false>(t, a, k, begin + 4 * lane);
+    } else {
+        const int64_t group = begin / kStateGroup + lane / 32;
+        if (left >= 2 * kStateGroup) adamw8_group<DT, GT, ROUND, true>(t, a, k, key, group, lane & 31);
+        else if (group * kStateGroup < t.n) adamw8_group<DT, GT, ROUND, false>(t, a, k, key, group, lane & 31);
     }
 }
 

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kLanes) void grad_squares_kernel(const NormTable ta
     double sum = 0.0;
     for (int64_t i = begin + threadIdx.x * 4; i < end; i += kLanes * 4) {
         float f[4];
-        load_four<GT>(table.grad[which], i, end - i < 4 ? static_cast<int>(end - i) : 4, f);
+        load_four<GT, false>(table.grad[which], i, end - i < 4 ? static_cast<int>(end - i) : 4, f);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(f[e]), static_cast<double>(f[e]), sum);
     }

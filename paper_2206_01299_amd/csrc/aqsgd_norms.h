@@ -55,6 +55,7 @@ struct UpdateTensor {
     int64_t n;
     int64_t group0;                              // groups of the call's tensors in front of it
     double weight_decay;
+    float decay;                                 // 1 - lr * weight_decay
 };
 
 // A launch's tensors; first[i]: the first workgroup of tensor i, after the last one a number no workgroup has.
@@ -70,12 +71,14 @@ struct AdamwArgs {
     const int64_t* step_at;
     const float* scale;
     float beta1f, rest1, beta2f, rest2, eps;     // rest: 1 - beta
-    uint64_t seed;
+    float length, correct;                       // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    uint64_t seed, key;                          // key: seed + t
 };
 struct AdamwKind {
     int dtype, grad_dtype, state_bits, rounding;
 };
-// The binary64 power that both the host and the kernels take.
+// The factors of a step, formed in binary64 by the host and, where lr or the step are on the device, by the kernels: the same
+// operations, the same bits.
 __host__ __device__ inline double power_of(double base, int64_t n) {
     double p = 1.0;
     for (; n > 0; n >>= 1) {
@@ -84,6 +87,9 @@ __host__ __device__ inline double power_of(double base, int64_t n) {
     }
     return p;
 }
+__host__ __device__ inline float decay_factor(double lr, double weight_decay) { return static_cast<float>(1.0 - lr * weight_decay); }
+__host__ __device__ inline float length_factor(double lr, double beta1, int64_t step) { return static_cast<float>(lr / (1.0 - power_of(beta1, step))); }
+__host__ __device__ inline float correct_factor(double beta2, int64_t step) { return static_cast<float>(1.0 / sqrt(1.0 - power_of(beta2, step))); }
 int64_t adamw_workgroups(int64_t n);             // of a tensor
 hipError_t launch_adamw(const AdamwKind& kind, const UpdateTable& table, uint32_t blocks, const AdamwArgs& a, hipStream_t stream);
 

@@ -156,7 +156,10 @@ int aqsgd_adamw(const aqsgd_adamw_desc* d, const aqsgd_adamw_tensor* tensors, in
     a.beta1f = static_cast<float>(d->beta1); a.rest1 = static_cast<float>(1.0 - d->beta1);
     a.beta2f = static_cast<float>(d->beta2); a.rest2 = static_cast<float>(1.0 - d->beta2);
     a.eps = static_cast<float>(d->eps);
+    a.length = length_factor(d->lr, d->beta1, d->step);
+    a.correct = correct_factor(d->beta2, d->step);
     a.seed = d->rng_seed;
+    a.key = d->rng_seed + static_cast<uint64_t>(d->step);
     int32_t full = 0;                                       // tensors with elements: more than a table's take several launches
     for (int32_t i = 0; i < n_tensors; ++i) full += tensors[i].n > 0;
     std::optional<ProfileSpan> profile;
@@ -179,7 +182,7 @@ int aqsgd_adamw(const aqsgd_adamw_desc* d, const aqsgd_adamw_tensor* tensors, in
         if (held == kTableTensors || blocks + more > kMaxBlocks)
             if (const hipError_t err = send(); err != hipSuccess) return status(err);
         table.first[held] = static_cast<uint32_t>(blocks);
-        table.tensor[held] = {t.param, t.grad, static_cast<char*>(t.state), t.master, t.n, groups, t.weight_decay};
+        table.tensor[held] = {t.param, t.grad, static_cast<char*>(t.state), t.master, t.n, groups, t.weight_decay, decay_factor(d->lr, t.weight_decay)};
         ++held;
         blocks += more;
         groups += state_groups(t.n);
