@@ -178,7 +178,7 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
         }
     }
     const float m_step = divided_by<127 * 127>(*m_scale), r_step = divided_by<255 * 255>(*r_scale);
-    bool small = false;
+    uint32_t least = 0xffffffffu;                          // pattern of the smallest v that is not 0, less one
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
         mc[p] ^= 0x80808080u;                              // code + 128 as bytes
@@ -189,10 +189,10 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
             m[p][e] = (mk * fabsf(mk)) * m_step;
             v[p][e] = root * root;
             step_moments(a, k, g[p][e], m[p][e], v[p][e]);
-            small = small || __float_as_uint(v[p][e]) - 1u < 0x0f800000u - 1u;        // between 0 and 2^-96
+            least = min(least, __float_as_uint(v[p][e]) - 1u);
         }
     }
-    if (__any(small)) {
+    if (__any(least < 0x0f800000u - 1u)) {                 // 2^-96
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -211,7 +211,7 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
             w[p][e] = stepped_weight(a, k, w[p][e], m[p][e], r[p][e]);
             if (!FULL && e >= count[p]) m[p][e] = r[p][e] = 0.0f;
             m_top = max(m_top, __float_as_uint(m[p][e]) & 0x7fffffffu);
-            r_top = max(r_top, __float_as_uint(r[p][e]) & 0x7fffffffu);
+            r_top = max(r_top, __float_as_uint(r[p][e]));  // not below 0; a NaN of either sign lies above all numbers
         }
         const int64_t i = first + 128 * p;
         if (t.master) store_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
@@ -236,7 +236,7 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float mk = held_code<ROUND>(fabsf(m[p][e]), ms.inv, zm[e]);
-            const float rk = fmaxf(held_code<ROUND>(r[p][e], rs.inv, zr[e]), r[p][e] > 0.0f ? 1.0f : 0.0f);
+            const float rk = fmaxf(held_code<ROUND>(r[p][e], rs.inv, zr[e]), fminf(r[p][e] * 0x1p100f, 1.0f));
             mc[p] = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(mk, m[p][e]) + 128.0f, e, mc[p]);
             rc[p] = __builtin_amdgcn_cvt_pk_u8_f32(rk, e, rc[p]);
         }

@@ -7,37 +7,64 @@
 namespace aqsgd {
 namespace {
 
-constexpr int kLanes = 256;
+constexpr int kLanes = 256, kJoinLanes = 1024;
 
+template <int LANES>
 __device__ __forceinline__ double workgroup_sum(double v, double* part) {
     v = lanes_sum<kWave>(v);
     if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
-    return part[0] + part[1] + part[2] + part[3];
+    double sum = part[0];
+#pragma unroll
+    for (int w = 1; w < LANES / kWave; ++w) sum += part[w];
+    return sum;
 }
 
 template <int GT>
+__device__ __forceinline__ double added_squares(const u32x4_t& piece, double sum) {
+    float f[kPiece<GT>];
+    piece_values<GT>(piece, f);
+#pragma unroll
+    for (int e = 0; e < kPiece<GT>; ++e) sum = fma(static_cast<double>(f[e]), static_cast<double>(f[e]), sum);
+    return sum;
+}
+
+// Pieces of 16 bytes, kAhead of a lane's on their way at a time; spans are whole pieces, so that only the last one of a tensor
+// ends inside one.
+template <int GT>
 __global__ __launch_bounds__(kLanes) void grad_squares_kernel(const NormTable table, const int64_t span, double* partial) {
-    __shared__ double part[4];
+    constexpr int V = kPiece<GT>, kAhead = 4;
+    __shared__ double part[kLanes / kWave];
     const int which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(table.first[threadIdx.x & (kWave - 1)] <= blockIdx.x)) - 1);
     const int64_t n = table.n[which], begin = static_cast<int64_t>(blockIdx.x - table.first[which]) * span;
     const int64_t end = begin + span < n ? begin + span : n;
-    double sum = 0.0;
-    for (int64_t i = begin + threadIdx.x * 4; i < end; i += kLanes * 4) {
-        float f[4];
-        load_four<GT, false>(table.grad[which], i, end - i < 4 ? static_cast<int>(end - i) : 4, f);
+    const char* const grad = element_at<GT>(table.grad[which], 0);
+    // Past the caches: 123 M float16 41.2 us, with ordinary loads 47.2; float32 78.1 and 89.2.
+    const auto piece_at = [&](int64_t i) -> u32x4_t { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any_t*>(grad + i * ElemBytes<GT>::value)); };
+    double sum[2] = {};
+    int64_t i = begin + threadIdx.x * V;
+    for (; i + (kAhead - 1) * kLanes * V + V <= end; i += kAhead * kLanes * V) {
+        u32x4_t piece[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(f[e]), static_cast<double>(f[e]), sum);
+        for (int k = 0; k < kAhead; ++k) piece[k] = piece_at(i + k * kLanes * V);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) sum[k & 1] = added_squares<GT>(piece[k], sum[k & 1]);
     }
-    sum = workgroup_sum(sum, part);
-    if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+    for (; i + V <= end; i += kLanes * V) sum[0] = added_squares<GT>(piece_at(i), sum[0]);
+    for (; i < end; ++i) {                                   // one lane's, of the tensor's last piece
+        const double f = static_cast<double>(load_elem<GT>(grad, i));
+        sum[1] = fma(f, f, sum[1]);
+    }
+    const double all = workgroup_sum<kLanes>(sum[0] + sum[1], part);
+    if (threadIdx.x == 0) partial[blockIdx.x] = all;
 }
 
-__global__ __launch_bounds__(kLanes) void grad_norm_kernel(const double* partial, const int64_t count, const double max_norm, const float* loss_scale, float* result) {
-    __shared__ double part[4];
+__global__ __launch_bounds__(kJoinLanes) void grad_norm_kernel(const double* partial, const int64_t count, const double max_norm, const float* loss_scale, float* result) {
+    __shared__ double part[kJoinLanes / kWave];
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < count; i += kLanes) sum += partial[i];
-    sum = workgroup_sum(sum, part);
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < count; i += kJoinLanes) sum += partial[i];
+    sum = workgroup_sum<kJoinLanes>(sum, part);
     if (threadIdx.x != 0) return;
     const double inverse = loss_scale ? 1.0 / static_cast<double>(*loss_scale) : 1.0, norm = sqrt(sum) * inverse;
     const double clip = max_norm / norm;                    // 0 / 0, of no gradient at all: nothing to clip
@@ -57,7 +84,7 @@ hipError_t launch_grad_squares(int dtype, const NormTable& table, uint32_t block
 }
 
 hipError_t launch_grad_norm(const double* partial, int64_t count, double max_norm, const float* loss_scale, float* result, hipStream_t stream) {
-    return launch_kernel(grad_norm_kernel, dim3(1), dim3(kLanes), stream, partial, count, max_norm, loss_scale, result);
+    return launch_kernel(grad_norm_kernel, dim3(1), dim3(kJoinLanes), stream, partial, count, max_norm, loss_scale, result);
 }
 
 }  // namespace aqsgd
