@@ -175,14 +175,23 @@ struct TeamSpace {                       // of a workgroup that is one team
     uint32_t top[16];
 };
 
-__device__ __forceinline__ float inverse_deviation(double squares, int32_t cols, double eps) {
-    return static_cast<float>(1.0 / sqrt(squares / cols + eps));
+// 1 / sqrt of the variance in binary64, rounded once: the hardware's (2^-24 of it off at most) and two steps of Newton's, ten
+// operations instead of some sixty for a root and a quotient (4096 x 1600 float16 with residual and codes 12.8 -> 12.2 us).
+__device__ __forceinline__ float inverse_deviation(double squares, double each, double eps) {
+    const double v = squares * each + eps;
+    double y = __builtin_amdgcn_rsq(v);
+    if (v > 0.0 && v < __builtin_inf()) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-v * y, y, 1.0), y);
+    }
+    return static_cast<float>(y);
 }
 
 // ---- forward -----------------------------------------------------------------------------------
 template <int DT, int TEAM, int CPL, bool RAGGED>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(const LayernormArgs a) {
     constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM, V = kPiece<DT>;
+    static_assert(TEAM * V >= kCodePad, "the lanes that write a row's codes write the zeros behind them");
     __shared__ TeamSpace space;
     const int lane = threadIdx.x % TEAM, team = team_number<TEAM>();
     const auto column = [&](int i) { return (i * TEAM + lane) * V; };
@@ -220,7 +229,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
             for (int e = 0; e < V; ++e) total += static_cast<double>(f[e]);
         });
         if (a.sum && here) each_piece<CPL>([&](auto i, auto last) { store_piece_of<DT, last, RAGGED>(a.sum, row * a.cols, column(i), a.cols, held[i]); });
-        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) / a.cols);
+        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) * a.each);
         double squares = 0.0;
         each_piece<CPL>([&](auto i, auto last) {
             if (last && column(i) >= a.cols) return;
@@ -232,7 +241,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
                 squares = fma(d, d, squares);
             }
         });
-        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.cols, a.eps);
+        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.each, a.eps);
         if (a.mean && here && lane == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -318,12 +327,12 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_any_kernel(
             if (a.sum) store_elem<DT>(a.sum, at + c, f);
             total += static_cast<double>(f);
         }
-        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) / a.cols);
+        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) * a.each);
         for (int32_t c = lane; c < cols; c += TEAM) {
             const double d = static_cast<double>(again(c) - mean);
             squares = fma(d, d, squares);
         }
-        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.cols, a.eps);
+        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.each, a.eps);
         if (a.mean && here && lane == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -677,7 +686,13 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
 #define AQSGD_NORM(TEAM, CPL) \
     return ragged ? go(layernorm_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_kernel<DT, TEAM, CPL, false>, TEAM)
     if (a.cols < kPiece<DT>) return go(layernorm_any_kernel<DT, 64>, 64);
+    // Several rows to a wave where they are narrow: 32768 rows of 200 float16 8.6 us, with a wave to a row 18.6; of 40 3.6 and, with 16
+    // lanes, 5.7.
+    if constexpr (DT != AQSGD_F32) {
+        if (pieces <= 8) AQSGD_NORM(8, 1);
+    }
     if (pieces <= 16) AQSGD_NORM(16, 1);
+    if (pieces <= 32) AQSGD_NORM(32, 1);
     if (pieces <= 64) AQSGD_NORM(64, 1);
     if (pieces <= 128) AQSGD_NORM(64, 2);
     if (pieces <= 256 && few) AQSGD_NORM(256, 1);

@@ -20,7 +20,7 @@ struct LayernormArgs {
     float* scales;
     int64_t rows, ld;
     int64_t code_stride;                 // bytes
-    double eps;
+    double eps, each;                    // each: 1 / cols
     int32_t cols;
 };
 hipError_t launch_layernorm(int dtype, const LayernormArgs& a, hipStream_t stream);

@@ -103,6 +103,7 @@ int aqsgd_layernorm(const aqsgd_layernorm_desc* d, const void* x, const void* re
     a.sum = sum; a.y = y; a.mean = mean; a.rstd = rstd; a.codes = row_codes; a.scales = row_scales;
     a.rows = d->rows; a.ld = d->ld; a.code_stride = code_stride(d->cols);
     a.eps = d->eps;
+    a.each = 1.0 / static_cast<double>(d->cols);
     a.cols = static_cast<int32_t>(d->cols);
     return status(launch_layernorm(d->dtype, a, static_cast<hipStream_t>(stream)));
 }
