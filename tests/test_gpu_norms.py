@@ -286,6 +286,34 @@ def test_layernorm_grad_is_the_differences_of_the_norm():
             assert abs((more - less) / (2 * h) - got[c].double()) < rows * allow
 
 
+# ---- every kernel ------------------------------------------------------------------------------
+# Sizes at which the choice takes each of the kernels: pieces of 16 bytes a row, and rows; with whole pieces and with a
+# last one that is not.
+
+PIECES = {"f32": 4, "f16": 8, "bf16": 8}
+NORMS = [(7, 5), (16, 40), (30, 9), (64, 7), (100, 9), (190, 600), (250, 600), (200, 5), (500, 3), (700, 3), (1000, 3), (2000, 2), (2900, 2), (4000, 2)]
+GRADS = [(10, 1100), (30, 1100), (64, 1100), (100, 1100), (200, 1100), (400, 1100), (1000, 1100), (60, 20), (128, 20), (150, 20), (250, 20), (500, 5),
+         (900, 5), (1500, 5), (2048, 4), (4000, 3)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("pieces,rows", NORMS)
+def test_norms_by_every_kernel(dtype, pieces, rows):
+    for less in (0, 1, PIECES[dtype] // 2):
+        cols = pieces * PIECES[dtype] - less
+        x, res, w, b = inputs(rows, cols)
+        run_norm(x, dtype, residual=res, weight=w, bias=b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("pieces,rows", GRADS)
+def test_gradients_by_every_kernel(dtype, pieces, rows):
+    for less in (0, 1, PIECES[dtype] // 2):
+        cols = pieces * PIECES[dtype] - less
+        run_grad(rows, cols, dtype, add=less > 0, accumulate=less != 1)
+        run_grad(rows, cols, dtype, dw=False, db=False, add=True)
+
+
 # ---- streams, graphs, threads, both ways of the binding ----------------------------------------
 
 def block(x, res, dy, w, b, dtype, buf=None, stream=None):

@@ -12,7 +12,7 @@ import norms_reference as N
 import products8_reference as R
 from paper_2206_01299_amd import binding as B
 from test_gpu_norms import typed
-from test_gpu_products8 import DTYPES, MARK, Framed, stored
+from test_gpu_products8 import DTYPES, Framed, stage_inputs, stage_step, stored
 
 TYPES = [("f32", "f32"), ("f16", "f32"), ("f16", "f16"), ("bf16", "f32"), ("bf16", "bf16")]
 KINDS = [(32, 0), (8, 0), (8, 1)]                                               # state bits, rounding
@@ -397,3 +397,98 @@ def test_the_time_of_a_call_of_several_launches():
         call()
         torch.cuda.synchronize()
         assert 0.0005 < start.elapsed_time(stop) < 5.0
+
+
+# ---- together: a stage's step from its norm to its weights -----------------------------------------
+
+class Stage:
+    """A block behind a norm over the residual stream: float16 weights with binary32 copies, states in 8 bits, trained on
+    messages of the next stage."""
+
+    def __init__(self, m, k, f, seed=0):
+        self.m, self.k, self.f = m, k, f
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        self.masters = [1 + 0.1 * n(k), 0.1 * n(k), n(2 * f, k) / k ** 0.5, n(k, f) / f ** 0.5]
+        self.weights = [w.half() for w in self.masters]
+        self.grads = [torch.zeros_like(w) for w in self.masters]
+        self.desc = B.make_adamw_desc(dtype="f16", grad_dtype="f32", state_bits=8, rounding=B.STOCHASTIC, rng_seed=5, lr=1e-2)
+        self.states = [torch.zeros(B.adamw_state_bytes(self.desc, w.numel()), dtype=torch.uint8, device="cuda") for w in self.weights]
+        self.list = B.adamw_tensors(self.desc, params=self.weights, grads=self.grads, states=self.states, masters=self.masters, weight_decays=[0, 0, 0.1, 0.1])
+        self.at, self.result = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.empty(2, device="cuda")
+        self.ws = torch.empty(B.grad_norm_workspace_bytes(self.list), dtype=torch.uint8, device="cuda")
+        self.inner, self.buf = {}, {}
+
+    def step(self, x, res, message, scales):
+        d = B.make_layernorm_desc(rows=self.m, cols=self.k, dtype="f16")
+        b, (lw, lb, w1, w2) = self.buf, self.weights
+        for name, shape, t in (("sum", (self.m, self.k), torch.float16), ("y", (self.m, self.k), torch.float16), ("mean", (self.m,), torch.float32),
+                               ("rstd", (self.m,), torch.float32), ("row_codes", (self.m, R.stride(self.k)), torch.int8),
+                               ("row_scales", (self.m,), torch.float32), ("dx", (self.m, self.k), torch.float16)):
+            if name not in b:
+                b[name] = torch.zeros(shape, dtype=t, device="cuda")
+        B.layernorm(d, x, residual=res, weight=lw, bias=lb, **{n: b[n] for n in ("sum", "y", "mean", "rstd", "row_codes", "row_scales")})
+        out = stage_step(b["y"], w1, w2, message, scales, "f16", self.inner)
+        B.layernorm_grad(d, out["dx"], b["sum"], b["mean"], b["rstd"], b["dx"], weight=lw, add=out["dx"], dweight=self.grads[0], dbias=self.grads[1])
+        self.grads[2].copy_(out["dw1"])
+        self.grads[3].copy_(out["dw2"])
+        self.at.add_(1)
+        B.grad_norm(self.list, self.result, max_norm=1.0, workspace=self.ws)
+        B.adamw(self.desc, self.list, step=self.at, scale=self.result[1:])
+        return {**out, **b, "block_dx": out["dx"]}
+
+
+def test_a_stages_step_with_its_norm_and_its_update():
+    """Eager steps against the plain ones: the norm's codes are those that the block quantises its input to, its gradient is that
+    of the binary32 values, weights and states follow the plain update bit for bit; and a captured step, replayed with new inputs, goes
+    the same way."""
+    m, k, f = 300, 160, 224
+    eager, captured = Stage(m, k, f), Stage(m, k, f)
+    rng = np.random.default_rng(0)
+
+    def draw(seed):
+        x, _, _, message, scales = stage_inputs(m, k, f, "f16", seed)
+        return x, stored(rng.standard_normal((m, k)), "f16")[0], message, scales
+
+    data = [draw(i) for i in range(4)]
+    held = [t.clone() for t in data[0]]
+    captured.step(*held)                                                       # makes the buffers
+    torch.cuda.synchronize()
+    for a, b in zip(captured.masters + captured.weights + captured.states, eager.masters + eager.weights + eager.states):
+        a.copy_(b)
+    captured.at.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.step(*held)
+    for a, b in zip(captured.masters + captured.weights + captured.states, eager.masters + eager.weights + eager.states):
+        a.copy_(b)
+    captured.at.zero_()
+    plain = [N.State(w.numel(), 8) for w in eager.masters]
+    masters = [w.cpu().numpy().reshape(-1) for w in eager.masters]
+    for step, inputs in enumerate(data, 1):
+        out = eager.step(*inputs)
+        torch.cuda.synchronize()
+        codes, scales = R.quantise(out["y"].float().cpu().numpy())
+        assert np.array_equal(out["row_codes"].cpu().numpy(), codes) and np.array_equal(out["row_scales"].cpu().numpy(), scales)
+        dy = out["block_dx"].float().cpu().numpy()
+        want = N.norm_grad(dy, out["sum"].float().cpu().numpy(), out["mean"].cpu().numpy(), out["rstd"].cpu().numpy(), typed("f16")(masters[0]), dy)
+        for got, (w, off), dt in zip((out["dx"], eager.grads[0], eager.grads[1]), want, ("f16", "f32", "f32")):
+            R.close(got.double().cpu().numpy(), w, off, dt, f"step {step}")
+        norm = math.sqrt(sum((g.double() ** 2).sum().item() for g in eager.grads))
+        factor = eager.result[1].item()
+        assert abs(eager.result[0].item() - norm) <= 2 * N.U * norm and abs(factor - min(1.0, 1.0 / norm)) <= 2 * N.U * factor
+        first = 0
+        for i, s in enumerate(plain):
+            masters[i] = N.adamw(masters[i], eager.grads[i].cpu().numpy().reshape(-1), s, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, step=step,
+                                 decay=[0, 0, 0.1, 0.1][i], scale=np.float32(factor), seed=5, first=first)
+            first += N.up(s.n, 256)
+            assert np.array_equal(eager.masters[i].cpu().numpy().reshape(-1), masters[i]), f"step {step}: weight {i}"
+            for a, b in zip(B.adamw_state_views(eager.desc, eager.states[i], s.n), s.parts()):
+                assert np.array_equal(a.cpu().numpy(), b), f"step {step}: state {i}"
+        for a, b in zip(held, inputs):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(captured.masters + captured.weights + captured.states, eager.masters + eager.weights + eager.states):
+            assert torch.equal(a, b), f"replay {step}"
