@@ -33,19 +33,38 @@ __device__ __forceinline__ u32x4_t values_piece(const float (&f)[kPiece<DT>]) {
 }
 
 // The piece from column c on of a row that starts at element `at`.  Rows have at least a piece's elements.  LAST: a piece
-// that may lie across the row's end (RAGGED) or behind it; such a lane reads the row's last elements instead,
-// and whole_piece moves those it has down in registers; what does not exist is 0.
+// that may lie across the row's end (RAGGED) or behind it; such a lane reads the row's last elements instead.
 template <int DT, bool LAST>
 __device__ __forceinline__ u32x4_t load_piece(const void* base, int64_t at, int32_t c, int32_t cols) {
     const char* row = element_at<DT>(base, at);
     return *reinterpret_cast<const u32x4_any_t*>(row + (LAST ? min(c, cols - kPiece<DT>) : c) * ElemBytes<DT>::value);
 }
 
+// What was so read, each element at its column.  Where there is no column: some other element of the row.
+template <int DT, bool LAST, bool RAGGED>
+__device__ __forceinline__ u32x4_t placed_piece(u32x4_t r, int32_t c, int32_t cols) {
+    if constexpr (LAST && RAGGED) {
+        const int down = c + kPiece<DT> - cols;          // columns that do not exist
+        if (down > 0 && down < kPiece<DT>) {
+            if constexpr (DT == AQSGD_F32) {
+                if (down & 2) r = u32x4_t{r[2], r[3], r[0], r[1]};
+                if (down & 1) r = u32x4_t{r[1], r[2], r[3], r[0]};
+            } else {
+                if (down & 4) r = u32x4_t{r[2], r[3], r[0], r[1]};
+                if (down & 2) r = u32x4_t{r[1], r[2], r[3], r[0]};
+                if (down & 1) r = u32x4_t{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16, r[3] >> 16 | r[0] << 16};
+            }
+        }
+    }
+    return r;
+}
+
+// The same with 0 where there is no column.
 template <int DT, bool LAST, bool RAGGED>
 __device__ __forceinline__ u32x4_t whole_piece(u32x4_t r, int32_t c, int32_t cols) {
     if constexpr (!LAST) return r;
     if constexpr (RAGGED) {
-        const int down = c + kPiece<DT> - cols;          // elements that do not exist
+        const int down = c + kPiece<DT> - cols;
         if (down > 0 && down < kPiece<DT>) {
             if constexpr (DT == AQSGD_F32) {
                 if (down & 2) r = u32x4_t{r[2], r[3], 0, 0};
@@ -456,10 +475,10 @@ __global__ __launch_bounds__(kGradLanes) void layernorm_grad_kernel(const Layern
         const bool here = first + team < a.rows, more = first + stride < a.rows;
         const int64_t row = row_of(first);
         if (more) next.ask(a, row_of(first + stride), lane);
-        // Where there is no column or no row dy is 0, and with it whatever is summed.  x is then one of the row's, or the last
-        // row's: finite, unless that row's own sums are NaN anyway.
+        // Where there is no column or no row dy is 0, and with it whatever is summed: xh is then that of another of the row's
+        // elements, or of the last row's, so it is finite unless that row's own sums are NaN anyway.
         float along = 0.0f, across = 0.0f, g[V], xh[V], gw[V];
-        piece_values<DT>(whole_piece<DT, true, RAGGED>(now.x[0], c, a.cols), xh);
+        piece_values<DT>(placed_piece<DT, true, RAGGED>(now.x[0], c, a.cols), xh);
         piece_values<DT>(here ? whole_piece<DT, true, RAGGED>(now.dy[0], c, a.cols) : u32x4_t{0, 0, 0, 0}, g);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -530,7 +549,7 @@ __device__ __forceinline__ void columns_of_few(const LayernormGradArgs& a, int64
         for (int i = 0; i < kAhead; ++i) {
             if (first + i * kFewSlots >= a.rows) break;
             float xf[V], g[V];
-            piece_values<DT>(whole_piece<DT, true, RAGGED>(x[i], c, a.cols), xf);
+            piece_values<DT>(placed_piece<DT, true, RAGGED>(x[i], c, a.cols), xf);
             piece_values<DT>(whole_piece<DT, true, RAGGED>(dy[i], c, a.cols), g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -583,7 +602,7 @@ __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const Lay
         if (a.weight) each_piece<CPL>([&](auto i, auto last) { w[i] = load_piece<DT, last>(a.weight, 0, column(i), a.cols); });
         float along = 0.0f, across = 0.0f, xh[CPL][V], gw[CPL][V];
         each_piece<CPL>([&](auto i, auto last) {
-            piece_values<DT>(whole_piece<DT, last, RAGGED>(now.x[i], column(i), a.cols), xh[i]);
+            piece_values<DT>(placed_piece<DT, last, RAGGED>(now.x[i], column(i), a.cols), xh[i]);
             piece_values<DT>(whole_piece<DT, last, RAGGED>(now.dy[i], column(i), a.cols), gw[i]);
             if (a.weight) {
                 float wf[V];

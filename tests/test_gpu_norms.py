@@ -257,6 +257,28 @@ def test_layernorm_grad_keeps_a_bad_row_to_itself(dtype, cols):
         assert torch.isnan(b[7]) and torch.equal(a[others], b[others])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(20, 9), (20, 33), (20, 1537), (1100, 9), (1100, 33), (1100, 1537), (1100, 40), (9, 5000), (5, 40000), (5, 70001)])
+def test_layernorm_grad_of_constant_rows_of_large_values(dtype, rows, cols):
+    """Every deviation is 0, and so is xh; what is formed where a row has no column must not overflow into its sums."""
+    x = torch.full((rows, cols), 2.0 ** 127, device="cuda").to(B.DTYPE_NAME[dtype])
+    dy = torch.ones((rows, cols), device="cuda").to(B.DTYPE_NAME[dtype])
+    dy[:, 0] = 2.0
+    d = B.make_layernorm_desc(rows=rows, cols=cols, dtype=dtype)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    y = torch.empty_like(x)
+    B.layernorm(d, x, y=y, mean=mean, rstd=rstd)
+    assert (mean == 2.0 ** 127).all() and not y.any()
+    dx, dw, db = torch.empty_like(dy), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    for sums in (True, False):
+        B.layernorm_grad(d, dy, x, mean, rstd, dx, dweight=dw if sums else None, dbias=db if sums else None)
+        want = rstd.double()[:, None] * (dy.double() - dy.double().mean(dim=1, keepdim=True))
+        # a mean of ones and a two: exact but for its product with 1 / cols, two half steps of about 1, times rstd
+        allow = 4 * N.U * rstd.double()[:, None] + 1.01 * R.HALF_STEP[dtype] * want.abs()
+        assert ((dx.double() - want).abs() <= allow).all()
+    assert not dw.any() and (db[1:] == rows).all() and db[0] == 2 * rows
+
+
 def test_layernorm_grad_is_the_differences_of_the_norm():
     """In float32: each loss is a sum of 10 x 24 results, differences over 2^-6 steps."""
     rows, cols, h = 10, 24, 2.0 ** -6
