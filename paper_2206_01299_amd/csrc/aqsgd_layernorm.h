@@ -210,7 +210,7 @@ __device__ __forceinline__ float inverse_deviation(double squares, double each, 
 template <int DT, int TEAM, int CPL, bool RAGGED>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(const LayernormArgs a) {
     constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM, V = kPiece<DT>;
-    static_assert(TEAM * V >= kCodePad, "the lanes that write a row's codes write the zeros behind them");
+    static_assert(TEAM * V % kCodePad == 0, "the lanes that write a row's codes write the zeros behind them");
     __shared__ TeamSpace space;
     const int lane = threadIdx.x % TEAM, team = team_number<TEAM>();
     const auto column = [&](int i) { return (i * TEAM + lane) * V; };
@@ -705,10 +705,23 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
 #define AQSGD_NORM(TEAM, CPL) \
     return ragged ? go(layernorm_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_kernel<DT, TEAM, CPL, false>, TEAM)
     if (a.cols < kPiece<DT>) return go(layernorm_any_kernel<DT, 64>, 64);
-    // Several rows to a wave where they are narrow: 32768 rows of 200 float16 8.6 us, with a wave to a row 18.6; of 40 3.6 and, with 16
-    // lanes, 5.7.
-    if constexpr (DT != AQSGD_F32) {
-        if (pieces <= 8) AQSGD_NORM(8, 1);
+    // Many narrow rows: few lanes with several pieces each, so that a wave's sums and statistics serve several rows.  32768 rows (us; with a
+    // piece or two a lane in brackets): 130 float16 6.9 (10.7), 300 bfloat16 11.0 (17.7), 768 float16 17.8 (23.2), 129 float32 9.0 (13.9);
+    // 4096 rows: 3.2 (3.6), 3.5 (4.5), 4.1 (4.7), 2.9 (3.9); 1024 rows: 3.1 (3.1), 3.1 (3.1), 3.1 (2.9), 2.7 (2.9).
+    if (a.rows >= 4096) {
+        if constexpr (DT != AQSGD_F32) {
+            if (pieces <= 8) AQSGD_NORM(8, 1);
+            if (pieces <= 16) AQSGD_NORM(8, 2);
+            if (pieces <= 24) AQSGD_NORM(8, 3);
+            if (pieces <= 32) AQSGD_NORM(8, 4);
+        } else {
+            if (pieces <= 16) AQSGD_NORM(16, 1);
+            if (pieces <= 32) AQSGD_NORM(16, 2);
+        }
+        if (pieces <= 48) AQSGD_NORM(16, 3);
+        if (pieces <= 64) AQSGD_NORM(16, 4);
+        if (pieces <= 96) AQSGD_NORM(32, 3);
+        if (pieces <= 128) AQSGD_NORM(32, 4);
     }
     if (pieces <= 16) AQSGD_NORM(16, 1);
     if (pieces <= 32) AQSGD_NORM(32, 1);
