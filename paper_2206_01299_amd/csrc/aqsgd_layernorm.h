@@ -389,6 +389,7 @@ enum GradWay { kGradBlocks, kGradColumns, kGradAny };
 constexpr int kWideTeam = 1024;
 constexpr int kGradLanes = 1024;          // of a workgroup that takes many rows
 constexpr int64_t kFewRows = 1024;
+constexpr int kGradBlocksMost = 256;      // workgroups that take many rows: one to a CU
 
 // The workspace of the first way: sums of blocks of rows, for the weight [blocks, cols] and for the bias [blocks, cols].
 struct GradPlan {
@@ -410,7 +411,7 @@ inline GradPlan grad_plan(int64_t rows, int64_t cols, bool sums) {
     p.team = 16;
     while (p.team < pieces) p.team *= 2;
     const int64_t teams = kGradLanes / p.team, want = (rows + teams - 1) / teams;
-    p.blocks = want < 256 ? want : 256;
+    p.blocks = want < kGradBlocksMost ? want : kGradBlocksMost;
     return p;
 }
 

@@ -15,33 +15,37 @@ int64_t layernorm_grad_workspace_bytes(int dtype, int64_t rows, int64_t cols) {
     return 2 * p.blocks * cols * 4;
 }
 
-// Joins the blocks' sums of 32 columns: 32 lanes to a column, each every 32nd block, all asked for at once.
+// Joins the blocks' sums of 16 columns: 64 lanes to a column, each every 64th block, all asked for at once.  A row of sixteen lanes
+// is a row of columns, so that a wave's four meet in registers and the sixteen waves in LDS.  It is a launch and one chain of latencies:
+// the gradient of 4096 x 1600 float16 takes 16.6 us with it, 17.7 with 32 columns whose 32 lanes' sums met one after the other in LDS.
 // blockIdx.y: weight, bias.
-constexpr int kJoinCols = 32, kJoinSlots = 32;
+constexpr int kJoinCols = 16, kJoinSlots = 64, kJoinWaves = kJoinCols * kJoinSlots / kWave;
 
 static __global__ __launch_bounds__(kJoinCols * kJoinSlots) void layernorm_join_kernel(const LayernormGradArgs a, const int64_t blocks) {
-    __shared__ double part[kJoinSlots][kJoinCols];
+    __shared__ double part[kJoinWaves][kJoinCols];
     float* out = blockIdx.y == 0 ? a.dweight : a.dbias;
     if (!out) return;
     const float* from = a.workspace + blockIdx.y * blocks * a.cols;
     const int lane = threadIdx.x % kJoinCols, slot = threadIdx.x / kJoinCols;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + lane;
-    float v[256 / kJoinSlots];
+    float v[kGradBlocksMost / kJoinSlots];
 #pragma unroll
-    for (int i = 0; i < 256 / kJoinSlots; ++i) {
+    for (int i = 0; i < kGradBlocksMost / kJoinSlots; ++i) {
         const int64_t b = slot + i * kJoinSlots;
         v[i] = b < blocks && c < a.cols ? from[b * a.cols + c] : 0.0f;
     }
-    const float before = slot == 0 && a.accumulate && c < a.cols ? out[c] : 0.0f;
+    const float before = threadIdx.x < kJoinCols && a.accumulate && c < a.cols ? out[c] : 0.0f;
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 256 / kJoinSlots; ++i) s += static_cast<double>(v[i]);
-    part[slot][lane] = s;
+    for (int i = 0; i < kGradBlocksMost / kJoinSlots; ++i) s += static_cast<double>(v[i]);
+    s = halves_sum<32>(halves_sum<16>(s));
+    if ((threadIdx.x & (kWave - 1)) < kJoinCols) part[threadIdx.x / kWave][lane] = s;
     __syncthreads();
-    if (slot != 0 || c >= a.cols) return;
+    if (threadIdx.x >= kJoinCols || c >= a.cols) return;
+    double sum = 0.0;
 #pragma unroll
-    for (int i = 1; i < kJoinSlots; ++i) s += part[i][lane];
-    out[c] = a.accumulate ? before + static_cast<float>(s) : static_cast<float>(s);
+    for (int i = 0; i < kJoinWaves; ++i) sum += part[i][lane];
+    out[c] = a.accumulate ? before + static_cast<float>(sum) : static_cast<float>(sum);
 }
 
 hipError_t launch_layernorm_join(const LayernormGradArgs& a, int64_t blocks, hipStream_t stream) {
