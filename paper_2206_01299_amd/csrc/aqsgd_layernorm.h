@@ -206,6 +206,24 @@ __device__ __forceinline__ float inverse_deviation(double squares, double each, 
     return static_cast<float>(y);
 }
 
+// The codes of a piece of y.
+template <int DT>
+__device__ __forceinline__ void store_codes(int8_t* to, const u32x4_t& y, float inv) {
+    constexpr int V = kPiece<DT>;
+    float f[V];
+    piece_values<DT>(y, f);
+    uint32_t k[V / 4];
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+        int32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = code_of<AQSGD_ROUND_NEAREST>(f[4 * q + e], inv, 0.5f);
+        k[q] = pack_codes(c[0], c[1], c[2], c[3]);
+    }
+    if constexpr (V == 8) *reinterpret_cast<u32x2_t*>(to) = u32x2_t{k[0], k[1]};
+    else *reinterpret_cast<uint32_t*>(to) = k[0];
+}
+
 // ---- forward -----------------------------------------------------------------------------------
 template <int DT, int TEAM, int CPL, bool RAGGED>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(const LayernormArgs a) {
@@ -302,19 +320,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
                 if (lane == 0) a.scales[row] = s.scale;
                 int8_t* const to = a.codes + row * a.code_stride;
                 each_piece<CPL>([&](auto i, auto last) {
-                    if (last && column(i) >= a.code_stride) return;
-                    float f[V];
-                    piece_values<DT>(held[i], f);
-                    uint32_t k[V / 4];
-#pragma unroll
-                    for (int q = 0; q < V / 4; ++q) {
-                        int32_t c[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[e] = code_of<AQSGD_ROUND_NEAREST>(f[4 * q + e], s.inv, 0.5f);
-                        k[q] = pack_codes(c[0], c[1], c[2], c[3]);
-                    }
-                    if constexpr (V == 8) *reinterpret_cast<u32x2_t*>(to + column(i)) = u32x2_t{k[0], k[1]};
-                    else *reinterpret_cast<uint32_t*>(to + column(i)) = k[0];
+                    if (!last || column(i) < a.code_stride) store_codes<DT>(to + column(i), held[i], s.inv);
                 });
             }
         }
@@ -322,71 +328,136 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
     }
 }
 
-// Rows of any width, narrower than a piece or wider than a workgroup holds: read element by element, once for each sum
-// and once more for the result.
-template <int DT, int TEAM>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_any_kernel(const LayernormArgs a) {
-    constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM;
+// Rows wider than a workgroup holds in registers: read again for each sum and for the result, from the caches as far as those go.
+// A lane always comes back to its own columns, so that sum and y may lie where x or the residual do.
+constexpr int kWideLanes = 1024;
+
+template <int DT>
+__global__ __launch_bounds__(kWideLanes) void layernorm_wide_kernel(const LayernormArgs a) {
+    constexpr int V = kPiece<DT>;
     __shared__ TeamSpace space;
-    const int lane = threadIdx.x % TEAM;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows) {
-        const int64_t row = first + threadIdx.x / TEAM;
-        const bool here = row < a.rows;
+    const int32_t begin = threadIdx.x * V, step = kWideLanes * V;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t at = row * a.cols;
-        const int32_t cols = here ? a.cols : 0;
-        const auto value = [&](int32_t c) {              // as it is stored, for `sum` may be x or the residual
-            float f = load_elem<DT>(a.x, row * a.ld + c);
-            if (a.residual) f = rounded_to<DT>(f + load_elem<DT>(a.residual, at + c));
-            return f;
+        const auto piece = [&](const void* base, int64_t from, int32_t c) { return whole_piece<DT, true, true>(load_piece<DT, true>(base, from, c, a.cols), c, a.cols); };
+        const auto values = [&](int32_t c, float (&f)[V]) {              // as they are stored
+            piece_values<DT>(piece(a.x, row * a.ld, c), f);
+            if (!a.residual) return;
+            float r[V];
+            piece_values<DT>(piece(a.residual, at, c), r);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] += r[e];
+            piece_values<DT>(values_piece<DT>(f), f);
         };
-        const auto again = [&](int32_t c) { return a.sum ? load_elem<DT>(a.sum, at + c) : value(c); };
+        const auto again = [&](int32_t c, float (&f)[V]) {
+            if (a.sum) piece_values<DT>(piece(a.sum, at, c), f);
+            else values(c, f);
+        };
         double total = 0.0, squares = 0.0;
-        for (int32_t c = lane; c < cols; c += TEAM) {
-            const float f = value(c);
-            if (a.sum) store_elem<DT>(a.sum, at + c, f);
-            total += static_cast<double>(f);
+        for (int32_t c = begin; c < a.cols; c += step) {
+            float f[V];
+            values(c, f);
+            if (a.sum) store_piece_of<DT, true, true>(a.sum, at, c, a.cols, values_piece<DT>(f));
+#pragma unroll
+            for (int e = 0; e < V; ++e) total += static_cast<double>(f[e]);
         }
-        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) * a.each);
-        for (int32_t c = lane; c < cols; c += TEAM) {
-            const double d = static_cast<double>(again(c) - mean);
-            squares = fma(d, d, squares);
+        const float mean = static_cast<float>(team_sum<kWideLanes>(total, space.first) * a.each);
+        for (int32_t c = begin; c < a.cols; c += step) {
+            float f[V];
+            again(c, f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const double d = static_cast<double>(c + e < a.cols ? f[e] - mean : 0.0f);
+                squares = fma(d, d, squares);
+            }
         }
-        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.each, a.eps);
-        if (a.mean && here && lane == 0) {
+        const float rstd = inverse_deviation(team_sum<kWideLanes>(squares, space.second), a.each, a.eps);
+        if (a.mean && threadIdx.x == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
         }
         const auto result = [&](int32_t c) {
-            float y = (again(c) - mean) * rstd;
-            if (a.weight) y = y * load_elem<DT>(a.weight, c);
-            if (a.bias) y = y + load_elem<DT>(a.bias, c);
-            return rounded_to<DT>(y);
+            float f[V], more[V];
+            again(c, f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = (f[e] - mean) * rstd;
+            if (a.weight) {
+                piece_values<DT>(piece(a.weight, 0, c), more);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = f[e] * more[e];
+            }
+            if (a.bias) {
+                piece_values<DT>(piece(a.bias, 0, c), more);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = f[e] + more[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = c + e < a.cols ? f[e] : 0.0f;
+            return values_piece<DT>(f);
         };
-        uint32_t top = 0;
-        if (a.codes)                                      // before y is stored: it may be what `again` reads
-            for (int32_t c = lane; c < cols; c += TEAM) top = max(top, magnitude_bits(result(c)));
         CodeScale s = {};
-        if (a.codes) s = code_scale(team_top<TEAM>(top, space.top));
-        if (a.codes && here && lane == 0) a.scales[row] = s.scale;
+        if (a.codes) {                                    // before y is stored: it may be what `again` reads
+            uint32_t top = 0;
+            for (int32_t c = begin; c < a.cols; c += step) {
+                float f[V];
+                piece_values<DT>(result(c), f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) top = max(top, magnitude_bits(f[e]));
+            }
+            s = code_scale(team_top<kWideLanes>(top, space.top));
+            if (threadIdx.x == 0) a.scales[row] = s.scale;
+        }
+        const int32_t end = a.codes ? static_cast<int32_t>(a.code_stride) : a.cols;
         if (a.codes || a.y) {
-            const int64_t end = !here ? 0 : a.codes ? a.code_stride : a.cols;
-            for (int64_t c = lane; c < end; c += TEAM) {
-                const float y = c < a.cols ? result(static_cast<int32_t>(c)) : 0.0f;
-                if (a.codes) a.codes[row * a.code_stride + c] = static_cast<int8_t>(code_of<AQSGD_ROUND_NEAREST>(y, s.inv, 0.5f));
-                if (a.y && c < a.cols) store_elem<DT>(a.y, at + c, y);
+            for (int32_t c = begin; c < end; c += step) {
+                const u32x4_t y = c < a.cols ? result(c) : u32x4_t{0, 0, 0, 0};
+                if (a.codes) store_codes<DT>(a.codes + row * a.code_stride + c, y, s.inv);
+                if (a.y) store_piece_of<DT, true, true>(a.y, at, c, a.cols, y);
             }
         }
-        if constexpr (TEAM > kWave) __syncthreads();
+        __syncthreads();
+    }
+}
+
+// Rows narrower than a piece: a wave to a row, a lane to an element.
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_narrow_kernel(const LayernormArgs a) {
+    const int lane = threadIdx.x % kWave;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; row < a.rows; row += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t at = row * a.cols;
+        const bool exists = lane < a.cols;
+        float f = 0.0f;
+        if (exists) {
+            f = load_elem<DT>(a.x, row * a.ld + lane);
+            if (a.residual) f = rounded_to<DT>(f + load_elem<DT>(a.residual, at + lane));
+            if (a.sum) store_elem<DT>(a.sum, at + lane, f);
+        }
+        const float mean = static_cast<float>(lanes_sum<kWave>(static_cast<double>(f)) * a.each);
+        const double d = static_cast<double>(exists ? f - mean : 0.0f);
+        const float rstd = inverse_deviation(lanes_sum<kWave>(d * d), a.each, a.eps);
+        if (a.mean && lane == 0) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+        float y = (f - mean) * rstd;
+        if (exists && a.weight) y = y * load_elem<DT>(a.weight, lane);
+        if (exists && a.bias) y = y + load_elem<DT>(a.bias, lane);
+        y = exists ? rounded_to<DT>(y) : 0.0f;
+        if (a.y && exists) store_elem<DT>(a.y, at + lane, y);
+        if (a.codes) {
+            const CodeScale s = code_scale(__float_as_uint(team_max<kWave>(__uint_as_float(magnitude_bits(y)))));
+            if (lane == 0) a.scales[row] = s.scale;
+            a.codes[row * a.code_stride + lane] = static_cast<int8_t>(code_of<AQSGD_ROUND_NEAREST>(y, s.inv, 0.5f));      // a stride of 64
+        }
     }
 }
 
 // ---- backward ----------------------------------------------------------------------------------
 // Three ways.  Many rows: a workgroup takes many and keeps the columns' sums of them, which a second launch joins.  Few rows,
 // or rows wider than a workgroup has lanes: the columns' sums by workgroups of their own, which read dy and x a second time.
-// Rows of any width: the same, element by element.
-enum GradWay { kGradBlocks, kGradColumns, kGradAny };
+// Rows narrower than a piece: the same, element by element.
+enum GradWay { kGradBlocks, kGradColumns, kGradNarrow };
 
-constexpr int kWideTeam = 1024;
 constexpr int kGradLanes = 1024;          // of a workgroup that takes many rows
 constexpr int64_t kFewRows = 1024;
 constexpr int kGradBlocksMost = 256;      // workgroups that take many rows: one to a CU
@@ -403,8 +474,8 @@ struct GradPlan {
 template <int DT>
 inline GradPlan grad_plan(int64_t rows, int64_t cols, bool sums) {
     const int64_t pieces = (cols + kPiece<DT> - 1) / kPiece<DT>;
-    GradPlan p = {kGradAny, 0, 0};
-    if (cols < kPiece<DT> || pieces > (DT == AQSGD_F32 ? 4096 : 2048)) return p;
+    GradPlan p = {kGradNarrow, 0, 0};
+    if (cols < kPiece<DT>) return p;
     p.way = kGradColumns;
     if (!sums || rows <= kFewRows || pieces > kGradLanes) return p;
     p.way = kGradBlocks;
@@ -631,63 +702,91 @@ __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const Lay
     }
 }
 
-// Rows of any width.  The columns' sums, in binary64 for a lane adds as many rows as there are: 16 columns to a workgroup, 16
-// lanes to a column.
-constexpr int kAnyCols = 16;
-
+// Rows wider than a workgroup holds in registers: read once for the sums and once for dx.
 template <int DT>
-__global__ __launch_bounds__(256) void layernorm_grad_columns_kernel(const LayernormGradArgs a) {
-    __shared__ double part[2][16][kAnyCols];
-    const int col = threadIdx.x % kAnyCols, slot = threadIdx.x / kAnyCols;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kAnyCols + col;
-    double dw = 0.0, db = 0.0;
-    if (c < a.cols) {
-#pragma unroll 4
-        for (int64_t row = slot; row < a.rows; row += 16) {
-            const float g = load_elem<DT>(a.dy, row * a.cols + c);
-            dw += static_cast<double>(g * ((load_elem<DT>(a.x, row * a.ld + c) - a.mean[row]) * a.rstd[row]));
-            db += static_cast<double>(g);
-        }
-    }
-    part[0][slot][col] = dw;
-    part[1][slot][col] = db;
-    __syncthreads();
-    float* out = slot == 0 ? a.dweight : slot == 1 ? a.dbias : nullptr;
-    if (!out || c >= a.cols) return;
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum += part[slot][i][col];
-    out[c] = a.accumulate ? out[c] + static_cast<float>(sum) : static_cast<float>(sum);
-}
-
-template <int DT, int TEAM>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_grad_any_kernel(const LayernormGradArgs a) {
-    constexpr int kRows = (TEAM < 256 ? 256 : TEAM) / TEAM;
-    __shared__ float part[2][2][16];
-    const int lane = threadIdx.x % TEAM;
+__global__ __launch_bounds__(kWideLanes) void layernorm_grad_wide_kernel(const LayernormGradArgs a) {
+    constexpr int V = kPiece<DT>;
+    __shared__ float2 part[2][kWideLanes / kWave];
+    const int32_t begin = threadIdx.x * V, step = kWideLanes * V;
+    const float each = 1.0f / static_cast<float>(a.cols);
     int turn = 0;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kRows; first < a.rows; first += static_cast<int64_t>(gridDim.x) * kRows, turn ^= 1) {
-        const int64_t row = first + threadIdx.x / TEAM, at = row * a.cols;
-        const int32_t cols = row < a.rows ? a.cols : 0;
-        const float mean = cols ? a.mean[row] : 0.0f, rstd = cols ? a.rstd[row] : 0.0f;
-        const auto hat = [&](int32_t c) { return (load_elem<DT>(a.x, row * a.ld + c) - mean) * rstd; };
-        const auto weighted = [&](int32_t c) {
-            const float g = load_elem<DT>(a.dy, at + c);
-            return a.weight ? g * load_elem<DT>(a.weight, c) : g;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const int64_t at = row * a.cols;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        const auto piece = [&](const void* base, int64_t from, int32_t c) { return whole_piece<DT, true, true>(load_piece<DT, true>(base, from, c, a.cols), c, a.cols); };
+        const auto read = [&](int32_t c, float (&xh)[V], float (&gw)[V]) {
+            piece_values<DT>(placed_piece<DT, true, true>(load_piece<DT, true>(a.x, row * a.ld, c, a.cols), c, a.cols), xh);
+            piece_values<DT>(piece(a.dy, at, c), gw);
+            if (a.weight) {
+                float w[V];
+                piece_values<DT>(piece(a.weight, 0, c), w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) gw[e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) xh[e] = (xh[e] - mean) * rstd;
         };
         float along = 0.0f, across = 0.0f;
-        for (int32_t c = lane; c < cols; c += TEAM) {
-            const float g = weighted(c);
-            along += g;
-            across += g * hat(c);
+        for (int32_t c = begin; c < a.cols; c += step) {
+            float xh[V], gw[V];
+            read(c, xh, gw);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                along += gw[e];
+                across = fmaf(gw[e], xh[e], across);
+            }
         }
-        along = team_sum<TEAM>(along, part[turn][0]) / a.cols;
-        across = team_sum<TEAM>(across, part[turn][1]) / a.cols;
-        for (int32_t c = lane; c < cols; c += TEAM) {
-            float g = rstd * (weighted(c) - along - hat(c) * across);
-            if (a.add) g += load_elem<DT>(a.add, at + c);
-            store_elem<DT>(a.dx, at + c, g);
+        team_sums<kWideLanes>(along, across, part[turn]);
+        along *= each;
+        across *= each;
+        for (int32_t c = begin; c < a.cols; c += step) {
+            float xh[V], gw[V], out[V] = {};
+            read(c, xh, gw);
+            if (a.add) piece_values<DT>(piece(a.add, at, c), out);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = fmaf(rstd, fmaf(-xh[e], across, gw[e] - along), out[e]);
+            store_piece_of<DT, true, true>(a.dx, at, c, a.cols, values_piece<DT>(out));
         }
+    }
+}
+
+// Rows narrower than a piece.  The columns' sums, in binary64 for a lane adds as many rows as there are: a workgroup to a column.
+template <int DT>
+__global__ __launch_bounds__(kWideLanes) void layernorm_grad_narrow_columns_kernel(const LayernormGradArgs a) {
+    __shared__ double part[2][kWideLanes / kWave];
+    const int32_t c = blockIdx.x;
+    double dw = 0.0, db = 0.0;
+#pragma unroll 4
+    for (int64_t row = threadIdx.x; row < a.rows; row += kWideLanes) {
+        const float g = load_elem<DT>(a.dy, row * a.cols + c);
+        dw += static_cast<double>(g * ((load_elem<DT>(a.x, row * a.ld + c) - a.mean[row]) * a.rstd[row]));
+        db += static_cast<double>(g);
+    }
+    dw = team_sum<kWideLanes>(dw, part[0]);
+    db = team_sum<kWideLanes>(db, part[1]);
+    if (threadIdx.x != 0) return;
+    if (a.dweight) a.dweight[c] = a.accumulate ? a.dweight[c] + static_cast<float>(dw) : static_cast<float>(dw);
+    if (a.dbias) a.dbias[c] = a.accumulate ? a.dbias[c] + static_cast<float>(db) : static_cast<float>(db);
+}
+
+// A wave to a row, a lane to an element.
+template <int DT>
+__global__ __launch_bounds__(256) void layernorm_grad_narrow_kernel(const LayernormGradArgs a) {
+    const int lane = threadIdx.x % kWave;
+    const float each = 1.0f / static_cast<float>(a.cols);
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; row < a.rows; row += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t at = row * a.cols + lane;
+        const bool exists = lane < a.cols;
+        float xh = 0.0f, gw = 0.0f;
+        if (exists) {
+            xh = (load_elem<DT>(a.x, row * a.ld + lane) - a.mean[row]) * a.rstd[row];
+            gw = load_elem<DT>(a.dy, at);
+            if (a.weight) gw *= load_elem<DT>(a.weight, lane);
+        }
+        const float along = lanes_sum<kWave>(gw) * each, across = lanes_sum<kWave>(gw * xh) * each;
+        if (!exists) continue;
+        const float more = a.add ? load_elem<DT>(a.add, at) : 0.0f;
+        store_elem<DT>(a.dx, at, fmaf(a.rstd[row], fmaf(-xh, across, gw - along), more));
     }
 }
 
@@ -705,7 +804,7 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
     const bool ragged = a.cols % kPiece<DT> != 0, few = a.rows <= 512;
 #define AQSGD_NORM(TEAM, CPL) \
     return ragged ? go(layernorm_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_kernel<DT, TEAM, CPL, false>, TEAM)
-    if (a.cols < kPiece<DT>) return go(layernorm_any_kernel<DT, 64>, 64);
+    if (a.cols < kPiece<DT>) return go(layernorm_narrow_kernel<DT>, kWave);
     // Many narrow rows: few lanes with several pieces each, so that a wave's sums and statistics serve several rows.  32768 rows (us; with a
     // piece or two a lane in brackets): 130 float16 6.9 (10.7), 300 bfloat16 11.0 (17.7), 768 float16 17.8 (23.2), 129 float32 9.0 (13.9);
     // 4096 rows: 3.2 (3.6), 3.5 (4.5), 4.1 (4.7), 2.9 (3.9); 1024 rows: 3.1 (3.1), 3.1 (3.1), 3.1 (2.9), 2.7 (2.9).
@@ -734,40 +833,54 @@ hipError_t launch_layernorm_as(const LayernormArgs& a, hipStream_t stream) {
     if (pieces <= 512) AQSGD_NORM(256, 2);
     if (pieces <= 768) AQSGD_NORM(256, 3);
     if (pieces <= 1024) AQSGD_NORM(256, 4);
-    if (pieces <= 2048) AQSGD_NORM(1024, 2);
+    // Rows of 16384 bfloat16: 2048 of them 29.9 us, by 1024 lanes 36.3; 16 rows 4.9 and 4.5, 256 rows 5.9 and 5.7.
+    if (pieces <= 2048 && a.rows <= 256) AQSGD_NORM(1024, 2);
+    if (pieces <= 1536) AQSGD_NORM(512, 3);
+    if (pieces <= 2048) AQSGD_NORM(512, 4);
     if (pieces <= 3 * 1024) AQSGD_NORM(1024, 3);
     if (pieces <= 4096) AQSGD_NORM(1024, 4);
 #undef AQSGD_NORM
-    return go(layernorm_any_kernel<DT, kWideTeam>, kWideTeam);
+    return go(layernorm_wide_kernel<DT>, kWideLanes);
 }
 
 hipError_t launch_layernorm_join(const LayernormGradArgs& a, int64_t blocks, hipStream_t stream);
+
+// The columns' launch, if the sums are asked for, and the rows' behind it.
+template <typename C, typename R>
+hipError_t launch_columns_and_rows(bool sums, C&& columns, R&& rows) {
+    std::optional<ProfileSpan> span;
+    if (sums) {
+        span.emplace();
+        const hipError_t err = columns();
+        if (err != hipSuccess) return err;
+        span->last();
+    }
+    return rows();
+}
 
 template <int DT>
 hipError_t launch_layernorm_grad_columns(const LayernormGradArgs& a, hipStream_t stream) {
     const int64_t pieces = (a.cols + kPiece<DT> - 1) / kPiece<DT>;
     const bool ragged = a.cols % kPiece<DT> != 0, sums = a.dweight || a.dbias;
     const uint32_t columns = sums ? static_cast<uint32_t>((pieces + kFewPieces - 1) / kFewPieces) : 0;
-    std::optional<ProfileSpan> span;
-    if (sums && a.dx == a.dy) span.emplace();
+    const int64_t most = int64_t{1} << 21;                                     // workgroups of up to 1024 lanes
+    const auto launch = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int64_t blocks, uint32_t column_blocks) {
+        return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFewLanes), stream, a, column_blocks);
+    };
     const auto go = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int team) {
-        const int64_t per = kFewLanes / team, want = (a.rows + per - 1) / per, most = int64_t{1} << 22;      // 2^31 lanes
-        const unsigned rows = static_cast<unsigned>(want < most ? want : most);
-        if (!span) return launch_kernel(kernel, dim3(columns + rows), dim3(kFewLanes), stream, a, columns);
-        const hipError_t err = launch_kernel(kernel, dim3(columns), dim3(kFewLanes), stream, a, columns);
-        if (err != hipSuccess) return err;
-        span->last();
-        return launch_kernel(kernel, dim3(rows), dim3(kFewLanes), stream, a, uint32_t{0});
+        const int64_t per = kFewLanes / team, want = (a.rows + per - 1) / per, rows = want < most ? want : most;
+        if (a.dx != a.dy) return launch(kernel, columns + rows, columns);
+        return launch_columns_and_rows(sums, [&] { return launch(kernel, columns, columns); }, [&] { return launch(kernel, rows, 0); });
     };
 #define AQSGD_NORM(TEAM, CPL) \
     if (pieces <= TEAM * CPL) \
         return ragged ? go(layernorm_grad_few_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_grad_few_kernel<DT, TEAM, CPL, false>, TEAM);
-    AQSGD_NORM(64, 1) AQSGD_NORM(64, 2) AQSGD_NORM(64, 3) AQSGD_NORM(64, 4) AQSGD_NORM(512, 1) AQSGD_NORM(512, 2) AQSGD_NORM(512, 3)
-    if constexpr (DT == AQSGD_F32) {
-        if (pieces > 2048) AQSGD_NORM(512, 8)
-    }
+    AQSGD_NORM(64, 1) AQSGD_NORM(64, 2) AQSGD_NORM(64, 3) AQSGD_NORM(64, 4) AQSGD_NORM(512, 1) AQSGD_NORM(512, 2) AQSGD_NORM(512, 3) AQSGD_NORM(512, 4)
+    if constexpr (DT == AQSGD_F32) AQSGD_NORM(512, 8)
 #undef AQSGD_NORM
-    return ragged ? go(layernorm_grad_few_kernel<DT, 512, 4, true>, 512) : go(layernorm_grad_few_kernel<DT, 512, 4, false>, 512);
+    const auto few = ragged ? layernorm_grad_few_kernel<DT, 64, 1, true> : layernorm_grad_few_kernel<DT, 64, 1, false>;      // its columns alone
+    return launch_columns_and_rows(sums, [&] { return launch(few, columns, columns); },
+                                   [&] { return launch_kernel(layernorm_grad_wide_kernel<DT>, dim3(static_cast<unsigned>(a.rows < most ? a.rows : most)), dim3(kWideLanes), stream, a); });
 }
 
 template <int DT>
@@ -788,18 +901,11 @@ hipError_t launch_layernorm_grad_blocks(const LayernormGradArgs& a, const GradPl
 }
 
 template <int DT>
-hipError_t launch_layernorm_grad_any(const LayernormGradArgs& a, hipStream_t stream) {
-    const bool sums = a.dweight || a.dbias, narrow = a.cols < kPiece<DT>;
-    std::optional<ProfileSpan> span;
-    if (sums) {
-        span.emplace();
-        const hipError_t err = launch_kernel(layernorm_grad_columns_kernel<DT>, dim3(static_cast<unsigned>((a.cols + kAnyCols - 1) / kAnyCols)), dim3(256), stream, a);
-        if (err != hipSuccess) return err;
-        span->last();
-    }
-    const int64_t per = narrow ? 4 : 1, blocks = (a.rows + per - 1) / per, most = int64_t{1} << 20;
-    return launch_kernel(narrow ? layernorm_grad_any_kernel<DT, 64> : layernorm_grad_any_kernel<DT, kWideTeam>,
-                         dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(narrow ? 256u : unsigned{kWideTeam}), stream, a);
+hipError_t launch_layernorm_grad_narrow(const LayernormGradArgs& a, hipStream_t stream) {
+    const int64_t blocks = (a.rows + 3) / 4, most = int64_t{1} << 20;
+    return launch_columns_and_rows(a.dweight || a.dbias,
+                                   [&] { return launch_kernel(layernorm_grad_narrow_columns_kernel<DT>, dim3(static_cast<unsigned>(a.cols)), dim3(kWideLanes), stream, a); },
+                                   [&] { return launch_kernel(layernorm_grad_narrow_kernel<DT>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), dim3(256), stream, a); });
 }
 
 template <int DT>
@@ -809,7 +915,7 @@ hipError_t launch_layernorm_grad_as(const LayernormGradArgs& a, hipStream_t stre
     switch (p.way) {
     case kGradBlocks:  return launch_layernorm_grad_blocks<DT>(a, p, stream);
     case kGradColumns: return launch_layernorm_grad_columns<DT>(a, stream);
-    default:           return launch_layernorm_grad_any<DT>(a, stream);
+    default:           return launch_layernorm_grad_narrow<DT>(a, stream);
     }
 }
 

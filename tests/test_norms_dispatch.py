@@ -59,14 +59,15 @@ def by_pieces(pairs, name):
 def test_every_kernel_of_the_norm_runs_in_the_gpu_tests(client):
     rows = sizes(G.test_layernorm, "rows,cols")
     made = taken(client(*(("n", t, 0, r, c) for n, t in TYPES.items() for r, c in rows + by_pieces(G.NORMS, n))))
-    for name in ("layernorm_kernel", "layernorm_any_kernel"):
+    for name in ("layernorm_kernel", "layernorm_wide_kernel", "layernorm_narrow_kernel"):
         assert compiled(name) and compiled(name) <= made, compiled(name) - made
 
 
 def test_every_kernel_of_the_gradient_runs_in_the_gpu_tests(client):
     rows = sizes(G.test_layernorm_grad, "rows,cols") + sizes(G.test_layernorm_grad_by_rows, "rows,cols")
     made = taken(client(*(("g", t, which, r, c) for n, t in TYPES.items() for r, c in rows + by_pieces(G.GRADS, n) for which in (0, 1, 3))))
-    for name in ("layernorm_grad_kernel", "layernorm_grad_few_kernel", "layernorm_grad_any_kernel", "layernorm_grad_columns_kernel"):
+    for name in ("layernorm_grad_kernel", "layernorm_grad_few_kernel", "layernorm_grad_wide_kernel", "layernorm_grad_narrow_kernel",
+                 "layernorm_grad_narrow_columns_kernel"):
         assert compiled(name) and compiled(name) <= made, compiled(name) - made
 
 
@@ -86,8 +87,9 @@ def test_launches_of_many_tensors(client):
 def test_launches_of_the_gradient(client):
     """One launch for few rows, two where dx takes dy's place, two for many rows, one without sums."""
     made = client(("g", 1, 1, 1024, 1600), ("g", 1, 3, 1024, 1600), ("g", 1, 1, 1025, 1600), ("g", 1, 3, 1025, 1600), ("g", 1, 0, 100000, 1600),
-                  ("g", 1, 2, 100000, 1600), ("g", 1, 1, 0, 1600), ("g", 1, 1, 5000, 16384), ("g", 1, 1, 100, 3))
-    assert [len(m) for m in made] == [1, 2, 2, 2, 1, 1, 1, 1, 2]
+                  ("g", 1, 2, 100000, 1600), ("g", 1, 1, 0, 1600), ("g", 1, 1, 5000, 16384), ("g", 1, 1, 100, 3), ("g", 1, 1, 100, 70001),
+                  ("g", 1, 0, 100, 70001))
+    assert [len(m) for m in made] == [1, 2, 2, 2, 1, 1, 1, 1, 2, 2, 1]
 
 
 def test_the_largest_calls_stay_within_a_grid(client):
