@@ -433,10 +433,10 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  *               (nearest) makes of the rows of y, whether y itself is stored or not; both or neither NULL
  * sum and y may each be x itself (ld == cols) or residual itself, but not the same one of them; no output may
  * overlap an input or another output otherwise.  A row with an infinity or a NaN in it gives NaN, the others
- * nothing of it.
+ * nothing of it; so does a row whose deviations pass binary32, or a constant one with eps 0.
  *
  * aqsgd_layernorm_grad, the backward pass.  With x the normalised s (of the call above: sum, where
- * there was a residual), xh = (x - mean) * rstd and g = dy * weight, in binary32:
+ * there was a residual), xh = (x - mean) * rstd and g = dy * weight, in binary32 (products and sums may be fused):
  *     dx      = dtype( rstd * (g - sum g / cols - xh * sum (g * xh) / cols)  (+ add) )
  *     dweight = sum over the rows of dy * xh,  dbias = sum over the rows of dy
  * desc.accumulate: dweight and dbias are added to what is there (earlier micro-batches').  Sums are formed
@@ -516,7 +516,7 @@ int aqsgd_layernorm_grad(const aqsgd_layernorm_desc* desc, const void* dy, const
  * Of the tensors only grad and n are looked at.  The order of the sum is fixed by the sizes alone: the same bits on every call.
  *   grad_dtype  aqsgd_dtype of every grad
  *   max_norm    not negative, infinity for no clipping (else AQSGD_ERR_SHAPE)
- *   loss_scale  device float, or NULL for 1;  result out float[2]
+ *   loss_scale  device float above 0, or NULL for 1;  result out float[2]
  *   workspace   aqsgd_grad_norm_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use once the
  *               call's work has run
  */

