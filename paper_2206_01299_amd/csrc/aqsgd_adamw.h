@@ -325,12 +325,14 @@ __global__ __launch_bounds__(kWave * kUpdateWaves) void adamw_kernel(const Updat
     }
 }
 
+// The table goes to the runtime from where it is: launch_kernel's copies of its arguments would cost the host more here than elsewhere.
 template <int DT, int GT>
 hipError_t launch_adamw_as(const AdamwKind& kind, const UpdateTable& table, uint32_t blocks, const AdamwArgs& a, hipStream_t stream) {
-    const dim3 grid(blocks), block(kWave * kUpdateWaves);
-    if (kind.state_bits == 32) return launch_kernel(adamw_kernel<DT, GT, 32, AQSGD_ROUND_NEAREST>, grid, block, stream, table, a);
-    if (kind.rounding == AQSGD_ROUND_NEAREST) return launch_kernel(adamw_kernel<DT, GT, 8, AQSGD_ROUND_NEAREST>, grid, block, stream, table, a);
-    return launch_kernel(adamw_kernel<DT, GT, 8, AQSGD_ROUND_STOCHASTIC>, grid, block, stream, table, a);
+    void (*const kernel)(const UpdateTable, const AdamwArgs) = kind.state_bits == 32                     ? adamw_kernel<DT, GT, 32, AQSGD_ROUND_NEAREST>
+                                                               : kind.rounding == AQSGD_ROUND_NEAREST ? adamw_kernel<DT, GT, 8, AQSGD_ROUND_NEAREST>
+                                                                                                      : adamw_kernel<DT, GT, 8, AQSGD_ROUND_STOCHASTIC>;
+    void* argv[] = {const_cast<UpdateTable*>(&table), const_cast<AdamwArgs*>(&a)};
+    return launch_with(reinterpret_cast<const void*>(kernel), dim3(blocks), dim3(kWave * kUpdateWaves), stream, argv);
 }
 
 }  // namespace aqsgd

@@ -973,21 +973,24 @@ private:
 
 // Returns the status of this launch alone (an earlier error that the calling
 // thread has not collected is neither reported here nor cleared).
+inline hipError_t launch_with(const void* kernel, dim3 grid, dim3 block, hipStream_t stream, void** argv) {
+    ProfileRequest& pr = g_profile_request;
+    if (pr.start || pr.stop) {
+        const hipError_t err = hipExtLaunchKernel(kernel, grid, block, argv, 0, stream, pr.start, pr.stop, 0);
+        pr.start = nullptr;
+        pr.stop = nullptr;
+        return err;
+    }
+    return hipLaunchKernel(kernel, grid, block, argv, 0, stream);
+}
+
 template <typename... KArgs, typename... Args>
 hipError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t stream,
                          Args... args) {
     std::tuple<KArgs...> held(args...);
     void* argv[sizeof...(KArgs)];
     fill_arg_pointers(held, argv, std::index_sequence_for<KArgs...>{});
-    ProfileRequest& pr = g_profile_request;
-    if (pr.start || pr.stop) {
-        const hipError_t err = hipExtLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv,
-                                                  0, stream, pr.start, pr.stop, 0);
-        pr.start = nullptr;
-        pr.stop = nullptr;
-        return err;
-    }
-    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, argv, 0, stream);
+    return launch_with(reinterpret_cast<const void*>(kernel), grid, block, stream, argv);
 }
 
 // Team shapes the dispatcher may pick; index into the table below.

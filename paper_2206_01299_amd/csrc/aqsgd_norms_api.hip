@@ -166,7 +166,7 @@ int aqsgd_adamw(const aqsgd_adamw_desc* d, const aqsgd_adamw_tensor* tensors, in
     std::optional<ProfileSpan> profile;
     if (full > kTableTensors) profile.emplace();
     const AdamwKind kind = {d->dtype, d->grad_dtype, d->state_bits, d->rounding};
-    UpdateTable table = {};
+    UpdateTable table;                                      // entries behind the last tensor's are never looked at
     int held = 0;
     int64_t blocks = 0, groups = 0;
     const auto send = [&] {
@@ -217,7 +217,7 @@ int aqsgd_grad_norm(int32_t grad_dtype, const aqsgd_adamw_tensor* tensors, int32
     double* const partial = static_cast<double*>(workspace);
     std::optional<ProfileSpan> profile;
     if (parts) profile.emplace();
-    NormTable table = {};
+    NormTable table;
     int held = 0;
     int64_t blocks = 0, sent = 0;
     const auto send = [&] {

@@ -470,13 +470,17 @@ AQSGD_ENTRY(py_layernorm_grad, 12, {
 })
 
 // The binding's list of tensors: its array's memory while this lives, on the current device.
+struct ListNames {
+    PyObject *array, *device, *whole, *kind;
+} g_list_names;
+
 class List {
 public:
     List(PyObject* o, Placed& c) {
-        PyObject* array = attribute(o, "array");
-        PyObject* device = attribute(o, "device");
-        PyObject* whole_flag = attribute(o, "whole");
-        kind_ = attribute(o, "kind");
+        PyObject* array = attribute(o, g_list_names.array);
+        PyObject* device = attribute(o, g_list_names.device);
+        PyObject* whole_flag = attribute(o, g_list_names.whole);
+        kind_ = attribute(o, g_list_names.kind);
         ok_ = array && device && whole_flag && kind_ && PyLong_Check(device) && PyLong_AsLong(device) == c.device &&
               PyTuple_CheckExact(kind_) && PyTuple_GET_SIZE(kind_) == 3 && PyObject_GetBuffer(array, &view_, PyBUF_SIMPLE) == 0;
         whole = whole_flag == Py_True;
@@ -500,8 +504,8 @@ public:
     bool whole = false;
 
 private:
-    static PyObject* attribute(PyObject* o, const char* name) {
-        PyObject* v = PyObject_GetAttrString(o, name);
+    static PyObject* attribute(PyObject* o, PyObject* name) {
+        PyObject* v = PyObject_GetAttr(o, name);
         if (!v) PyErr_Clear();
         return v;
     }
@@ -652,6 +656,9 @@ PyObject* py_setup(PyObject*, PyObject* const* p, Py_ssize_t np) {
     AQSGD_TAKE(layernorm) AQSGD_TAKE(layernorm_grad_workspace_bytes) AQSGD_TAKE(layernorm_grad) AQSGD_TAKE(adamw)
     AQSGD_TAKE(grad_norm_workspace_bytes) AQSGD_TAKE(grad_norm)
 #undef AQSGD_TAKE
+    g_list_names = {PyUnicode_InternFromString("array"), PyUnicode_InternFromString("device"), PyUnicode_InternFromString("whole"),
+                    PyUnicode_InternFromString("kind")};
+    if (!g_list_names.array || !g_list_names.device || !g_list_names.whole || !g_list_names.kind) return nullptr;
     for (Py_ssize_t i = 0; i < kTypes; ++i) Py_INCREF(p[i]);
     g_quant8_type = reinterpret_cast<PyTypeObject*>(p[2]);
     g_matmul8_type = reinterpret_cast<PyTypeObject*>(p[3]);
