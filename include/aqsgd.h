@@ -444,7 +444,7 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  *   dy          in   [rows, cols] dense;  x in, as above;  mean, rstd in float[rows]
  *   weight      in   [cols], or NULL for 1;  add in [rows, cols] dense, or NULL: the gradient that arrives along
  *               the residual stream
- *   dx          out  [rows, cols] dense; may be dy or add itself, and must not overlap an input otherwise
+ *   dx          out  [rows, cols] dense; may be dy or add itself, and must not overlap an input otherwise (x itself: AQSGD_ERR_SHAPE)
  *   dweight     out  float[cols], or NULL;  dbias out float[cols], or NULL
  *   workspace   aqsgd_layernorm_grad_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use
  *               once the call's work has run; NULL where that is 0 or neither dweight nor dbias is asked for

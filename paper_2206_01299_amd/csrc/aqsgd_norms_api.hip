@@ -128,6 +128,7 @@ int aqsgd_layernorm_grad(const aqsgd_layernorm_desc* d, const void* dy, const vo
         const size_t need = sums ? aqsgd_layernorm_grad_workspace_bytes(d) : 0;
         if (need && (!workspace || workspace_bytes < need)) return AQSGD_ERR_WORKSPACE;
         if (need && !aligned(workspace, 16)) return AQSGD_ERR_ALIGN;
+        if (dx == x) return AQSGD_ERR_SHAPE;                // other workgroups read x for the columns' sums
     }
     LayernormGradArgs a;
     a.dy = dy; a.x = x; a.mean = mean; a.rstd = rstd; a.weight = weight; a.add = add; a.dx = dx;

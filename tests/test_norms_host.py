@@ -92,6 +92,7 @@ def test_layernorm_grad_refusals():
                      ("dw", 4098), ("db", 4098), ("ws", 4104)):
         assert lg(d, **{name: ctypes.c_void_p(at)}) == -6, name
     assert lg(d, ws=NULL) == -9 and lg(d, n=need - 1) == -9
+    assert lg(d, dx=OK, x=OK) == -5 and lg(row_desc(), dx=OK, x=OK, dw=NULL, db=NULL) == -5      # in x's place
     for few in (row_desc(), row_desc(rows=4096, cols=2 ** 20, ld=2 ** 20)):             # no block's sums to join
         assert B.layernorm_grad_workspace_bytes(few) == 0
 
