@@ -27,6 +27,7 @@ extern "C" hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void
 int main(int argc, char** argv) {
     char* at = reinterpret_cast<char*>(uintptr_t{1} << 20);
     char* other = at + (uintptr_t{1} << 30);
+    char* third = other + (uintptr_t{1} << 30);
     auto* floats = reinterpret_cast<float*>(at);
     const size_t plenty = size_t{1} << 40;
     for (int i = 1; i < argc; ++i) {
@@ -38,7 +39,7 @@ int main(int argc, char** argv) {
         if (what == 'n' || what == 'g') {
             aqsgd_layernorm_desc d = {x, y, y, dtype, 0, 1e-5};
             status = what == 'n' ? aqsgd_layernorm(&d, at, nullptr, at, at, nullptr, other, floats, floats, nullptr, nullptr, nullptr)
-                                 : aqsgd_layernorm_grad(&d, at, at, floats, floats, at, nullptr, kind & 2 ? at : other, kind & 1 ? floats : nullptr,
+                                 : aqsgd_layernorm_grad(&d, at, third, floats, floats, at, nullptr, kind & 2 ? at : other, kind & 1 ? floats : nullptr,
                                                         kind & 1 ? floats : nullptr, at, plenty, nullptr);
         } else {
             std::vector<aqsgd_adamw_tensor> tensors(static_cast<size_t>(y), {at, at, at, nullptr, x, 0.0});
