@@ -100,6 +100,10 @@ struct NormTable {
     int64_t n[kTableTensors];
 };
 hipError_t launch_grad_squares(int dtype, const NormTable& table, uint32_t blocks, int64_t span, double* partial, hipStream_t stream);
+// Up to so many chunks of norm_chunk() elements, a tensor's last one shorter, in one launch: first[i] counts chunks.
+constexpr int kFewChunks = 64;
+int64_t norm_chunk(int dtype);
+hipError_t launch_grad_norm_few(int dtype, const NormTable& table, uint32_t chunks, double max_norm, const float* loss_scale, float* result, hipStream_t stream);
 hipError_t launch_grad_norm(const double* partial, int64_t count, double max_norm, const float* loss_scale, float* result, hipStream_t stream);
 
 }  // namespace aqsgd

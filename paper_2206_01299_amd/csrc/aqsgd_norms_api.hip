@@ -204,10 +204,14 @@ int aqsgd_grad_norm(int32_t grad_dtype, const aqsgd_adamw_tensor* tensors, int32
     if (rc != AQSGD_OK) return rc;
     if (!(max_norm >= 0.0)) return AQSGD_ERR_SHAPE;
     if (!result) return AQSGD_ERR_NULL;
+    int64_t chunks = 0;
+    int32_t full = 0;
     for (int32_t i = 0; i < n_tensors; ++i) {
         if (tensors[i].n == 0) continue;
         if (!tensors[i].grad) return AQSGD_ERR_NULL;
         if (!aligned(tensors[i].grad, elem_bytes(grad_dtype))) return AQSGD_ERR_ALIGN;
+        chunks += parts_of(tensors[i].n, norm_chunk(grad_dtype));
+        ++full;
     }
     if (!aligned(loss_scale, 4) || !aligned(result, 4)) return AQSGD_ERR_ALIGN;
     const int64_t parts = norm_parts(tensors, n_tensors), span = norm_span(tensors, n_tensors);
@@ -215,11 +219,24 @@ int aqsgd_grad_norm(int32_t grad_dtype, const aqsgd_adamw_tensor* tensors, int32
         if (!workspace || workspace_bytes < static_cast<size_t>(8 * parts)) return AQSGD_ERR_WORKSPACE;
         if (!aligned(workspace, 16)) return AQSGD_ERR_ALIGN;
     }
+    NormTable table;
+    int held = 0;
+    if (full > 0 && full <= kTableTensors && chunks <= kFewChunks) {
+        uint32_t at = 0;
+        for (int i = held; i < kTableTensors; ++i) table.first[i] = 0xffffffffu;
+        for (const aqsgd_adamw_tensor* t = tensors; t != tensors + n_tensors; ++t) {
+            if (t->n == 0) continue;
+            table.first[held] = at;
+            table.grad[held] = t->grad;
+            table.n[held] = t->n;
+            ++held;
+            at += static_cast<uint32_t>(parts_of(t->n, norm_chunk(grad_dtype)));
+        }
+        return status(launch_grad_norm_few(grad_dtype, table, at, max_norm, loss_scale, result, static_cast<hipStream_t>(stream)));
+    }
     double* const partial = static_cast<double*>(workspace);
     std::optional<ProfileSpan> profile;
     if (parts) profile.emplace();
-    NormTable table;
-    int held = 0;
     int64_t blocks = 0, sent = 0;
     const auto send = [&] {
         for (int i = held; i < kTableTensors; ++i) table.first[i] = 0xffffffffu;

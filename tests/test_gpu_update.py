@@ -309,6 +309,31 @@ def test_grad_norm(dtype, sizes):
         assert abs(got[1] - min(1.0, most / norm) * inverse) <= 2 * N.U * abs(got[1])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sizes", [[2, 7, 8, 9, 0, 255, 256, 257, 1, 511, 512, 513], [512] * 32, [1] * 64, [256] * 65, [16384], [16385], [32768], [32769], [9, 16000]])
+def test_grad_norm_of_few_elements(dtype, sizes):
+    """Around what one launch takes; from addresses of any alignment, among infinities that belong to nothing."""
+    grads, want = [], 0.0
+    for i, g in enumerate(grads_of(sizes, dtype, 1)):
+        at = 1 + i % 7
+        held = torch.full((g.numel() + 16,), math.inf, dtype=g.dtype, device="cuda")
+        held[at:at + g.numel()] = g
+        grads.append(held[at:at + g.numel()])
+        want += (g.double() ** 2).sum().item()
+    made, result = B.adamw_tensors(B.make_adamw_desc(dtype=dtype), grads=grads), Framed((2,), torch.float32)
+    ws = Framed((B.grad_norm_workspace_bytes(made),), torch.uint8)
+    got = []
+    for _ in range(2):
+        B.grad_norm(made, result.t, max_norm=0.5, workspace=ws.t)
+        torch.cuda.synchronize()
+        got.append(result.t.tolist())
+    ws.check("workspace")
+    result.check("result")
+    want = math.sqrt(want)
+    assert got[0] == got[1] and abs(got[0][0] - want) <= 2 * N.U * want
+    assert abs(got[0][1] - min(1.0, 0.5 / want)) <= 2 * N.U * got[0][1]
+
+
 def test_grad_norm_of_what_is_no_ordinary_number():
     for dtype, value in (("f32", 3e38), ("bf16", 3e38), ("f16", 65504.0), ("f32", 2.0 ** -149), ("f16", 2.0 ** -24)):
         g = torch.full((5000,), value, dtype=B.DTYPE_NAME[dtype], device="cuda")
@@ -318,9 +343,9 @@ def test_grad_norm_of_what_is_no_ordinary_number():
         want = g[0].double().item() * math.sqrt(5000) / 256
         assert abs(result[0].item() - want) <= 2 * N.U * want + 2.0 ** -149
         assert abs(result[1].item() - min(1.0, 1.0 / want) / 256) <= 2 * N.U / 256
-    for bad in (math.inf, math.nan, -math.inf):
-        g = torch.ones(5000, device="cuda")
-        g[4999] = bad
+    for bad, n in ((math.inf, 5000), (math.nan, 5000), (-math.inf, 5000), (math.nan, 50000), (math.inf, 50000)):
+        g = torch.ones(n, device="cuda")
+        g[n - 1] = bad
         result = torch.empty(2, device="cuda")
         B.grad_norm(B.adamw_tensors(B.make_adamw_desc(dtype="f32"), grads=[g]), result, max_norm=1.0)
         assert not math.isfinite(result[0].item()) and math.isnan(result[1].item())

@@ -78,10 +78,10 @@ def test_every_kernel_of_the_update_runs_in_the_gpu_tests(client):
 
 
 def test_launches_of_many_tensors(client):
-    """64 tensors to a launch; a norm has one launch more; none for tensors of no elements."""
-    made = client(("a", 0, 0, 100, 64), ("a", 0, 0, 100, 65), ("a", 0, 0, 100, 200), ("a", 0, 0, 0, 200), ("r", 1, 0, 100, 64), ("r", 1, 0, 100, 65),
-                  ("r", 1, 0, 0, 3), ("a", 0, 0, 1 << 34, 3))
-    assert [len(m) for m in made] == [1, 2, 4, 0, 2, 3, 1, 3]
+    """64 tensors to a launch; a norm has one launch more, a small one of up to 64 tensors just one; none for tensors of no elements."""
+    made = client(("a", 0, 0, 100, 64), ("a", 0, 0, 100, 65), ("a", 0, 0, 100, 200), ("a", 0, 0, 0, 200), ("r", 1, 0, 513, 64), ("r", 1, 0, 100, 65),
+                  ("r", 1, 0, 0, 3), ("a", 0, 0, 1 << 34, 3), ("r", 1, 0, 512, 64), ("r", 0, 0, 16384, 1), ("r", 0, 0, 16385, 1))
+    assert [len(m) for m in made] == [1, 2, 4, 0, 2, 3, 1, 3, 1, 1, 2]
 
 
 def test_launches_of_the_gradient(client):
