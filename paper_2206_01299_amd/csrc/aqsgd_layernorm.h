@@ -597,16 +597,16 @@ __global__ __launch_bounds__(kGradLanes) void layernorm_grad_kernel(const Layern
     if (a.dbias) leave(db, to + blocks * a.cols);
 }
 
-// The second way in one launch: the first workgroups take the columns, 64 bytes of every row, the others the rows; neither needs
+// The second way in one launch: the first workgroups take the columns, PIECES of every row, the others the rows; neither needs
 // the other's sums.  Where dx is dy itself the columns go first, in a launch of their own.
-constexpr int kFewLanes = 512, kFewPieces = 4, kFewSlots = kFewLanes / kFewPieces;      // pieces side by side, rows at a time
+constexpr int kFewLanes = 512;
 
-template <int DT, bool RAGGED>
+template <int DT, int PIECES, bool RAGGED>
 __device__ __forceinline__ void columns_of_few(const LayernormGradArgs& a, int64_t block) {
-    constexpr int V = kPiece<DT>, kCols = kFewPieces * V, kGroups = kFewLanes / kCols, kAhead = 4;
+    constexpr int V = kPiece<DT>, kCols = PIECES * V, kGroups = kFewLanes / kCols, kFewSlots = kFewLanes / PIECES, kAhead = 4;
     __shared__ float part[2][kFewSlots][kCols + 1];
     __shared__ float last[2][kGroups][kCols + 1];
-    const int slot = threadIdx.x / kFewPieces, across = threadIdx.x % kFewPieces;
+    const int slot = threadIdx.x / PIECES, across = threadIdx.x % PIECES;
     const int32_t c = static_cast<int32_t>(block * kCols) + across * V;
     float dw[V] = {}, db[V] = {};
     for (int64_t first = slot; first < a.rows; first += kFewSlots * kAhead) {
@@ -657,10 +657,10 @@ __device__ __forceinline__ void columns_of_few(const LayernormGradArgs& a, int64
     out[at] = a.accumulate ? out[at] + sum : sum;
 }
 
-template <int DT, int TEAM, int CPL, bool RAGGED>
+template <int DT, int TEAM, int CPL, int PIECES, bool RAGGED>
 __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const LayernormGradArgs a, const uint32_t column_blocks) {
     if (blockIdx.x < column_blocks) {
-        columns_of_few<DT, RAGGED>(a, blockIdx.x);
+        columns_of_few<DT, PIECES, RAGGED>(a, blockIdx.x);
         return;
     }
     constexpr int kTeams = kFewLanes / TEAM, V = kPiece<DT>;
@@ -865,27 +865,35 @@ template <int DT>
 hipError_t launch_layernorm_grad_columns(const LayernormGradArgs& a, hipStream_t stream) {
     const int64_t pieces = (a.cols + kPiece<DT> - 1) / kPiece<DT>;
     const bool ragged = a.cols % kPiece<DT> != 0, sums = a.dweight || a.dbias;
-    const uint32_t columns = sums ? static_cast<uint32_t>((pieces + kFewPieces - 1) / kFewPieces) : 0;
     const int64_t most = int64_t{1} << 21;                                     // workgroups of up to 1024 lanes
-    const auto launch = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int64_t blocks, uint32_t column_blocks) {
-        return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFewLanes), stream, a, column_blocks);
+    const auto column_blocks = [&](int each) { return sums ? static_cast<uint32_t>((pieces + each - 1) / each) : 0; };
+    const auto launch = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int64_t blocks, uint32_t columns) {
+        return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kFewLanes), stream, a, columns);
     };
-    const auto go = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int team) {
+    const auto go = [&](void (*kernel)(const LayernormGradArgs, const uint32_t), int team, int each) {
         const int64_t per = kFewLanes / team, want = (a.rows + per - 1) / per, rows = want < most ? want : most;
+        const uint32_t columns = column_blocks(each);
         if (a.dx != a.dy) return launch(kernel, columns + rows, columns);
         return launch_columns_and_rows(sums, [&] { return launch(kernel, columns, columns); }, [&] { return launch(kernel, rows, 0); });
     };
-#define AQSGD_NORM(TEAM, CPL) \
+#define AQSGD_NORM(TEAM, CPL, PIECES) \
     if (pieces <= TEAM * CPL) \
-        return ragged ? go(layernorm_grad_few_kernel<DT, TEAM, CPL, true>, TEAM) : go(layernorm_grad_few_kernel<DT, TEAM, CPL, false>, TEAM);
+        return ragged ? go(layernorm_grad_few_kernel<DT, TEAM, CPL, PIECES, true>, TEAM, PIECES) \
+                      : go(layernorm_grad_few_kernel<DT, TEAM, CPL, PIECES, false>, TEAM, PIECES);
     // Few rows go by four waves each where one would take several pieces a lane: 8 rows of 1600 float16 2.6 us, by a wave 3.8; 256 rows
     // 3.1 and 4.1, 512 rows 4.6 and 4.5, 4096 rows without sums 8.6 and 7.6.
-    if (a.rows <= 256 && pieces > 64) AQSGD_NORM(256, 1)
-    AQSGD_NORM(64, 1) AQSGD_NORM(64, 2) AQSGD_NORM(64, 3) AQSGD_NORM(64, 4) AQSGD_NORM(512, 1) AQSGD_NORM(512, 2) AQSGD_NORM(512, 3) AQSGD_NORM(512, 4)
-    if constexpr (DT == AQSGD_F32) AQSGD_NORM(512, 8)
+    if (a.rows <= 256 && pieces > 64) AQSGD_NORM(256, 1, 4)
+    // Columns: 64 bytes of a row to a workgroup, 128 where that still makes 128 workgroups, 32 where the rows are many and their
+    // columns' workgroups would be the last to end.  2, 4 and 8 pieces (us): 1000 x 200 float16 3.7, 4.5, 6.5; 1024 x 1600 7.6, 7.4, 10.0;
+    // 1000 x 6144 bfloat16 23.4, 15.4, 16.0; 1024 x 4096 float32 31.7, 19.5, 17.0; 2048 x 8192 float32 122, 80, 62.
+    if (a.rows > 256) AQSGD_NORM(64, 1, 2)
+    AQSGD_NORM(64, 1, 4) AQSGD_NORM(64, 2, 4) AQSGD_NORM(64, 3, 4) AQSGD_NORM(64, 4, 4) AQSGD_NORM(512, 1, 4)
+    if (pieces < 1024) AQSGD_NORM(512, 2, 4)
+    AQSGD_NORM(512, 2, 8) AQSGD_NORM(512, 3, 8) AQSGD_NORM(512, 4, 8)
+    if constexpr (DT == AQSGD_F32) AQSGD_NORM(512, 8, 8)
 #undef AQSGD_NORM
-    const auto few = ragged ? layernorm_grad_few_kernel<DT, 64, 1, true> : layernorm_grad_few_kernel<DT, 64, 1, false>;      // its columns alone
-    return launch_columns_and_rows(sums, [&] { return launch(few, columns, columns); },
+    const auto few = ragged ? layernorm_grad_few_kernel<DT, 64, 1, 8, true> : layernorm_grad_few_kernel<DT, 64, 1, 8, false>;      // its columns alone
+    return launch_columns_and_rows(sums, [&] { const uint32_t columns = column_blocks(8); return launch(few, columns, columns); },
                                    [&] { return launch_kernel(layernorm_grad_wide_kernel<DT>, dim3(static_cast<unsigned>(a.rows < most ? a.rows : most)), dim3(kWideLanes), stream, a); });
 }
 
