@@ -462,7 +462,6 @@ __global__ __launch_bounds__(256) void layernorm_narrow_kernel(const LayernormAr
 enum GradWay { kGradBlocks, kGradColumns, kGradNarrow };
 
 constexpr int kGradLanes = 1024;          // of a workgroup that takes many rows
-constexpr int64_t kFewRows = 1024;
 constexpr int kGradBlocksMost = 256;      // workgroups that take many rows: one to a CU
 
 // The workspace of the first way: sums of blocks of rows, for the weight [blocks, cols] and for the bias [blocks, cols].
@@ -472,15 +471,21 @@ struct GradPlan {
     int64_t blocks;                       // workgroups, and sums of each column
 };
 
-// 1024 rows (us, both ways): 1600 float16 10.7 by blocks and 7.6 by columns, 4096 float32 19.7 and 19.7; 2048 rows: 13.0 and 12.8,
-// 32.4 and 38.5, 200 float16 7.3 and 9.5.  Without sums rows alone are left, which blocks would only hold up.
+// Both ways (us, by blocks and by columns): 1024 x 1600 float16 10.7 and 7.3, 1400 x 1600 11.2 and 9.3, 2048 x 1600 11.7 and 12.7; 1280 x 400 6.8
+// and 5.8, 2048 x 400 7.2 and 8.5; 1100 x 768 bfloat16 7.3 and 7.8; 1400 x 4096 float32 23.8 and 22.6, 2048 x 4096 32.2 and 32.9; 2048 x 5120 bfloat16
+// 30.0 and 25.3, 2048 x 8192 43.9 and 33.2, 6000 x 8192 86 and 94.  Without sums rows alone are left, which blocks would only hold up.
+template <int DT>
+inline int64_t most_rows_by_columns(int64_t pieces) {
+    return DT != AQSGD_F32 && pieces > kGradLanes / 2 ? 2048 : pieces > 64 && pieces <= 128 ? 1024 : 1408;
+}
+
 template <int DT>
 inline GradPlan grad_plan(int64_t rows, int64_t cols, bool sums) {
     const int64_t pieces = (cols + kPiece<DT> - 1) / kPiece<DT>;
     GradPlan p = {kGradNarrow, 0, 0};
     if (cols < kPiece<DT>) return p;
     p.way = kGradColumns;
-    if (!sums || rows <= kFewRows || pieces > kGradLanes) return p;
+    if (!sums || rows <= most_rows_by_columns<DT>(pieces) || pieces > kGradLanes) return p;
     p.way = kGradBlocks;
     p.team = 16;
     while (p.team < pieces) p.team *= 2;

@@ -58,8 +58,8 @@ def sums_off(terms, longest):
 def norm_grad(dy, x, mean, rstd, weight, add):
     """dx, dweight, dbias in 64 bits from the binary32 statistics, and how far off each may be.  Roundings, in half steps:
     x - mean and its product with rstd 2 (xh); dy * weight 1 (g); a term g * xh 4.  No lane adds more than 128 + cols / 64
-    terms of a row one behind the other (twelve more levels join the lanes), nor more than 128 + rows / 128 rows of a
-    column (and a workgroup's 64 at most); the joined sums are added in binary64."""
+    terms of a row one behind the other (twelve more levels join the lanes), nor more than 128 + rows / 64 rows of a
+    column (a workgroup that takes 128 bytes of every row reads 64 rows at a time; and its 64 sums at most); the joined sums are added in binary64."""
     rows, cols = x.shape
     dy, x = dy.astype(np.float64), x.astype(np.float64)
     mean, rstd = mean.astype(np.float64)[:, None], rstd.astype(np.float64)[:, None]
@@ -75,7 +75,7 @@ def norm_grad(dy, x, mean, rstd, weight, add):
     dx, dx_off = rstd * inner, rstd * inner_off + U * np.abs(rstd * inner)
     if add is not None:
         dx, dx_off = R.plus(dx, dx_off, add.astype(np.float64))
-    deepest = 128 + rows // 128 + 64
+    deepest = 128 + rows // 64 + 64
     dw, db = (dy * xh).sum(axis=0), dy.sum(axis=0)
     dw_off = (deepest + 5) * U * np.abs(dy * xh).sum(axis=0)
     db_off = (deepest + 1) * U * np.abs(dy).sum(axis=0)

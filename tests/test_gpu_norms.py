@@ -316,7 +316,8 @@ PIECES = {"f32": 4, "f16": 8, "bf16": 8}
 NORMS = [(7, 5), (16, 40), (30, 9), (64, 7), (100, 9), (190, 600), (250, 600), (200, 5), (500, 3), (700, 3), (1000, 3), (2000, 2), (2900, 2), (4000, 2),
          (1500, 300), (2000, 300), (7, 4100), (15, 4100), (22, 4100), (30, 4100), (45, 4100), (60, 4100), (90, 4100), (120, 4100)]
 GRADS = [(10, 1100), (30, 1100), (64, 1100), (100, 1100), (200, 1100), (400, 1100), (1000, 1100), (60, 20), (200, 20), (128, 300), (150, 300), (250, 300), (500, 5),
-         (900, 5), (1500, 5), (2048, 4), (4000, 3), (3, 300), (25, 700), (64, 1024), (1024, 6), (1024, 140), (1100, 130)]
+         (900, 5), (1500, 5), (2048, 4), (4000, 3), (3, 300), (25, 700), (64, 1024), (1024, 6), (1024, 140), (1100, 130),
+         (10, 1409), (30, 1409), (64, 1500), (200, 1500), (400, 1409), (600, 2049), (600, 1409)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
