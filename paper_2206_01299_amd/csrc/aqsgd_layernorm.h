@@ -888,12 +888,12 @@ hipError_t launch_layernorm_grad_columns(const LayernormGradArgs& a, hipStream_t
     // Few rows go by four waves each where one would take several pieces a lane: 8 rows of 1600 float16 2.6 us, by a wave 3.8; 256 rows
     // 3.1 and 4.1, 512 rows 4.6 and 4.5, 4096 rows without sums 8.6 and 7.6.
     if (a.rows <= 256 && pieces > 64) AQSGD_NORM(256, 1, 4)
-    // Columns: 64 bytes of a row to a workgroup, 128 where that still makes 128 workgroups, 32 where the rows are many and their
+    // Columns: 64 bytes of a row to a workgroup, 128 where that still makes 100 workgroups, 32 where the rows are many and their
     // columns' workgroups would be the last to end.  2, 4 and 8 pieces (us): 1000 x 200 float16 3.7, 4.5, 6.5; 1024 x 1600 7.6, 7.4, 10.0;
     // 1000 x 6144 bfloat16 23.4, 15.4, 16.0; 1024 x 4096 float32 31.7, 19.5, 17.0; 2048 x 8192 float32 122, 80, 62.
     if (a.rows > 256) AQSGD_NORM(64, 1, 2)
     AQSGD_NORM(64, 1, 4) AQSGD_NORM(64, 2, 4) AQSGD_NORM(64, 3, 4) AQSGD_NORM(64, 4, 4) AQSGD_NORM(512, 1, 4)
-    if (pieces < 1024) AQSGD_NORM(512, 2, 4)
+    if (pieces < 800) AQSGD_NORM(512, 2, 4)
     AQSGD_NORM(512, 2, 8) AQSGD_NORM(512, 3, 8) AQSGD_NORM(512, 4, 8)
     if constexpr (DT == AQSGD_F32) AQSGD_NORM(512, 8, 8)
 #undef AQSGD_NORM
