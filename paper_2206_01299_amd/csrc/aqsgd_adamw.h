@@ -3,11 +3,12 @@
 // Every element is read and written once, past the caches.  With states in 32 bits memory bounds the step: 30.7 M float16
 // weights with binary32 copies and gradients 153 us, 6.0 TB/s.  In 8 bits what is moved halves and the arithmetic doubles (a root and a
 // quotient for the step, two roots for the codes): 123 M such weights 359 us, 6.2 TB/s, but 28.3 M bfloat16 ones without
-// copies 76 us, 3.8 TB/s, and 87 with draws, where the vector units issue in 93 % of the cycles.
+// copies 74 us, 3.9 TB/s, and 83 with draws, where vector instructions are what bounds it.
 //
 // Lanes take four neighbouring elements at a time, so that binary32 accesses are contiguous.  With states in 8 bits half a wave
 // takes a group in two such pieces: what a lane does once for its group (four quotients, two maxima over the lanes) is shared by eight
-// elements (28.3 M bfloat16 weights 77 us, with a wave to a group and four elements a lane 110).  Everything stays in
+// elements (28.3 M bfloat16 weights 77 us, with a wave to a group and four elements a lane 110).  Root and quotient by a step from the
+// hardware's reciprocals, where a vote says that their ranges allow it: with draws 83 us, by the compiler's quotient 87.  Everything stays in
 // registers between the loads and the stores.  A workgroup's tensor is found in the launch's table by one load and a vote of the wave.
 #pragma once
 
@@ -78,13 +79,12 @@ __device__ __forceinline__ void store_four(void* base, int64_t i, int count, con
 // What all of a tensor's elements share.
 struct UpdateFactors {
     float decay, length, correct;         // 1 - lr * weight_decay, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-    float scale;
-    bool scaled;
+    float scale;                          // 1 where there is none
 };
 
 // The moments of one element after this step.
 __device__ __forceinline__ void step_moments(const AdamwArgs& a, const UpdateFactors& k, float g, float& m, float& v) {
-    if (k.scaled) g = g * k.scale;
+    g = g * k.scale;
     m = m * a.beta1f + g * a.rest1;
     v = v * a.beta2f + (g * a.rest2) * g;
 }
@@ -93,14 +93,19 @@ __device__ __forceinline__ float stepped_weight(const AdamwArgs& a, const Update
     return w * k.decay - (m / (r * k.correct + a.eps)) * k.length;
 }
 
-// The root of a v that is 0 or at least 2^-96 (or no finite number), rounded once: the hardware's is within an ulp, and the
-// residuals of its neighbours say which of the three it is (checked on every significand of eleven binades from -96 to 127); below,
-// the residuals are no longer exact.  Twelve issue cycles a value instead of nineteen.
+// The root of a v that is 0 or between 2^-96 and 2^127, rounded once: v times the hardware's reciprocal root is within two ulps, and
+// one step by the residual, which is exact, ends at the right one (tried on every significand of twelve binades).
 __device__ __forceinline__ float root_of(float v) {
-    const float s = __builtin_amdgcn_sqrtf(v);
-    const float down = __uint_as_float(__float_as_uint(s) - 1u), up = __uint_as_float(__float_as_uint(s) + 1u);
-    float r = fmaf(-down, s, v) <= 0.0f ? down : s;
-    return fmaf(-up, s, v) > 0.0f ? up : r;
+    const float y = __builtin_amdgcn_rsqf(fmaxf(v, 0x1p-126f)), s = v * y;
+    return fmaf(fmaf(-s, s, v), 0.5f * y, s);
+}
+
+// A quotient, rounded once, of an m that is 0 or between 2^-70 and 2^60 in magnitude by a d between 2^-48 and 2^50.  The reciprocal is the
+// rounded one after a step (tried on every significand of d); from that, a residual without error, which these ranges grant, leads
+// to the rounded quotient (Markstein's theorem).  The residual is formed the other way round so that a zero keeps its sign.
+__device__ __forceinline__ float quotient_of(float m, float d) {
+    const float y = __builtin_amdgcn_rcpf(d), inverse = fmaf(fmaf(-d, y, 1.0f), y, y), q = m * inverse;
+    return fmaf(-fmaf(d, q, -m), inverse, q);
 }
 
 // ---- states in 8 bits ----------------------------------------------------------------------------
@@ -125,9 +130,9 @@ __device__ __forceinline__ HeldScale held_scale(uint32_t bits, float top) {
 // changes nothing: from either side the distance leads to the same neighbour.  Draws ask for the right one: the
 // root is taken a little low, and raised where the next square is not above u (both checked on every u to 255^2, draws with the
 // smallest and largest z).  No code passes T: u is at most T^2 (1 + 2^-23), nearer to T^2 than any threshold (z (2 T + 1), z at
-// least 2^-16).
+// least 2^-16).  z is (word + 1) / 65536; its product with 2 k + 1 is one fused step.
 template <int ROUND>
-__device__ __forceinline__ float held_code(float x, float inv, float z) {
+__device__ __forceinline__ float held_code(float x, float inv, float word) {
     const float u = x * inv;
     if constexpr (ROUND == AQSGD_ROUND_NEAREST) {
         const float k = floorf(__builtin_amdgcn_sqrtf(u));
@@ -136,7 +141,8 @@ __device__ __forceinline__ float held_code(float x, float inv, float z) {
         float k = floorf(__builtin_amdgcn_sqrtf(u) * (1.0f - 0x1p-21f));
         const float next = k + 1.0f;
         k = next * next <= u ? next : k;
-        return fmaf(-k, k, u) >= z * fmaf(2.0f, k, 1.0f) ? k + 1.0f : k;
+        const float width = fmaf(k, 0x1p-15f, 0x1p-16f);
+        return fmaf(-k, k, u) >= fmaf(word, width, width) ? k + 1.0f : k;
     }
 }
 
@@ -184,7 +190,7 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
         }
     }
     const float m_step = divided_by<127 * 127>(*m_scale), r_step = divided_by<255 * 255>(*r_scale);
-    uint32_t least = 0xffffffffu;                          // pattern of the smallest v that is not 0, less one
+    uint32_t m_least = 0xffffffffu, v_least = 0xffffffffu, m_top = 0, r_top = 0;      // patterns of magnitudes; of the smallest that is not 0, less one
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
         mc[p] ^= 0x80808080u;                              // code + 128 as bytes
@@ -195,30 +201,36 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
             m[p][e] = (mk * fabsf(mk)) * m_step;
             v[p][e] = root * root;
             step_moments(a, k, g[p][e], m[p][e], v[p][e]);
-            least = min(least, __float_as_uint(v[p][e]) - 1u);
-        }
-    }
-    if (__any(least < 0x0f800000u - 1u)) {                 // 2^-96
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[p][e] = sqrtf(v[p][e]);
-    } else {
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[p][e] = root_of(v[p][e]);
-    }
-    uint32_t m_top = 0, r_top = 0;
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[p][e] = stepped_weight(a, k, w[p][e], m[p][e], r[p][e]);
-            if (!FULL && e >= count[p]) m[p][e] = r[p][e] = 0.0f;
-            m_top = max(m_top, __float_as_uint(m[p][e]) & 0x7fffffffu);
+            if (!FULL && e >= count[p]) m[p][e] = v[p][e] = 0.0f;
+            r[p][e] = root_of(v[p][e]);
+            const uint32_t size = __float_as_uint(m[p][e]) & 0x7fffffffu;
+            m_least = min(m_least, size - 1u);
+            m_top = max(m_top, size);
+            v_least = min(v_least, __float_as_uint(v[p][e]) - 1u);
             r_top = max(r_top, __float_as_uint(r[p][e]));  // not below 0; a NaN of either sign lies above all numbers
         }
+    }
+    // What root_of and quotient_of ask for holds of any usual step; d is eps or more, and "1 / sqrt(1 - beta2^t)" below 2^27.
+    const bool usual = m_least >= 0x1c800000u - 1u && m_top < 0x5d800000u && v_least >= 0x0f800000u - 1u && r_top < 0x49800000u &&
+                       a.eps >= 0x1p-48f && a.eps <= 0x1p48f;      // m 2^-70, 2^60; v 2^-96; r 2^20
+    if (__all(usual)) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[p][e] = w[p][e] * k.decay - quotient_of(m[p][e], r[p][e] * k.correct + a.eps) * k.length;
+    } else {
+        r_top = 0;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                r[p][e] = sqrtf(v[p][e]);
+                r_top = max(r_top, __float_as_uint(r[p][e]));
+                w[p][e] = stepped_weight(a, k, w[p][e], m[p][e], r[p][e]);
+            }
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
         const int64_t i = first + 128 * p;
         if (t.master) store_four<AQSGD_F32, FULL>(t.master, i, count[p], w[p]);
         store_four<DT, FULL>(t.param, i, count[p], w[p]);
@@ -226,7 +238,7 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
     const HeldScale ms = held_scale(half_wave_max(m_top), kMTop), rs = held_scale(half_wave_max(r_top), kRTop);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        float zm[4], zr[4];
+        float m_word[4], r_word[4];
         if constexpr (ROUND == AQSGD_ROUND_STOCHASTIC) {
             const uint64_t block = static_cast<uint64_t>(t.group0 + group) * (kStateGroup / 4) + static_cast<uint32_t>(32 * p + l);
             uint32_t words[4];
@@ -234,15 +246,15 @@ __device__ __forceinline__ void adamw8_group(const UpdateTensor& t, const AdamwA
                           static_cast<uint32_t>(key >> 32), words);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                zm[e] = fmaf(static_cast<float>(words[e] & 0xffffu), 0x1p-16f, 0x1p-16f);
-                zr[e] = fmaf(static_cast<float>(words[e] >> 16), 0x1p-16f, 0x1p-16f);
+                m_word[e] = static_cast<float>(words[e] & 0xffffu);
+                r_word[e] = static_cast<float>(words[e] >> 16);
             }
         }
         mc[p] = rc[p] = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float mk = held_code<ROUND>(fabsf(m[p][e]), ms.inv, zm[e]);
-            const float rk = fmaxf(held_code<ROUND>(r[p][e], rs.inv, zr[e]), fminf(r[p][e] * 0x1p100f, 1.0f));
+            const float mk = held_code<ROUND>(fabsf(m[p][e]), ms.inv, m_word[e]);
+            const float rk = fmaxf(held_code<ROUND>(r[p][e], rs.inv, r_word[e]), fminf(fmaxf(r[p][e] * 0x1p100f, 0.0f), 1.0f));
             mc[p] = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(mk, m[p][e]) + 128.0f, e, mc[p]);
             rc[p] = __builtin_amdgcn_cvt_pk_u8_f32(rk, e, rc[p]);
         }
@@ -295,8 +307,7 @@ template <int DT, int GT, int BITS, int ROUND>
 __global__ __launch_bounds__(kWave * kUpdateWaves) void adamw_kernel(const UpdateTable table, const AdamwArgs a) {
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     UpdateFactors k;
-    k.scaled = a.scale != nullptr;
-    k.scale = k.scaled ? *a.scale : 1.0f;
+    k.scale = a.scale ? *a.scale : 1.0f;
     if (!(fabsf(k.scale) < __builtin_inff())) return;                     // a step that is skipped
     const int which = __builtin_amdgcn_readfirstlane(__popcll(__ballot(table.first[lane] <= blockIdx.x)) - 1);
     const UpdateTensor& t = table.tensor[which];
