@@ -167,6 +167,29 @@ def test_adamw_of_gradients_that_are_no_ordinary_numbers(dtype, bits, rounding):
 
 
 @pytest.mark.parametrize("bits,rounding", KINDS)
+@pytest.mark.parametrize("settings", [{}, dict(eps=0.0), dict(eps=1e-30), dict(eps=2.0 ** -48), dict(eps=1e-15), dict(eps=2.0 ** 48), dict(eps=1e16),
+                                      dict(beta2=1 - 2.0 ** -53), dict(beta1=1 - 2.0 ** -53, beta2=1 - 2.0 ** -53, eps=2.0 ** 48)])
+def test_adamw_at_the_ends_of_the_quick_ranges(settings, bits, rounding):
+    """Gradients of every size, and such whose moments lie right at or beside 2^-70, 2^60 (m), 2^-48 and 2^20 (r)."""
+    p = Program([256 * 40, 777], "f32", "f32", bits, rounding, seed=9, **settings)
+    d = p.desc
+    for step in (1, 2, 3):
+        p.draw()
+        g = p.grads[0].t
+        signs = torch.where(torch.arange(256 * 8, device="cuda") % 3 == 0, -1.0, 1.0)
+        g[:256 * 8] = signs * torch.exp2(torch.linspace(-149, 126, 256 * 8, device="cuda", dtype=torch.float64)).float()
+        for group, (at, part) in enumerate(((2.0 ** -70, 1 - d.beta1), (2.0 ** 60, 1 - d.beta1), (2.0 ** -48, (1 - d.beta2) ** 0.5), (2.0 ** 20, (1 - d.beta2) ** 0.5)), 8):
+            exact = np.float32(at / part)
+            beside = [exact]
+            for _ in range(4):
+                beside = [np.nextafter(beside[0], np.float32(0)), *beside, np.nextafter(beside[-1], np.float32(np.inf))]
+            for k, v in enumerate(beside):                                      # one such element to a group
+                g[256 * (group + 6 * (k % 4)) + 17 * k] = float(v)
+        p.step(step)
+        p.check(f"step {step}")
+
+
+@pytest.mark.parametrize("bits,rounding", KINDS)
 def test_a_factor_that_is_not_finite_skips_the_step(bits, rounding):
     p = Program([700, 70], "f16", "f32", bits, rounding, master=True)
     p.draw()
