@@ -675,7 +675,12 @@ __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const Lay
     const float each = 1.0f / static_cast<float>(a.cols);
     const int64_t stride = static_cast<int64_t>(gridDim.x - column_blocks) * kTeams;
     int turn = 0;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x - column_blocks) * kTeams + team; row < a.rows; row += stride, turn ^= 1) {
+    for (int64_t first = static_cast<int64_t>(blockIdx.x - column_blocks) * kTeams; first < a.rows; first += stride, turn ^= 1) {
+        // A team of one wave waits for nobody and may leave; of several, all go on to team_sums' barrier, one without a row with
+        // the last row again: what it reads there, dx perhaps over dy by then, is not used.
+        const bool here = first + team < a.rows;
+        if (TEAM <= kWave && !here) break;
+        const int64_t row = here ? first + team : a.rows - 1;
         GradRow<DT, TEAM, CPL> now;
         now.ask(a, row, lane);
         u32x4_t w[CPL];
@@ -705,7 +710,7 @@ __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const Lay
             if (a.add) piece_values<DT>(whole_piece<DT, last, RAGGED>(now.more[i], column(i), a.cols), out);
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = fmaf(now.rstd, fmaf(-xh[i][e], across, gw[i][e] - along), out[e]);
-            store_piece_of<DT, last, RAGGED>(a.dx, row * a.cols, column(i), a.cols, values_piece<DT>(out));
+            if (here) store_piece_of<DT, last, RAGGED>(a.dx, row * a.cols, column(i), a.cols, values_piece<DT>(out));
         });
     }
 }

@@ -37,3 +37,35 @@ extern "C" __global__ void units(char* p, Raw<AQSGD_F32> r) { store_raw_units(p,
     asm = _compile(tmp_path, text)
     wide = [l for l in asm.splitlines() if re.search(r"global_store_dwordx4 .*\bnt\b", l)]
     assert len(wide) == len(stores), asm
+
+
+def _bodies(text, opening):
+    """(head, body) of every block that a match of `opening` begins; the match ends with the opening brace."""
+    for m in re.finditer(opening, text):
+        depth, end = 1, m.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(text[end], 0)
+            end += 1
+        yield m.group(0), text[m.end():end - 1]
+
+
+def test_loops_with_a_barrier_turn_as_often_for_every_wave_of_a_workgroup():
+    """A barrier waits for the whole workgroup, so a loop that has one in it goes by the workgroup's number, never by a team's
+    or a lane's: where only some of the teams have a row, the others go along without storing.  Sums over a team of several waves have a
+    barrier in them."""
+    barrier = re.compile(r"__syncthreads\(|\bteam_(?:sum|sums|top)<|\bworkgroup_sum<")
+    own = re.compile(r"\bteam\b|\blane\b|\bslot\b|threadIdx")
+    loops = 0
+    for name in ("aqsgd_layernorm.h", "aqsgd_layernorm.hip", "aqsgd_grad_norm.hip", "aqsgd_adamw.h"):
+        text = re.sub(r"//[^\n]*", "", (_build.CSRC / name).read_text())
+        for head, body in _bodies(text, r"__global__[^;{]*\{"):
+            kernel = re.search(r"(\w+)\(const", head).group(1)
+            for loop, inside in _bodies(body, r"\bfor \([^{;]*;[^{;]*;[^{;]*\) \{"):
+                if not barrier.search(inside):
+                    continue
+                loops += 1
+                init, until = loop.split(";")[:2]
+                assert not own.search(init) and not own.search(until), f"{kernel}: {loop}"
+                for leave in re.finditer(r"^\s*if \(([^{;]*)\) (?:return|continue|break);", inside, re.M):
+                    assert "TEAM <= kWave" in leave.group(1) or not re.search(own.pattern + r"|\bhere\b", leave.group(1)), f"{kernel}: {leave.group(0)}"
+    assert loops >= 5
