@@ -421,8 +421,10 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  * For every row of x [rows, cols], s = x, or s = dtype(x + residual):
  *     mean = RN( sum s / cols ),  d = RN(s - mean),  rstd = RN( 1 / sqrt( sum d^2 / cols + eps ) )
  *     y    = dtype( RN( RN( RN(d * rstd) * weight ) + bias ) )
- * with the sums, quotients and the root in binary64, everything else in binary32.  Without a weight
- * its factor is left out, without a bias its term.
+ * with the sums (in an order that the sizes fix), the quotients and the root's inverse (to two units of its last
+ * place) in binary64, everything else in binary32.  The same sizes give the same bits on every call; between sizes mean and rstd of
+ * equal rows differ only where the last places of a binary64 sum decide how it rounds.  Without a weight its factor is left out,
+ * without a bias its term.
  *   x           in   [rows, cols], desc.ld elements from one row to the next
  *   residual    in   [rows, cols] dense, or NULL; added to x in binary32
  *   weight      in   [cols], or NULL;  bias in [cols], or NULL; of desc.dtype

@@ -4,9 +4,8 @@
 // 1024), which forms the row's sums between the load and the store.  What bounds them is memory, and in small calls a launch and
 // one chain of load, two sums and store: one row of 1600 float16 3.0 us, 4096 such rows with residual, codes and statistics 12.2 (4.8
 // TB/s), 16384 of 4096 float32 96 (5.6 TB/s); their gradients 2.6, 16.6 and 188.  The forward pass sums in
-// binary64, which costs little here, so that mean and rstd are
-// the definition's binary32 numbers whatever the order, and codes that hang on them do not change with the launch.  Lanes take pieces
-// of 16 bytes side by side.
+// binary64, which costs little here: statistics then depend on the order, and with it on the launch, only where a sum's last places in
+// binary64 decide how it rounds to binary32.  Lanes take pieces of 16 bytes side by side.
 #pragma once
 
 #include <optional>
@@ -197,10 +196,20 @@ struct TeamSpace {                       // of a workgroup that is one team
     uint32_t top[16];
 };
 
-// 1 / sqrt of the variance in binary64, rounded once: the hardware's (2^-24 of it off at most) and two steps of Newton's, ten
+// A sum over the columns by their number, the quotient rounded once.  Its product with the rounded inverse `each` is up to 1.5 units
+// of the last place off, which at a width of 49, 300 or 1537 puts a quotient in the middle between two binary32 numbers on
+// one side of it.  The residual is a multiple of that unit below 1.5 cols of them, so it has no error, and the step by it none of
+// 2^-52 units.  A quotient that is not in the middle between two binary64 numbers is 1 / (2 cols) units or more from it, cols being
+// at most 2^24, and none is in the middle: that has 54 bits, and its product with cols, the sum, no fewer.
+__device__ __forceinline__ double column_mean(double sum, int32_t cols, double each) {
+    const double q = sum * each;
+    return fabs(q) < __builtin_inf() ? fma(fma(-q, static_cast<double>(cols), sum), each, q) : q;
+}
+
+// 1 / sqrt of the variance, in binary64 to its last places and then rounded: the hardware's (2^-24 of it off at most) and two steps of Newton's, ten
 // operations instead of some sixty for a root and a quotient (4096 x 1600 float16 with residual and codes 12.8 -> 12.2 us).
-__device__ __forceinline__ float inverse_deviation(double squares, double each, double eps) {
-    const double v = squares * each + eps;
+__device__ __forceinline__ float inverse_deviation(double squares, int32_t cols, double each, double eps) {
+    const double v = column_mean(squares, cols, each) + eps;
     double y = __builtin_amdgcn_rsq(v);
     if (v > 0.0 && v < __builtin_inf()) {
 #pragma unroll
@@ -269,7 +278,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
             for (int e = 0; e < V; ++e) total += static_cast<double>(f[e]);
         });
         if (a.sum && here) each_piece<CPL>([&](auto i, auto last) { store_piece_of<DT, last, RAGGED>(a.sum, row * a.cols, column(i), a.cols, held[i]); });
-        const float mean = static_cast<float>(team_sum<TEAM>(total, space.first) * a.each);
+        const float mean = static_cast<float>(column_mean(team_sum<TEAM>(total, space.first), a.cols, a.each));
         double squares = 0.0;
         each_piece<CPL>([&](auto i, auto last) {
             if (last && column(i) >= a.cols) return;
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void layernorm_kernel(cons
                 squares = fma(d, d, squares);
             }
         });
-        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.each, a.eps);
+        const float rstd = inverse_deviation(team_sum<TEAM>(squares, space.second), a.cols, a.each, a.eps);
         if (a.mean && here && lane == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(kWideLanes) void layernorm_wide_kernel(const Layern
 #pragma unroll
             for (int e = 0; e < V; ++e) total += static_cast<double>(f[e]);
         }
-        const float mean = static_cast<float>(team_sum<kWideLanes>(total, space.first) * a.each);
+        const float mean = static_cast<float>(column_mean(team_sum<kWideLanes>(total, space.first), a.cols, a.each));
         for (int32_t c = begin; c < a.cols; c += step) {
             float f[V];
             again(c, f);
@@ -374,7 +383,7 @@ __global__ __launch_bounds__(kWideLanes) void layernorm_wide_kernel(const Layern
                 squares = fma(d, d, squares);
             }
         }
-        const float rstd = inverse_deviation(team_sum<kWideLanes>(squares, space.second), a.each, a.eps);
+        const float rstd = inverse_deviation(team_sum<kWideLanes>(squares, space.second), a.cols, a.each, a.eps);
         if (a.mean && threadIdx.x == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -435,9 +444,9 @@ __global__ __launch_bounds__(256) void layernorm_narrow_kernel(const LayernormAr
             if (a.residual) f = rounded_to<DT>(f + load_elem<DT>(a.residual, at + lane));
             if (a.sum) store_elem<DT>(a.sum, at + lane, f);
         }
-        const float mean = static_cast<float>(lanes_sum<kWave>(static_cast<double>(f)) * a.each);
+        const float mean = static_cast<float>(column_mean(lanes_sum<kWave>(static_cast<double>(f)), a.cols, a.each));
         const double d = static_cast<double>(exists ? f - mean : 0.0f);
-        const float rstd = inverse_deviation(lanes_sum<kWave>(d * d), a.each, a.eps);
+        const float rstd = inverse_deviation(lanes_sum<kWave>(d * d), a.cols, a.each, a.eps);
         if (a.mean && lane == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
