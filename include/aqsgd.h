@@ -435,7 +435,8 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  *               (nearest) makes of the rows of y, whether y itself is stored or not; both or neither NULL
  * sum and y may each be x itself (ld == cols) or residual itself, but not the same one of them; no output may
  * overlap an input or another output otherwise.  A row with an infinity or a NaN in it gives NaN, the others
- * nothing of it; so does a row whose deviations pass binary32, or a constant one with eps 0.
+ * nothing of it; so does a constant row with eps 0.  A row with deviations that pass binary32 has rstd 0: NaN where they do,
+ * 0 * weight + bias elsewhere.
  *
  * aqsgd_layernorm_grad, the backward pass.  With x the normalised s (of the call above: sum, where
  * there was a residual), xh = (x - mean) * rstd and g = dy * weight, in binary32 (products and sums may be fused):

@@ -59,3 +59,23 @@ def test_means_in_the_middle_between_two_numbers(dtype, rows, cols):
     x = rows_of_totals(means * cols, cols, dtype, rng)
     got = G.run_norm(x, dtype)["mean"].t.cpu().numpy()
     assert np.array_equal(got, means.astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(5, 3), (5, 40), (5, 1600), (5000, 96), (600, 1600), (5, 5001), (3, 20001)])
+def test_deviations_that_pass_binary32(dtype, rows, cols):
+    """Where x - mean overflows the row's rstd is 0: NaN at those elements, the bias at the others, no more than that."""
+    big = {"bf16": 3.3895e38, "f32": 3.4028e38}[dtype]
+    rng = np.random.default_rng([rows, cols])
+    x, b, w = rng.standard_normal((rows, cols)), 1 + rng.random(cols), rng.standard_normal(cols)
+    clean = G.run_norm(x, dtype, weight=w, bias=b)["y"].t.clone()
+    x[1] = -big
+    x[1, 1:3 if cols > 3 else 2] = big
+    got = G.run_norm(x, dtype, weight=w, bias=b)
+    assert np.isfinite(got["mean"].t[1].item()) and got["rstd"].t[1].item() == 0.0
+    y, over = got["y"].t, torch.from_numpy(x[1] > 0).cuda()
+    assert torch.isnan(y[1, over]).all()
+    assert torch.equal(y[1, ~over], torch.from_numpy(b).float().cuda().to(y.dtype)[~over])
+    assert torch.isnan(got["row_scales"].t[1]) and not got["row_codes"].t[1].any()
+    others = torch.arange(rows, device="cuda") != 1
+    assert torch.equal(y[others], clean[others])
