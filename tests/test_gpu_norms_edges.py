@@ -79,3 +79,65 @@ def test_deviations_that_pass_binary32(dtype, rows, cols):
     assert torch.isnan(got["row_scales"].t[1]) and not got["row_codes"].t[1].any()
     others = torch.arange(rows, device="cuda") != 1
     assert torch.equal(y[others], clean[others])
+
+
+# ---- columns' sums of many rows ----------------------------------------------------------------
+
+def added_in_a_row(rows, cols, dtype):
+    """How many rows a lane adds one behind the other, and then teams, where 256 workgroups take the rows: pieces of 16 bytes to a lane, teams
+    of 16 lanes or more, 1024 lanes to a workgroup."""
+    team = 16
+    while team * G.PIECES[dtype] < cols:
+        team *= 2
+    teams = 1024 // team
+    return -(-rows // (256 * teams)) + teams
+
+
+def sums_within(got, terms, longest, each):
+    """Against the sum in 64 bits of terms that are `each` half steps off: `longest` additions and the last rounding."""
+    want, size = terms.sum(dim=0), terms.abs().sum(dim=0)
+    assert ((got.double() - want).abs() <= 1.01 * (longest + each + 1) * N.U * size).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(70000, 24), (20000, 300), (30000, 129), (9000, 1537), (5000, 4096)])
+def test_sums_of_many_rows_are_as_near_as_their_order_allows(dtype, rows, cols):
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x, dy = (torch.randn((rows, cols), device="cuda", generator=g).to(B.DTYPE_NAME[dtype]) for _ in range(2))
+    d = B.make_layernorm_desc(rows=rows, cols=cols, dtype=dtype)
+    mean, rstd, dw, db = (torch.empty(n, device="cuda") for n in (rows, rows, cols, cols))
+    B.layernorm(d, x, mean=mean, rstd=rstd)
+    B.layernorm_grad(d, dy, x, mean, rstd, torch.empty_like(x), dweight=dw, dbias=db)
+    longest = added_in_a_row(rows, cols, dtype)
+    sums_within(dw, dy.double() * ((x.double() - mean.double()[:, None]) * rstd.double()[:, None]), longest, 2)
+    sums_within(db, dy.double(), longest, 0)
+
+
+def test_the_gradient_of_more_rows_than_a_grid_has_teams():
+    """70 million rows of 8, a period of 999983 again and again, by workgroups that keep the columns' sums: every period's dx is that of a call on
+    one, whose rows go by teams as wide, and both sums are within their roundings."""
+    period, rows, cols = 999983, 70_000_000, 8
+    if torch.cuda.mem_get_info()[0] < (60 << 30):
+        pytest.skip("needs 40 GB")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x1, dy1 = (torch.randn((period, cols), device="cuda", generator=g).half() for _ in range(2))
+    few, d = (B.make_layernorm_desc(rows=n, cols=cols, dtype="f16") for n in (period, rows))
+    mean1, rstd1 = torch.empty(period, device="cuda"), torch.empty(period, device="cuda")
+    B.layernorm(few, x1, mean=mean1, rstd=rstd1)
+    sums = [torch.empty(cols, device="cuda") for _ in range(4)]
+    dx1 = torch.empty_like(x1)
+    B.layernorm_grad(few, dy1, x1, mean1, rstd1, dx1, dweight=sums[0], dbias=sums[1])
+    x, dy, mean, rstd = (t.repeat(rows // period + 1, *[1] * (t.dim() - 1))[:rows].contiguous() for t in (x1, dy1, mean1, rstd1))
+    dx = torch.empty_like(x)
+    B.layernorm_grad(d, dy, x, mean, rstd, dx, dweight=sums[2], dbias=sums[3])
+    for at in range(0, rows, period):
+        n = min(period, rows - at)
+        assert torch.equal(dx[at:at + n], dx1[:n]), at
+    xh1 = (x1.double() - mean1.double()[:, None]) * rstd1.double()[:, None]
+    times = torch.full((period, 1), rows // period, dtype=torch.float64, device="cuda")
+    times[:rows % period] += 1
+    for terms, each, one, all_ in ((dy1.double() * xh1, 2, sums[0], sums[2]), (dy1.double(), 0, sums[1], sums[3])):
+        sums_within(one, terms, added_in_a_row(period, cols, "f16"), each)
+        sums_within(all_, terms * times, added_in_a_row(rows, cols, "f16"), each)
+    del x, dy, dx
+    torch.cuda.empty_cache()
