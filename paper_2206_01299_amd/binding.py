@@ -829,10 +829,13 @@ def adamw_state_views(desc: AdamwDesc, state, n: int) -> tuple:
 
 class AdamwTensors:
     """The tensors of :func:`adamw` and :func:`grad_norm` calls, checked once and kept alive: what a program builds
-    before its first step.  ``whole``: with weights and states, not gradients alone."""
+    before its first step.  ``whole``: with weights and states, not gradients alone.  ``listed``: the tensors, gradients first, then
+    weights, states and copies; ``places``: storage, offset and size of each.  A call looks whether each still lies there and refuses
+    a list with one that has got other memory since (by ``t.data = ...``, ``set_`` or ``resize_``)."""
 
-    def __init__(self, array, kind: tuple, whole: bool, device: int, held):
+    def __init__(self, array, kind: tuple, whole: bool, device: int, held, listed: tuple = (), places=None):
         self.array, self.kind, self.whole, self.device, self.held = array, kind, whole, device, held
+        self.listed, self.places = listed, places
 
     def __len__(self) -> int:
         return len(self.array)
@@ -845,7 +848,9 @@ def _kind_of(desc: AdamwDesc) -> tuple:
 def adamw_tensors(desc: AdamwDesc, *, grads, params=None, states=None, masters=None, weight_decays=None) -> AdamwTensors:
     """``params`` (any shapes, contiguous), ``grads`` of the same shapes, ``states`` (uint8, :func:`adamw_state_bytes` each),
     ``masters`` (float32 copies of 16-bit weights) and ``weight_decays`` (numbers), each a sequence with an entry a
-    tensor.  ``grads`` alone serve :func:`grad_norm`."""
+    tensor.  ``grads`` alone serve :func:`grad_norm`.  The list is of these tensors where they are now: gradients have to be formed in
+    them again at every step (a backward pass that makes new ones, as after ``zero_grad(set_to_none=True)``, is not seen), and after
+    a tensor has got other memory the list has to be made anew."""
     grads = list(grads)
     whole = params is not None
     lists = {"params": params, "states": states, "masters": masters, "weight_decays": weight_decays}
@@ -878,12 +883,28 @@ def adamw_tensors(desc: AdamwDesc, *, grads, params=None, states=None, masters=N
     for a, b in zip(written, written[1:]):
         if a[0] + a[1] > b[0]:
             raise ValueError(f"{a[2]}[{a[3]}] and {b[2]}[{b[3]}] overlap")
-    return AdamwTensors(array, _kind_of(desc), whole, torch.cuda.current_device(), (grads, lists))
+    listed = (*grads, *(t for name in _LISTS[1:] for t in lists.get(name, ())))
+    places = (ctypes.c_uint64 * (3 * len(listed)))(*(n for t in listed for n in _place(t)))
+    return AdamwTensors(array, _kind_of(desc), whole, torch.cuda.current_device(), (grads, lists), listed, places)
 
 
-def _check_tensors(tensors: AdamwTensors) -> None:
+_LISTS = ("grads", "params", "states", "masters")
+
+
+def _place(t) -> tuple:
+    """Where a tensor's elements are: its storage's address, its offset in there, their number; one of none is nowhere."""
+    n = t.numel()
+    return (t.untyped_storage().data_ptr(), t.storage_offset(), n) if n else (0, 0, 0)
+
+
+def _check_tensors(tensors: AdamwTensors, grads_alone: bool = False) -> None:
     if tensors.device != torch.cuda.current_device():
         raise ValueError(f"the tensors are on cuda:{tensors.device}, the call is made on cuda:{torch.cuda.current_device()}")
+    n = len(tensors)
+    types = (_TORCH_OF_CODE[tensors.kind[1]], _TORCH_OF_CODE[tensors.kind[0]], torch.uint8, torch.float32)
+    for i, t in enumerate(tensors.listed[:n] if grads_alone else tensors.listed):
+        if t.dtype != types[i // n] or not t.is_contiguous() or tensors.places[3 * i:3 * i + 3] != list(_place(t)):
+            raise ValueError(f"{_LISTS[i // n]}[{i % n}] is no longer what or where it was when the list was made")
 
 
 def adamw(desc: AdamwDesc, tensors: AdamwTensors, *, lr=None, step=None, scale=None, stream=None) -> None:
@@ -919,7 +940,7 @@ def grad_norm(tensors: AdamwTensors, result, *, max_norm: float = float("inf"), 
     if rc is not None:
         return _raise(rc) if rc else None
     _check_stream(stream)
-    _check_tensors(tensors)
+    _check_tensors(tensors, grads_alone=True)
     if loss_scale is not None:
         _want(loss_scale, "loss_scale", torch.float32, 1, exact=True)
     args = [_here("loss_scale", loss_scale, torch.float32, loss_scale.shape) if loss_scale is not None else None,

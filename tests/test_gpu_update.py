@@ -540,3 +540,40 @@ def test_a_stages_step_with_its_norm_and_its_update():
         torch.cuda.synchronize()
         for a, b in zip(captured.masters + captured.weights + captured.states, eager.masters + eager.weights + eager.states):
             assert torch.equal(a, b), f"replay {step}"
+
+
+@pytest.mark.parametrize("which", ["params", "grads", "states", "masters"])
+@pytest.mark.parametrize("how", ["data", "grown"])
+def test_a_list_whose_tensors_have_moved_is_refused(which, how):
+    """Both ways of the binding refuse it before anything is launched; a list made anew goes on."""
+    d = B.make_adamw_desc(dtype="f16", grad_dtype="f32", state_bits=8)
+    sizes = [700, 0, 3, 5000]
+    lists = {"params": [torch.nn.Parameter(torch.ones(n, device="cuda").half(), requires_grad=False) for n in sizes],
+             "grads": [torch.ones(n, device="cuda") for n in sizes], "masters": [torch.ones(n, device="cuda") for n in sizes],
+             "states": [torch.zeros(B.adamw_state_bytes(d, n), dtype=torch.uint8, device="cuda") for n in sizes]}
+    made, result = B.adamw_tensors(d, **lists), torch.empty(2, device="cuda")
+    ws = torch.empty(B.grad_norm_workspace_bytes(made), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        return (B._native.adamw(d, made, None, None, None, None), B._native.grad_norm(made, result, 1.0, None, ws, None))
+
+    assert calls() == (0, 0)
+    t = lists[which][3]
+    size = t.numel()
+    if how == "data":
+        t.data = t.data.clone()
+    else:
+        t.resize_(1 << 20)
+    torch.cuda.synchronize()
+    before = [p.clone() for p in lists["params"]]
+    assert calls() == (None, None if which == "grads" else 0)
+    with pytest.raises(ValueError, match=which + r"\[3\] is no longer"):
+        B.adamw(d, made)
+    torch.cuda.synchronize()
+    for a, b in zip(before, lists["params"]):
+        assert torch.equal(a, b)
+    t.resize_(size)
+    made = B.adamw_tensors(d, **lists)
+    assert calls() == (0, 0)
+    torch.cuda.synchronize()
+    assert result[0] > 0 and (lists["params"][0] != before[0]).all()

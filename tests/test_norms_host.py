@@ -205,6 +205,43 @@ def test_a_list_of_tensors_is_checked_when_it_is_made(host_tensors):
         B.adamw_tensors(bad, grads=[])
 
 
+def moved(t, how):
+    """Leaves the same tensor object with other memory, or with other elements in the same memory."""
+    if how == "data":
+        t.data = t.data.clone()
+    elif how == "set":
+        t.set_(torch.zeros_like(t))
+    elif how == "freed":
+        t.untyped_storage().resize_(0)
+    elif how == "grown":
+        t.resize_(100000)
+    elif how == "shrunk":
+        t.resize_(2)
+    elif how == "turned":
+        t.t_()
+
+
+@pytest.mark.parametrize("how", ["data", "set", "freed", "grown", "shrunk", "turned"])
+@pytest.mark.parametrize("which", ["params", "grads", "states", "masters"])
+def test_a_list_whose_tensors_have_moved_is_refused(host_tensors, which, how):
+    """The list holds addresses: what is written there after a tensor has got other memory is no weight any more."""
+    if how == "turned" and which == "states":
+        return                                                                # one dimension
+    d = B.make_adamw_desc(dtype="f16", grad_dtype="f32", state_bits=8)
+    shapes = [(3, 4), (0,), (30, 50)]
+    lists = {"params": [torch.zeros(s).half() for s in shapes], "grads": [torch.zeros(s) for s in shapes], "masters": [torch.zeros(s) for s in shapes],
+             "states": [torch.zeros(B.adamw_state_bytes(d, math.prod(s)), dtype=torch.uint8) for s in shapes]}
+    made, only = B.adamw_tensors(d, **lists), B.adamw_tensors(d, grads=lists["grads"])
+    moved(lists[which][2], how)
+    message = which + r"\[2\] is no longer"
+    with pytest.raises(ValueError, match=message):
+        B.adamw(d, made)
+    if which == "grads":
+        for listed in (made, only):
+            with pytest.raises(ValueError, match=message):
+                B.grad_norm(listed, torch.zeros(2))
+
+
 def test_the_binding_checks_rows_against_the_descriptor(host_tensors):
     z = torch.zeros
     d = B.make_layernorm_desc(rows=4, cols=6, dtype="f32")
