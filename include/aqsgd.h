@@ -640,7 +640,8 @@ int aqsgd_set_launch_shape(int64_t max_blocks, int32_t dequant_unroll);
  * stamps `start_event` and `stop_event` (hipEvent_t created with timing enabled,
  * passed as void*; either may be NULL) with the kernel's own begin and end, so
  * hipEventElapsedTime(start, stop) is that launch's duration on the device.  A message
- * that takes two or three kernels (groups of more than 32768 elements) counts as one
+ * that takes two or three kernels (groups of more than 32768 elements), and a call of the linear
+ * layers, the layer norm or the weights' update that takes several, counts as one
  * launch: its first kernel's begin and its last one's end.  The request applies to one
  * launch, the first of an aqsgd_run_jobs call that makes several, and is then cleared.
  * Such a launch cannot be recorded into a HIP graph.

@@ -162,14 +162,23 @@ int aqsgd_adamw(const aqsgd_adamw_desc* d, const aqsgd_adamw_tensor* tensors, in
     a.correct = correct_factor(d->beta2, d->step);
     a.seed = d->rng_seed;
     a.key = d->rng_seed + static_cast<uint64_t>(d->step);
-    int32_t full = 0;                                       // tensors with elements: more than a table's take several launches
-    for (int32_t i = 0; i < n_tensors; ++i) full += tensors[i].n > 0;
-    std::optional<ProfileSpan> profile;
-    if (full > kTableTensors) profile.emplace();
-    const AdamwKind kind = {d->dtype, d->grad_dtype, d->state_bits, d->rounding};
-    UpdateTable table;                                      // entries behind the last tensor's are never looked at
     int held = 0;
     int64_t blocks = 0, groups = 0;
+    const auto fits = [&](int64_t more) { return held < kTableTensors && blocks + more <= kMaxBlocks; };
+    bool several = false;                                   // more tensors than a table's, or more workgroups than a grid's
+    for (int32_t i = 0; i < n_tensors && !several; ++i) {
+        const int64_t more = adamw_workgroups(tensors[i].n);
+        if (more == 0) continue;
+        several = !fits(more);
+        ++held;
+        blocks += more;
+    }
+    held = 0;
+    blocks = 0;
+    std::optional<ProfileSpan> profile;
+    if (several) profile.emplace();
+    const AdamwKind kind = {d->dtype, d->grad_dtype, d->state_bits, d->rounding};
+    UpdateTable table;                                      // entries behind the last tensor's are never looked at
     const auto send = [&] {
         for (int i = held; i < kTableTensors; ++i) table.first[i] = 0xffffffffu;
         const hipError_t err = launch_adamw(kind, table, static_cast<uint32_t>(blocks), a, static_cast<hipStream_t>(stream));
@@ -181,7 +190,7 @@ int aqsgd_adamw(const aqsgd_adamw_desc* d, const aqsgd_adamw_tensor* tensors, in
         const aqsgd_adamw_tensor& t = tensors[i];
         if (t.n == 0) continue;
         const int64_t more = adamw_workgroups(t.n);
-        if (held == kTableTensors || blocks + more > kMaxBlocks)
+        if (!fits(more))
             if (const hipError_t err = send(); err != hipSuccess) return status(err);
         table.first[held] = static_cast<uint32_t>(blocks);
         table.tensor[held] = {t.param, t.grad, static_cast<char*>(t.state), t.master, t.n, groups, t.weight_decay, decay_factor(d->lr, t.weight_decay)};
