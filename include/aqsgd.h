@@ -448,7 +448,7 @@ int aqsgd_ffn8_grad(const aqsgd_ffn8_desc* desc, const void* dh, const void* pre
  *   weight      in   [cols], or NULL for 1;  add in [rows, cols] dense, or NULL: the gradient that arrives along
  *               the residual stream
  *   dx          out  [rows, cols] dense; may be dy or add itself, and must not overlap an input otherwise (x itself: AQSGD_ERR_SHAPE)
- *   dweight     out  float[cols], or NULL;  dbias out float[cols], or NULL
+ *   dweight     out  float[cols], or NULL;  dbias out float[cols], or NULL; neither may overlap anything else of the call
  *   workspace   aqsgd_layernorm_grad_workspace_bytes() bytes of device memory, 16-byte aligned, free for other use
  *               once the call's work has run; NULL where that is 0 or neither dweight nor dbias is asked for
  * 0 rows: dweight and dbias are 0, or stay as they are with accumulate; nothing else is written.  codes are

@@ -141,3 +141,42 @@ def test_the_gradient_of_more_rows_than_a_grid_has_teams():
         sums_within(all_, terms * times, added_in_a_row(rows, cols, "f16"), each)
     del x, dy, dx
     torch.cuda.empty_cache()
+
+
+# ---- several results in their inputs' places at once -------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(7, 3), (5000, 200), (33, 1537), (200, 1600), (9, 5001), (300, 8200), (3, 16385), (2, 70001)])
+def test_sum_and_result_in_both_inputs_places(dtype, rows, cols):
+    """The sum in x's place and the result in the residual's, and the other way round: as with buffers of their own, bit for bit."""
+    x, res, w, b = (torch.from_numpy(v).cuda().to(B.DTYPE_NAME[dtype]) for v in G.inputs(rows, cols))
+    d = B.make_layernorm_desc(rows=rows, cols=cols, dtype=dtype)
+
+    def call(x, res, sum, y):
+        rest = [torch.empty(rows, device="cuda") for _ in range(3)] + [torch.empty((rows, R.stride(cols)), dtype=torch.int8, device="cuda")]
+        B.layernorm(d, x, residual=res, weight=w, bias=b, sum=sum, y=y, mean=rest[0], rstd=rest[1], row_scales=rest[2], row_codes=rest[3])
+        return [sum, y, *rest]
+
+    want = call(x, res, torch.empty_like(x), torch.empty_like(x))
+    for swapped in (False, True):
+        x1, res1 = x.clone(), res.clone()
+        for got, good in zip(call(x1, res1, *((res1, x1) if swapped else (x1, res1))), want):
+            assert torch.equal(got, good)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(7, 3), (7, 1600), (255, 1537), (700, 300), (1100, 9001), (1500, 40), (4097, 1600), (3, 16385), (2, 70001)])
+def test_the_gradient_in_the_place_of_a_gradient_that_is_added_too(dtype, rows, cols):
+    """dy, add and dx one buffer, with x a view of wider rows: as with buffers of their own, bit for bit."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    td = B.DTYPE_NAME[dtype]
+    x = torch.randn((rows, cols + 5), device="cuda", generator=g).to(td)[:, :cols]
+    dy, w = torch.randn((rows, cols), device="cuda", generator=g).to(td), torch.randn(cols, device="cuda", generator=g).to(td)
+    d = B.make_layernorm_desc(rows=rows, cols=cols, ld=cols + 5, dtype=dtype)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.layernorm(d, x, mean=mean, rstd=rstd)
+    want, got = ([torch.empty(cols, device="cuda") for _ in range(2)] for _ in range(2))
+    dx, one = torch.empty_like(dy), dy.clone()
+    B.layernorm_grad(d, dy, x, mean, rstd, dx, weight=w, add=dy, dweight=want[0], dbias=want[1])
+    B.layernorm_grad(d, one, x, mean, rstd, one, weight=w, add=one, dweight=got[0], dbias=got[1])
+    assert torch.equal(one, dx) and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
