@@ -18,6 +18,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
+import struct
 import threading
 import warnings
 from pathlib import Path
@@ -833,7 +834,7 @@ class AdamwTensors:
     weights, states and copies; ``places``: storage, offset and size of each.  A call looks whether each still lies there and refuses
     a list with one that has got other memory since (by ``t.data = ...``, ``set_`` or ``resize_``)."""
 
-    def __init__(self, array, kind: tuple, whole: bool, device: int, held, listed: tuple = (), places=None):
+    def __init__(self, array, kind: tuple, whole: bool, device: int, held, listed: tuple = (), places: bytes = b""):
         self.array, self.kind, self.whole, self.device, self.held = array, kind, whole, device, held
         self.listed, self.places = listed, places
 
@@ -884,17 +885,17 @@ def adamw_tensors(desc: AdamwDesc, *, grads, params=None, states=None, masters=N
         if a[0] + a[1] > b[0]:
             raise ValueError(f"{a[2]}[{a[3]}] and {b[2]}[{b[3]}] overlap")
     listed = (*grads, *(t for name in _LISTS[1:] for t in lists.get(name, ())))
-    places = (ctypes.c_uint64 * (3 * len(listed)))(*(n for t in listed for n in _place(t)))
+    places = b"".join(_place(t) for t in listed)
     return AdamwTensors(array, _kind_of(desc), whole, torch.cuda.current_device(), (grads, lists), listed, places)
 
 
 _LISTS = ("grads", "params", "states", "masters")
 
 
-def _place(t) -> tuple:
+def _place(t) -> bytes:
     """Where a tensor's elements are: its storage's address, its offset in there, their number; one of none is nowhere."""
     n = t.numel()
-    return (t.untyped_storage().data_ptr(), t.storage_offset(), n) if n else (0, 0, 0)
+    return struct.pack("3Q", *((t.untyped_storage().data_ptr(), t.storage_offset(), n) if n else (0, 0, 0)))
 
 
 def _check_tensors(tensors: AdamwTensors, grads_alone: bool = False) -> None:
@@ -903,7 +904,7 @@ def _check_tensors(tensors: AdamwTensors, grads_alone: bool = False) -> None:
     n = len(tensors)
     types = (_TORCH_OF_CODE[tensors.kind[1]], _TORCH_OF_CODE[tensors.kind[0]], torch.uint8, torch.float32)
     for i, t in enumerate(tensors.listed[:n] if grads_alone else tensors.listed):
-        if t.dtype != types[i // n] or not t.is_contiguous() or tensors.places[3 * i:3 * i + 3] != list(_place(t)):
+        if t.dtype != types[i // n] or not t.is_contiguous() or tensors.places[24 * i:24 * i + 24] != _place(t):
             raise ValueError(f"{_LISTS[i // n]}[{i % n}] is no longer what or where it was when the list was made")
 
 

@@ -503,32 +503,30 @@ public:
     ~List() {
         if (held_) PyBuffer_Release(&view_);
         Py_XDECREF(kind_);
-        if (places_held_) PyBuffer_Release(&places_view_);
         Py_XDECREF(tensors_);
         Py_XDECREF(places_);
     }
     // Whether the tensors, or the gradients alone, still are what and where they were when the list was made.  By the tensors' fields:
     // 2 ns a tensor, by their methods 4 (64 weights with gradients and states: 0.3 us of a call's 4.7).
-    bool in_place(bool grads_alone) {
+    bool in_place(bool grads_alone) const {
         c10::ScalarType type[4] = {c10::ScalarType::Float, c10::ScalarType::Float, c10::ScalarType::Byte, c10::ScalarType::Float};
         if (!known_type(static_cast<int32_t>(kind(1)), type[0]) || !known_type(static_cast<int32_t>(kind(0)), type[1]) || !tensors_ || !places_ ||
-            !PyTuple_CheckExact(tensors_) || PyObject_GetBuffer(places_, &places_view_, PyBUF_SIMPLE) != 0) {
-            PyErr_Clear();
+            !PyTuple_CheckExact(tensors_) || !PyBytes_CheckExact(places_))
             return false;
-        }
-        places_held_ = true;
         const Py_ssize_t n = count(), all = PyTuple_GET_SIZE(tensors_);
-        if (places_view_.len != static_cast<Py_ssize_t>(sizeof(Place)) * all || all < n || all > 4 * n) return false;
-        const auto* place = static_cast<const Place*>(places_view_.buf);
+        if (PyBytes_GET_SIZE(places_) != static_cast<Py_ssize_t>(sizeof(Place)) * all || all < n || all > 4 * n) return false;
+        const char* at = PyBytes_AS_STRING(places_);
         for (Py_ssize_t first = 0; first < (grads_alone ? n : all); first += n)
             for (Py_ssize_t i = first; i < first + n && i < all; ++i) {
+                Place place;
+                std::memcpy(&place, at + i * static_cast<Py_ssize_t>(sizeof place), sizeof place);
                 PyObject* o = PyTuple_GET_ITEM(tensors_, i);
                 if (!THPVariable_CheckExact(o) && !THPVariable_Check(o)) return false;
                 const c10::TensorImpl* t = THPVariable_Unpack(o).unsafeGetTensorImpl();
-                if (t->numel() != place[i].elements || c10::typeMetaToScalarType(t->dtype()) != type[first / n]) return false;
-                if (place[i].elements == 0) continue;
+                if (t->numel() != place.elements || c10::typeMetaToScalarType(t->dtype()) != type[first / n]) return false;
+                if (place.elements == 0) continue;
                 c10::StorageImpl* storage = t->unsafe_storage().unsafeGetStorageImpl();
-                if (!storage || reinterpret_cast<uint64_t>(storage->mutable_data()) != place[i].storage || t->storage_offset() != place[i].offset ||
+                if (!storage || reinterpret_cast<uint64_t>(storage->mutable_data()) != place.storage || t->storage_offset() != place.offset ||
                     !t->is_contiguous_default(at::MemoryFormat::Contiguous))
                     return false;
             }
@@ -547,9 +545,8 @@ private:
         if (!v) PyErr_Clear();
         return v;
     }
-    Py_buffer view_, places_view_;
+    Py_buffer view_;
     PyObject *kind_ = nullptr, *tensors_ = nullptr, *places_ = nullptr;
-    bool places_held_ = false;
     bool held_ = false, ok_ = false;
 };
 
