@@ -684,12 +684,12 @@ __global__ __launch_bounds__(kFewLanes) void layernorm_grad_few_kernel(const Lay
     const float each = 1.0f / static_cast<float>(a.cols);
     const int64_t stride = static_cast<int64_t>(gridDim.x - column_blocks) * kTeams;
     int turn = 0;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x - column_blocks) * kTeams; first < a.rows; first += stride, turn ^= 1) {
-        // A team of one wave waits for nobody and may leave; of several, all go on to team_sums' barrier, one without a row with
-        // the last row again: what it reads there, dx perhaps over dy by then, is not used.
-        const bool here = first + team < a.rows;
-        if (TEAM <= kWave && !here) break;
-        const int64_t row = here ? first + team : a.rows - 1;
+    // A team of one wave goes by its own rows and waits for nobody.  Of several waves, all go on to team_sums' barrier, a team without a row
+    // with the last one again: what it reads there, dx perhaps over dy by then, is not used.
+    constexpr bool kAlone = TEAM <= kWave;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x - column_blocks) * kTeams + (kAlone ? team : 0); first < a.rows; first += stride, turn ^= 1) {
+        const bool here = kAlone || first + team < a.rows;
+        const int64_t row = kAlone ? first : here ? first + team : a.rows - 1;
         GradRow<DT, TEAM, CPL> now;
         now.ask(a, row, lane);
         u32x4_t w[CPL];
