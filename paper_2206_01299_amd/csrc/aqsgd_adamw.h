@@ -1,15 +1,16 @@
 // Kernels of aqsgd_adamw: one step of many tensors in one launch.
 //
 // Every element is read and written once, past the caches.  With states in 32 bits memory bounds the step: 30.7 M float16
-// weights with binary32 copies and gradients 153 us, 6.0 TB/s.  In 8 bits what is moved halves and the arithmetic doubles (a root and a
-// quotient for the step, two roots for the codes): 123 M such weights 359 us, 6.2 TB/s, but 28.3 M bfloat16 ones without
-// copies 74 us, 3.9 TB/s, and 83 with draws, where vector instructions are what bounds it.
+// weights with binary32 copies and gradients 154 us, 6.0 TB/s.  In 8 bits what is moved halves and the arithmetic doubles (a root and a
+// quotient for the step, two roots for the codes): 123 M such weights 362 us, 6.1 TB/s, with vector instructions in 90 % of the cycles, and
+// 28.3 M bfloat16 ones without copies 75 us, 3.8 TB/s, or 84 with draws, where it is they that bound it (95 %).
 //
 // Lanes take four neighbouring elements at a time, so that binary32 accesses are contiguous.  With states in 8 bits half a wave
 // takes a group in two such pieces: what a lane does once for its group (four quotients, two maxima over the lanes) is shared by eight
-// elements (28.3 M bfloat16 weights 77 us, with a wave to a group and four elements a lane 110).  Root and quotient by a step from the
-// hardware's reciprocals, where a vote says that their ranges allow it: with draws 83 us, by the compiler's quotient 87.  Everything stays in
-// registers between the loads and the stores.  A workgroup's tensor is found in the launch's table by one load and a vote of the wave.
+// elements (28.3 M bfloat16 weights 110 us with a wave to a group and four elements a lane, 77 so, before the next step).  Root and quotient
+// by a step from the hardware's reciprocals, where a vote says that their ranges allow it: with draws 83 us, 87 by the compiler's quotient.
+// Everything stays in registers between the loads and the stores.  A workgroup's tensor is found in the launch's table by one load and a
+// vote of the wave.
 #pragma once
 
 #include "aqsgd_norms.h"

@@ -2,8 +2,8 @@
 //
 // Both read a row once into the registers of a team of lanes (a fraction of a wave, a wave, or a workgroup of up to
 // 1024), which forms the row's sums between the load and the store.  What bounds them is memory, and in small calls a launch and
-// one chain of load, two sums and store: one row of 1600 float16 3.0 us, 4096 such rows with residual, codes and statistics 12.2 (4.8
-// TB/s), 16384 of 4096 float32 96 (5.6 TB/s); their gradients 2.6, 16.6 and 188.  The forward pass sums in
+// one chain of load, two sums and store: one row of 1600 float16 2.9 us, 4096 such rows with residual, codes and statistics 12.0 (4.9
+// TB/s), 16384 of 4096 float32 96 (5.6 TB/s); their gradients 2.4, 16.4 and 189.  The forward pass sums in
 // binary64, which costs little here: statistics then depend on the order, and with it on the launch, only where a sum's last places in
 // binary64 decide how it rounds to binary32.  Lanes take pieces of 16 bytes side by side.
 #pragma once
@@ -480,9 +480,13 @@ struct GradPlan {
     int64_t blocks;                       // workgroups, and sums of each column
 };
 
-// Both ways (us, by blocks and by columns): 1024 x 1600 float16 10.7 and 7.3, 1400 x 1600 11.2 and 9.3, 2048 x 1600 11.7 and 12.7; 1280 x 400 6.8
-// and 5.8, 2048 x 400 7.2 and 8.5; 1100 x 768 bfloat16 7.3 and 7.8; 1400 x 4096 float32 23.8 and 22.6, 2048 x 4096 32.2 and 32.9; 2048 x 5120 bfloat16
-// 30.0 and 25.3, 2048 x 8192 43.9 and 33.2, 6000 x 8192 86 and 94.  Without sums rows alone are left, which blocks would only hold up.
+// Up to how many rows the columns go by workgroups of their own.  By blocks costs the join's launch, 4 us; by columns the second read,
+// which grows with the rows and is shared by a workgroup for every 32 to 128 bytes of a row.  So the limit is where the read has
+// become the longer one: lower for 65 to 128 pieces, whose 17 to 32 workgroups take 64 bytes of every row each, and higher for wide 16-bit rows, which have more
+// than 64 of them and go one at a time through a workgroup of the blocks.  It is fitted (us, by blocks and by columns): 1024 x 1600 float16 10.7 and 7.3, 1400 x 1600 11.2 and 9.3, 2048 x 1600 11.7 and 12.7; 1280 x 400
+// 6.8 and 5.8, 2048 x 400 7.2 and 8.5; 1100 x 768 bfloat16 7.3 and 7.8; 1400 x 4096 float32 23.8 and 22.6, 2048 x 4096 32.2 and 32.9; 2048 x 5120
+// bfloat16 30.0 and 25.3, 2048 x 8192 43.9 and 33.2, 6000 x 8192 86 and 94; and misses 1280 x 768 float32, 9.0 and 9.4, and 3000 x 8192
+// bfloat16, 54 and 49.  Without sums rows alone are left, which blocks would only hold up.
 template <int DT>
 inline int64_t most_rows_by_columns(int64_t pieces) {
     return DT != AQSGD_F32 && pieces > kGradLanes / 2 ? 2048 : pieces > 64 && pieces <= 128 ? 1024 : 1408;
